@@ -399,6 +399,91 @@ int qift_kv4_attention_decode(const float* q, const uint8_t* k_codes, const floa
                               int Hq, int Hkv, int D, float* out, void* workspace, size_t workspace_bytes,
                               void* stream);
 
+/* KV4 of many requests: a pool of pages, ragged batches, drafted token trees.  (The paper fixes the quantizer, Sec. 4.1;
+ * pages, batches and trees are what serving it takes.)
+ *
+ * The pool (device memory, owned by the caller) is num_pages pages of qift_kv4_page_bytes(page_tokens, H, D) bytes:
+ * [H][page_tokens / 32] blocks of 4416 bytes, each 32 consecutive tokens of one KV head, 138 bytes a token:
+ *      0  key codes      16-byte pieces, piece ((n 4 + cq) 8 + (g ^ 2cq)) for token 8n + g: dimensions 32cq .. 32cq + 31, 4 bits
+ *                        each, ascending from the low bits of the first byte          (n, cq 0..3, g 0..7)
+ *   2048  value codes    16-byte pieces, piece ((w 4 + cq) 8 + (g ^ 2cq)); byte 4n + 2h of it (16 bits) for token 8n + 2cq + h:
+ *                        dimensions 32w + 4g .. + 3, ascending                        (w, cq, n 0..3, g 0..7, h 0..1)
+ *   4096 / 4224  fp32 scales of the keys / values by token     4352 / 4384  their zero-points, one byte by token
+ * value = scale * (code - zero), quantized exactly as qift_kv4_quantize does it (a range so small that its scale would round to 0
+ * counts as empty).  D must be 128; page_tokens is a multiple of
+ * 32, 32 .. 1024.  Every byte belongs to one token.
+ *
+ * A call takes `total` rows that R requests share:
+ *   row_start   [R + 1] int32, ascending: request r has rows row_start[r] .. row_start[r + 1] - 1 (possibly none); rows from
+ *               row_start[R] on belong to nobody: nothing of them is read or written
+ *   first       [R] int32: the cache position of the request's first row (= its cached tokens before this call)
+ *   page_table  [R][max_pages] int32: the page that holds positions i * page_tokens .. of a request.  Entries that are not
+ *               0 .. num_pages - 1 are no pages, and positions before 0 or from max_pages * page_tokens on have none: such
+ *               tokens are not written, not moved, seen by nobody, and their rows of a read are left as they were.
+ * Requests may share pages that are read; a position that two requests write in one call, or that one call writes twice, ends up
+ * with the bytes of either.  All four calls read these arrays on the device, in stream order: they can be captured into a graph
+ * and replayed with other contents (the same total, R and max_pages).
+ *
+ * qift_kv4_paged_write: quantizes the rows' keys and values into the cache.
+ *   K, V        in  [total][H][D] fp32 or bf16; rows are k_stride / v_stride elements apart (>= H * D, whole 16-byte units)
+ *   k_had_block, v_had_block   as had_block of qift_kv4_quantize, for keys and values;  clip_ratio in (0, 1]
+ *
+ * qift_kv4_paged_read: the reverse for positions first .. of the rows: scale * (code - zero) in fp32, rotated back
+ *   K, V        out [total][H][D] fp32 or bf16 (rounded once), strides as above; one of them may be NULL
+ *
+ * qift_kv4_paged_keep: after the check of a drafted tree that was written at positions first ..: position first + i takes the
+ * token at first + keep[row_start[r] + i], i = 0 .. kept_start[r + 1] - kept_start[r] - 1 (at most the request's rows).
+ *   keep        [total] int32, ascending within a request (the accepted path); indices outside its rows move nothing
+ *   kept_start  [R + 1] int32: the row_start of a batch of the kept tokens alone
+ *
+ * qift_kv4_paged_attention: out[row][h] = sum_t softmax_t(scale * q[row][h] . K[t]) V[t] for KV head h / (Hq / H), over the
+ * positions that the row sees: all before `first`, and of the drafted ones first + j (written before the call) those whose
+ * bit j & 31 of mask[row][j / 32] is set -- its ancestors and itself, for a tree.  A row that sees nothing gets zeros.
+ *   q           in  [total][Hq][D] fp32 or bf16, rows q_stride elements apart (>= Hq * D, whole 16-byte units);
+ *               out has its type, [total][Hq][D] contiguous
+ *   q_had_block the rotation of the keys, applied to the query in the call;  scale > 0, or 0 for 1 / sqrt(D)
+ *   mask        [total][mask_words] int32, mask_words 1 .. 32 (drafted tokens beyond its bits are not seen), or NULL: a row sees
+ *               the drafted tokens up to itself
+ *   Hq / H      1 .. 64
+ *   workspace   >= qift_kv4_paged_attention_workspace_bytes(total, R, Hq, H) bytes.  It may be shared by calls that follow
+ *               one another in a stream, captured or not, and needs no initial contents
+ *   fp32 calls keep fp32 accuracy; bf16 calls hold the rotated query and the weights in 16 bits (fp16) beside exact codes,
+ *   with fp32 scores, sums and results.
+ * Errors: INVALID_ARG (null pointer, sizes <= 0, mask_words, scale, clip_ratio, dtype), UNSUPPORTED_SHAPE (D != 128, page_tokens,
+ * had_block, Hq / H, strides), ALIGNMENT (arrays of codes and rows 16 bytes, int32 arrays 4), WORKSPACE, CUDA. */
+size_t qift_kv4_page_bytes(int page_tokens, int H, int D);
+int qift_kv4_paged_write(const void* K, const void* V, int x_dtype, long long k_stride, long long v_stride, int total, int H, int D,
+                         int k_had_block, int v_had_block, float clip_ratio, const int32_t* row_start, const int32_t* first, int R,
+                         const int32_t* page_table, int max_pages, void* pool, int num_pages, int page_tokens, void* stream);
+int qift_kv4_paged_read(void* K, void* V, int x_dtype, long long k_stride, long long v_stride, int total, int H, int D,
+                        int k_had_block, int v_had_block, const int32_t* row_start, const int32_t* first, int R,
+                        const int32_t* page_table, int max_pages, const void* pool, int num_pages, int page_tokens, void* stream);
+int qift_kv4_paged_keep(const int32_t* keep, const int32_t* kept_start, int total, int H, int D, const int32_t* row_start,
+                        const int32_t* first, int R, const int32_t* page_table, int max_pages, void* pool, int num_pages,
+                        int page_tokens, void* stream);
+size_t qift_kv4_paged_attention_workspace_bytes(int total, int R, int Hq, int H);
+int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int total, int Hq, int H, int D, int q_had_block,
+                             float scale, const int32_t* mask, int mask_words, const int32_t* row_start, const int32_t* first, int R,
+                             const int32_t* page_table, int max_pages, const void* pool, int num_pages, int page_tokens, void* out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Low-rank adapters of many requests beside a shared projection (whose product is any of the linear calls above):
+ *     out[m] = y[m] + scaling[a] * B[a] (A[a] x[m]),   a = adapter[r] of the request r that row m belongs to
+ *   X           in  [M][K] fp32 or bf16, the projection's input before its rotation; K % 8 == 0
+ *   A, B        in  bf16 [adapters][rank][K] and [adapters][N][rank]; rank a multiple of 8, 8 .. 128 (pad with zeros); N % 8 == 0
+ *   scaling     in  fp32 [adapters]
+ *   row_start   [R + 1] int32, ascending; rows before row_start[0] and from row_start[R] on belong to nobody and keep their `out`
+ *   adapter     [R] int32; values that are not 0 .. adapters - 1: no adapter, out = y
+ *   y           in  [M][N], or NULL for zeros;  out [M][N], may be y itself; both of X's type
+ *   workspace   >= qift_lora_workspace_bytes(M, rank, K) bytes, as for the attention
+ * Sums in fp32; the small product A x is kept in fp32; fp32 inputs are multiplied at (at least) 16-bit precision in two exact
+ * parts.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (K, N, rank), ALIGNMENT, WORKSPACE, CUDA. */
+size_t qift_lora_workspace_bytes(int M, int rank, int K);
+int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16_t* B, const float* scaling, int adapters, int rank,
+                     int M, int N, int K, const int32_t* row_start, const int32_t* adapter, int R, const void* y, void* out,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
 /* Quantizer diagnostics (not on the inference path).  Sec. 3.3 (list of evaluated grids), Sec. 4.5.1
  * (bucket diagnostic), Sec. 4.5.2 (scale-invariant ratio scan).
  *

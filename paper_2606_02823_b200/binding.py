@@ -30,6 +30,8 @@ EXPORTS = [
     "qift_group_plan_bytes", "qift_group_plan", "qift_group_quantize_act", "qift_group_linear", "qift_group_forward",
     "qift_group_forward_host", "qift_static_scratch_bytes", "qift_w2a4_linear_static",
     "qift_kv4_quantize", "qift_kv4_attention_workspace_bytes", "qift_kv4_attention_decode",
+    "qift_kv4_page_bytes", "qift_kv4_paged_write", "qift_kv4_paged_read", "qift_kv4_paged_keep",
+    "qift_kv4_paged_attention_workspace_bytes", "qift_kv4_paged_attention", "qift_lora_workspace_bytes", "qift_lora_linear",
     "qift_expand_weights", "qift_expanded_linear",
     "qift_diag_grid_quantize", "qift_diag_bucket_stats", "qift_diag_ratio_scan_workspace_bytes", "qift_diag_ratio_scan",
     "qift_selftest_wait_timeout", "qift_levels_bytes", "qift_forward_multi_scratch_bytes", "qift_forward_multi",
@@ -92,6 +94,19 @@ def lib() -> ctypes.CDLL:
         L.qift_kv4_attention_workspace_bytes.restype = sz
         L.qift_kv4_attention_workspace_bytes.argtypes = [ci, ci, ci]
         L.qift_kv4_attention_decode.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, sz, vp]
+        ll = ctypes.c_longlong
+        pages = [vp, vp, ci, vp, ci, vp, ci, ci]   # row_start, first, R, page_table, max_pages, pool, num_pages, page_tokens
+        L.qift_kv4_page_bytes.restype = sz
+        L.qift_kv4_page_bytes.argtypes = [ci, ci, ci]
+        L.qift_kv4_paged_write.argtypes = [vp, vp, ci, ll, ll, ci, ci, ci, ci, ci, cf] + pages + [vp]
+        L.qift_kv4_paged_read.argtypes = [vp, vp, ci, ll, ll, ci, ci, ci, ci, ci] + pages + [vp]
+        L.qift_kv4_paged_keep.argtypes = [vp, vp, ci, ci, ci] + pages + [vp]
+        L.qift_kv4_paged_attention_workspace_bytes.restype = sz
+        L.qift_kv4_paged_attention_workspace_bytes.argtypes = [ci, ci, ci, ci]
+        L.qift_kv4_paged_attention.argtypes = [vp, ci, ll, ci, ci, ci, ci, ci, cf, vp, ci] + pages + [vp, vp, sz, vp]
+        L.qift_lora_workspace_bytes.restype = sz
+        L.qift_lora_workspace_bytes.argtypes = [ci, ci, ci]
+        L.qift_lora_linear.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, ci, vp, vp, vp, sz, vp]
         L.qift_diag_grid_quantize.argtypes = [vp, ci, ci, vp, ci, vp, vp, vp]
         L.qift_diag_bucket_stats.argtypes = [vp, vp, ci, ci, vp, vp, ci, vp, vp, vp]
         L.qift_diag_ratio_scan_workspace_bytes.restype = sz
@@ -112,6 +127,7 @@ def lib() -> ctypes.CDLL:
             if name not in ("qift_diag_ratio_scan_workspace_bytes", "qift_status_string", "qift_packed_bytes", "qift_workspace_bytes",
                             "qift_forward_scratch_bytes", "qift_group_plan_bytes", "qift_static_scratch_bytes",
                             "qift_workspace_bytes_route", "qift_kv4_attention_workspace_bytes", "qift_levels_bytes",
+                            "qift_kv4_page_bytes", "qift_kv4_paged_attention_workspace_bytes", "qift_lora_workspace_bytes",
                             "qift_forward_multi_scratch_bytes", "qift_linear_multi_workspace_bytes"):
                 getattr(L, name).restype = ci
         _lib = L
@@ -558,6 +574,163 @@ def qift_kv4_attention_decode(q, K: Kv4Cache, V: Kv4Cache, T: int, out=None, wor
     _check(lib().qift_kv4_attention_decode(_ptr(q), _ptr(K.codes), _ptr(K.scale), _ptr(K.zero), _ptr(V.codes), _ptr(V.scale),
                                            _ptr(V.zero), T, K.T_cap, Hq, K.H, D, _ptr(_dev(out, torch.float32)),
                                            _ptr(workspace), workspace.numel(), _stream()), "qift_kv4_attention_decode")
+    return out
+
+
+# ---------------------------------------------------------------------------------------- KV4 of many requests
+KV_BLOCK_TOKENS, KV_BLOCK_BYTES = 32, 4416
+
+
+def _call(t, name, *args):
+    """Calls an entry point on the current stream of the tensors' device (which need not be the current one)."""
+    if t.device.index == torch.cuda.current_device():
+        rc = getattr(_lib or lib(), name)(*args, _stream())
+    else:
+        with torch.cuda.device(t.device):
+            rc = getattr(_lib or lib(), name)(*args, _stream())
+    if rc != OK:
+        raise QiftError(rc, name)
+
+
+def _same_device(t, *others):
+    for o in others:
+        assert o is None or o.device == t.device, f"tensors on {t.device} and {o.device}"
+
+
+def _float_type(t):
+    assert t.dtype in (torch.float32, torch.bfloat16), f"expected float32 or bfloat16, got {t.dtype}"
+    return F32 if t.dtype == torch.float32 else BF16
+
+
+def _rows(t, heads=None):
+    """[total, heads, D] rows whose heads are contiguous; the rows may be strided (a slice of a wider projection)."""
+    assert t.is_cuda and t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2], "expected CUDA rows [total, heads, D]"
+    assert heads is None or t.shape[1] == heads, f"expected {heads} heads, got {t.shape[1]}"
+    # a single row has no distance to the next one: any valid stride does
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+class Kv4Pages:
+    """A pool of KV4 pages, uint8 [num_pages, H, page_tokens / 32 * 4416], and the page table int32 [R, max_pages] of the
+    requests of a batch (the layout is described in include/qift.h)."""
+
+    def __init__(self, pool, page_table, page_tokens: int):
+        _dev(pool, torch.uint8), _dev(page_table, torch.int32), _same_device(pool, page_table)
+        assert pool.dim() == 3 and page_table.dim() == 2
+        assert pool.shape[2] * KV_BLOCK_TOKENS == page_tokens * KV_BLOCK_BYTES, "the pool's last dimension is page_tokens / 32 * 4416 bytes"
+        self.pool, self.page_table, self.page_tokens = pool, page_table, page_tokens
+        self.num_pages, self.H = pool.shape[0], pool.shape[1]
+        self.R, self.max_pages = page_table.shape
+
+    @classmethod
+    def empty(cls, num_pages: int, H: int, page_tokens: int, page_table):
+        pool = torch.zeros((num_pages, H, page_tokens // KV_BLOCK_TOKENS * KV_BLOCK_BYTES), dtype=torch.uint8, device=page_table.device)
+        return cls(pool, page_table, page_tokens)
+
+    def _batch(self, row_start, first):
+        _dev(row_start, torch.int32), _dev(first, torch.int32), _same_device(self.pool, row_start, first)
+        assert row_start.numel() == self.R + 1 and first.numel() == self.R, "row_start has R + 1 entries, first R, like the page table"
+        return (_ptr(row_start), _ptr(first), self.R, _ptr(self.page_table), self.max_pages, _ptr(self.pool), self.num_pages,
+                self.page_tokens)
+
+
+def qift_kv4_page_bytes(page_tokens: int, H: int, D: int = 128) -> int:
+    return int(lib().qift_kv4_page_bytes(page_tokens, H, D))
+
+
+def qift_kv4_paged_write(K, V, pages: Kv4Pages, row_start, first, k_had_block: int = 0, v_had_block: int = 0, clip_ratio: float = 0.95):
+    """K, V fp32 or bf16 [total, H, D] -> quantized into positions first[r] .. of each request's pages."""
+    _same_device(pages.pool, K, V)
+    assert K.dtype == V.dtype and K.shape == V.shape
+    ks, vs = _rows(K, pages.H), _rows(V, pages.H)
+    _call(K, "qift_kv4_paged_write", _ptr(K), _ptr(V), _float_type(K), ks, vs, K.shape[0], pages.H, K.shape[2], k_had_block,
+          v_had_block, clip_ratio, *pages._batch(row_start, first))
+
+
+def qift_kv4_paged_read(pages: Kv4Pages, row_start, first, total: int, dtype=torch.float32, k_had_block: int = 0, v_had_block: int = 0,
+                        K=None, V=None):
+    """-> (K, V) [total, H, 128]: what positions first[r] .. of each request hold, rotated back.  Rows of no request (and
+    positions without a page) are left as they are in K and V where those are given."""
+    if K is None:
+        K = torch.empty((total, pages.H, 128), dtype=dtype, device=pages.pool.device)
+    if V is None:
+        V = torch.empty((total, pages.H, 128), dtype=dtype, device=pages.pool.device)
+    _same_device(pages.pool, K, V)
+    assert K.dtype == V.dtype and K.shape == V.shape and K.shape[0] == total
+    ks, vs = _rows(K, pages.H), _rows(V, pages.H)
+    _call(K, "qift_kv4_paged_read", _ptr(K), _ptr(V), _float_type(K), ks, vs, total, pages.H, K.shape[2], k_had_block, v_had_block,
+          *pages._batch(row_start, first))
+    return K, V
+
+
+def qift_kv4_paged_keep(pages: Kv4Pages, row_start, first, keep, kept_start):
+    """After the check of drafted trees at first[r] ..: position first[r] + i takes the token at first[r] + keep[row_start[r] + i]
+    for the kept_start[r + 1] - kept_start[r] accepted tokens of each request (ascending indices)."""
+    _dev(keep, torch.int32), _dev(kept_start, torch.int32), _same_device(pages.pool, keep, kept_start)
+    assert kept_start.numel() == pages.R + 1
+    _call(keep, "qift_kv4_paged_keep", _ptr(keep), _ptr(kept_start), keep.numel(), pages.H, 128, *pages._batch(row_start, first))
+
+
+def qift_kv4_paged_attention_workspace_bytes(total: int, R: int, Hq: int, H: int) -> int:
+    return int(lib().qift_kv4_paged_attention_workspace_bytes(total, R, Hq, H))
+
+
+def qift_kv4_paged_attention(q, pages: Kv4Pages, row_start, first, mask=None, q_had_block: int = 0, scale: float = 0.0, out=None,
+                             workspace=None):
+    """q fp32 or bf16 [total, Hq, D] -> out of the same shape and type: the attention of each row over its request's cached tokens
+    before first[r] and the drafted ones that mask (int32 [total, words], bit j: drafted token j) lets it see; without a mask,
+    those up to itself."""
+    Hq, D = q.shape[1], q.shape[2]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    qs = _rows(q)
+    _dev(out, q.dtype), _same_device(pages.pool, q, out, mask)
+    assert out.shape == q.shape
+    words = 0
+    if mask is not None:
+        _dev(mask, torch.int32)
+        assert mask.dim() == 2 and mask.shape[0] == q.shape[0]
+        words = mask.shape[1]
+    if workspace is None:
+        need = (_lib or lib()).qift_kv4_paged_attention_workspace_bytes(q.shape[0], pages.R, Hq, pages.H)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    _same_device(q, workspace)
+    _call(q, "qift_kv4_paged_attention", _ptr(q), _float_type(q), qs, q.shape[0], Hq, pages.H, D, q_had_block, scale, _ptr(mask),
+          words, *pages._batch(row_start, first), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size())
+    return out
+
+
+# ---------------------------------------------------------------------------------------- adapters of many requests
+def qift_lora_workspace_bytes(M: int, rank: int, K: int) -> int:
+    return int(lib().qift_lora_workspace_bytes(M, rank, K))
+
+
+def qift_lora_linear(x, A, B, scaling, row_start, adapter, y=None, out=None, workspace=None):
+    """x fp32 or bf16 [M, K], A bf16 [adapters, rank, K], B bf16 [adapters, N, rank], scaling fp32 [adapters], adapter int32 [R] ->
+    out [M, N] of x's type: y + scaling[a] * B[a] (A[a] x) for the rows row_start[r] .. of each request and its adapter a (none
+    where it is negative).  y (None: zeros) is the shared projection's product; out may be y."""
+    _dev(x), _dev(A, torch.bfloat16), _dev(B, torch.bfloat16), _dev(scaling, torch.float32)
+    _dev(row_start, torch.int32), _dev(adapter, torch.int32)
+    M, K = x.shape
+    n, rank = A.shape[0], A.shape[1]
+    N = B.shape[1]
+    assert A.shape == (n, rank, K) and B.shape == (n, N, rank) and scaling.numel() == n
+    R = adapter.numel()
+    assert row_start.numel() == R + 1
+    if y is not None:
+        _dev(y, x.dtype)
+        assert y.shape == (M, N)
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    else:
+        _dev(out, x.dtype)
+        assert out.shape == (M, N)
+    if workspace is None:
+        need = (_lib or lib()).qift_lora_workspace_bytes(M, rank, K)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=x.device)
+    _same_device(x, A, B, scaling, row_start, adapter, y, out, workspace)
+    _call(x, "qift_lora_linear", _ptr(x), _float_type(x), _ptr(A), _ptr(B), _ptr(scaling), n, rank, M, N, K, _ptr(row_start),
+          _ptr(adapter), R, _ptr(y), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size())
     return out
 
 

@@ -1,0 +1,657 @@
+// Attention of drafted token trees over the paged KV4 cache.
+//
+// The rows of a request that one KV head serves are its n drafted tokens times the G query heads of the head, in tiles of ROWS.  A
+// work item is one 32-token block for one (request, KV head, row tile); the items of the whole call, in that order, are dealt to
+// the warps of the grid in equal contiguous runs, whatever the requests' lengths.  A warp works alone: its own ring of blocks in
+// shared memory (one 4416-byte bulk copy each), its own running maximum, sum and numerator.  A tile that lies within one warp's run
+// is finished there; the pieces of the others go to the workspace -- a warp has at most two, its first and its last -- and the
+// second kernel joins them, one CTA for the tile that begins in a warp and ends in a later one.
+//
+// Both products run on mma.sync.m16n8k16 (fp16, fp32 sums) with the query rows as A:
+//   S[row][token] = sum_d q[row][d] kc[token][d],        O[row][d] += sum_t w[row][t] vc[t][d],  w = p * vs.
+// A code c in the low mantissa bits of an fp16 number is the subnormal c * 2^-24, exactly: `word & 0x000f000f` IS a pair of
+// operands, `word & 0x00f000f0` one of 16 c * 2^-24 (the 16 is taken out of the query, and out of the result).  Zero-points enter
+// as one more k-step (query sums against key zeros) and one more column tile (weights against value zeros), so they cancel
+// against the same rounded operands.
+//   q is scaled by a power of two per row (largest value 2^7 .. 2^8) and held in fp16: exact for bf16 queries that are not
+//   rotated, else off by 2^-12.  fp32 calls hold q and w in two fp16 parts each (residual 2^-22), rows g and g + 8 of the same
+//   instruction, and their value codes lessened by 8 (1024 + c - 1032 in fp16, exact): the sums of an average over many tokens
+//   would otherwise be far larger than the result and lose what the zero-points take away.  w is normalised by the largest value scale seen so far (a power of two, one for the warp) and by the row's
+//   reference point, which moves only when a score exceeds it by more than kTreeSlack.
+#pragma once
+
+#include "kv4_paged.cuh"
+
+namespace qift {
+
+struct KvTreeParams {
+    KvPages pages;
+    KvRows rows;
+    const void* q;           // [total][Hq][128], rows q_stride elements apart
+    void* out;               // [total][Hq][128], contiguous
+    const int32_t* mask;     // [total][mask_words] or nullptr: a drafted token sees the drafted ones up to itself
+    int mask_words;
+    long long q_stride;
+    int Hq, G;               // query heads, query heads per KV head
+    int q_had;
+    float q_inv_sqrt, scale_log2;   // score scale times log2(e)
+    int4* desc;              // [warps]: tile that begins in this warp's run and ends in a later one's: request, head, tile, pieces
+    float* partial;          // [2 * warps][ROWS][kTreeRow]
+};
+
+constexpr int kTreeRow = 132;        // floats of a row's piece: numerator, reference point, sum, two unused
+constexpr int kTreeMinRun = 2;       // items of a warp's run at least
+constexpr float kTreeSlack = 6.0f;   // binary orders that a weight may exceed its reference by: w * 2^8 stays below 2^14
+constexpr int kTreeSite = 48;        // site of an expired wait
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t lessened(uint32_t x, uint32_t by) {   // fp16 pairs, x + by
+    uint32_t y;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(by));
+    return y;
+}
+
+// What a call makes of a request.
+struct TreeRequest {
+    int n, first, len, blocks, tiles;   // drafted tokens, cached before them, positions in all, blocks and row tiles (0 without rows)
+};
+template <int ROWS>
+__device__ __forceinline__ TreeRequest tree_request(const KvTreeParams& p, int r, int capacity) {
+    TreeRequest q;
+    q.n = p.rows.count(r), q.first = p.rows.first[r];
+    const long long end = static_cast<long long>(q.first) + q.n;
+    q.len = static_cast<int>(max(0ll, min(end, static_cast<long long>(capacity))));
+    q.blocks = q.n > 0 ? max(1, (q.len + kPgTokens - 1) / kPgTokens) : 0;   // rows over nothing still get their zeros
+    q.tiles = (q.n * p.G + ROWS - 1) / ROWS;
+    return q;
+}
+
+template <bool BF16, int ROWS>
+struct TreeShape {
+    static constexpr bool kSplit = !BF16;                      // operands in two parts, rows g and g + 8
+    static constexpr int kMT = kSplit ? ROWS / 8 : (ROWS + 15) / 16;
+    static constexpr bool kHalf = BF16 && ROWS == 8;           // rows g + 8 unused
+    static constexpr int kLR = (kSplit || kHalf) ? 1 : 2;      // logical rows of a lane per m-tile
+    static constexpr int kWarps = kMT == 1 ? 12 : 8;           // one CTA per SM: 168 and 255 registers a thread
+    static constexpr int kStages = kMT == 1 ? 3 : 4;
+    static constexpr int kOpRows = kMT * 16;
+    static constexpr int kWarpBytes = kStages * kPgBlock + kOpRows * 256 + kOpRows * 16 + 64;   // ring, query operands, row facts, barriers
+    static constexpr int kSmem = kWarps * kWarpBytes;
+};
+
+// Where the operands of dimensions 32cq + 8c .. + 7 of an operand row stand: 16 bytes, spread so that a warp's 128-bit reads (rows
+// g, pieces cq) meet no bank twice.
+__device__ __forceinline__ uint32_t tree_operand(int row, int cq, int c) {
+    return static_cast<uint32_t>(row * 256 + (((c * 4 + cq) ^ ((row & 1) * 4)) << 4));
+}
+// Query rows of a tile -> fp16 operands in fragment order: row, then 16 bytes for dimensions 8c .. 8c + 7 as pairs (0,4) (1,5)/16
+// (2,6) (3,7)/16.  fact[row] = {-sum of the row's operands in three fp16 parts, factor from an accumulated product to a score}.
+template <bool BF16, int ROWS>
+__device__ __forceinline__ void tree_load_query(const KvTreeParams& p, int begin, int n, int h, int tile, uint8_t* operands, uint4* fact) {
+    using S = TreeShape<BF16, ROWS>;
+    const int lane = threadIdx.x & 31, l = lane & 7, sub = lane >> 3;
+    const int valid = min(ROWS, n * p.G - tile * ROWS);
+    for (int base = 0; base < ROWS; base += 4) {
+        const int row = base + sub, rho = tile * ROWS + row;
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = 0.0f;
+        if (base < valid) {                      // the same for the whole warp
+            if (row < valid) {
+                const int i = rho / p.G, g = rho - i * p.G;
+                kv_load16<BF16>(p.q, static_cast<size_t>((static_cast<long long>(begin) + i) * p.q_stride) + (h * p.G + g) * kKvD + 16 * l, v);
+            }
+            kv_rotate16(v, l, p.q_had, p.q_inv_sqrt);
+        }
+        float top = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(v[e]));
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        // power of two that brings the largest value to 2^7 .. 2^8 (exponent field of the factor: 127 + 7 - (field - 127))
+        const int field = max(16, min(254, static_cast<int>(__float_as_uint(top) >> 23)));
+        const float up = __uint_as_float(static_cast<uint32_t>(min(254, 261 - field)) << 23);
+        const float down = __uint_as_float(static_cast<uint32_t>(max(1, field - 7)) << 23);   // 1 / up
+        const bool ok = row < ROWS;              // ROWS is a multiple of 4
+#pragma unroll
+        for (int part = 0; part < (S::kSplit ? 2 : 1); ++part) {
+            float sum = 0.0f;
+            uint4 w[2];
+            uint32_t* ww = reinterpret_cast<uint32_t*>(w);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = v[8 * c + e] * (part ? 1.0f : up), b = v[8 * c + e + 4] * (part ? 1.0f : up);
+                    const float f = (e & 1) ? 0.0625f : 1.0f;
+                    const __half2 hh = __floats2half2_rn(a * f, b * f);
+                    const float2 back = __half22float2(hh);
+                    const float ra = back.x * ((e & 1) ? 16.0f : 1.0f), rb = back.y * ((e & 1) ? 16.0f : 1.0f);
+                    sum += ra + rb;
+                    if (S::kSplit && part == 0) v[8 * c + e] = a - ra, v[8 * c + e + 4] = b - rb;   // the residual is the second part
+                    ww[4 * c + e] = *reinterpret_cast<const uint32_t*>(&hh);
+                }
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            // operand row: m-tile, then g (first part or rows 0..7) or g + 8 (second part or rows 8..15)
+            const int op = S::kSplit ? (row >> 3) * 16 + (row & 7) + 8 * part : row;
+            if (ok) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) *reinterpret_cast<uint4*>(operands + tree_operand(op, l >> 1, 2 * (l & 1) + c)) = w[c];
+                if (l == 0) {
+                    const __half hi = __float2half_rn(-sum);
+                    const __half lo = __float2half_rn(-sum - __half2float(hi));
+                    const __half third = __float2half_rn((-sum - __half2float(hi)) - __half2float(lo));
+                    fact[op] = make_uint4(static_cast<uint32_t>(__half_as_ushort(hi)) | static_cast<uint32_t>(__half_as_ushort(lo)) << 16,
+                                          __half_as_ushort(third), __float_as_uint(down * 0x1p24f * p.scale_log2), 0u);
+                }
+            }
+        }
+    }
+}
+
+// Which tokens of block b a drafted token sees: bit k for position 32 b + k.
+__device__ __forceinline__ uint32_t tree_seen(const KvTreeParams& p, int row, int i, int b, int first, int len) {
+    const long long lo = static_cast<long long>(first) - static_cast<long long>(b) * kPgTokens;   // drafted token 0's bit in this block
+    uint32_t seen = lo >= 32 ? 0xffffffffu : lo > 0 ? (1u << lo) - 1u : 0u;
+    if (lo < 32) {
+        if (p.mask) {
+            const int32_t* m = p.mask + static_cast<size_t>(row) * p.mask_words;
+            if (lo >= 0) {
+                seen |= static_cast<uint32_t>(m[0]) << lo;
+            } else {
+                const long long j = -lo;
+                const long long word = j >> 5;
+                const int shift = static_cast<int>(j & 31);
+                const uint32_t a = word < p.mask_words ? static_cast<uint32_t>(m[word]) : 0u;
+                const uint32_t c = word + 1 < p.mask_words ? static_cast<uint32_t>(m[word + 1]) : 0u;
+                seen |= __funnelshift_r(a, c, shift);
+            }
+        } else {
+            const long long last = lo + i;   // bits lo .. lo + i
+            const uint32_t upto = last >= 31 ? 0xffffffffu : last >= 0 ? (2u << last) - 1u : 0u;
+            const uint32_t from = lo > 0 ? ~((1u << lo) - 1u) : 0xffffffffu;
+            seen |= upto & from;
+        }
+    }
+    const int left = len - b * kPgTokens;
+    if (left < 32) seen &= left > 0 ? (1u << left) - 1u : 0u;
+    return seen;
+}
+
+template <bool BF16, int ROWS>
+__global__ void __launch_bounds__(32 * TreeShape<BF16, ROWS>::kWarps, 1)
+kv4_tree_mma_kernel(const KvTreeParams p) {
+    using S = TreeShape<BF16, ROWS>;
+    constexpr int MT = S::kMT, LR = S::kLR, ST = S::kStages;
+    extern __shared__ __align__(16) uint8_t smem[];
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, cq = lane & 3;
+    uint8_t* ring = smem + warp * S::kWarpBytes;
+    uint8_t* operands = ring + ST * kPgBlock;
+    uint4* fact = reinterpret_cast<uint4*>(operands + S::kOpRows * 256);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(fact + S::kOpRows);
+    if (lane < ST) mbar_init(&bars[lane], 1);
+    mbar_fence_init();
+    __syncwarp();
+    pdl_wait();
+
+    // this warp's run of items
+    const int cap = p.pages.capacity(), H = p.pages.H, R = p.rows.R;
+    const int warps = gridDim.x * S::kWarps, me = blockIdx.x * S::kWarps + warp;
+    long long total = 0;
+    for (int base = 0; base < R; base += 32) {
+        long long n = 0;
+        if (base + lane < R) {
+            const TreeRequest q = tree_request<ROWS>(p, base + lane, cap);
+            n = static_cast<long long>(q.tiles) * q.blocks * H;
+        }
+        total += n;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    const long long run = max(static_cast<long long>(kTreeMinRun), (total + warps - 1) / warps);
+    const long long u0 = min(total, me * run), u1 = min(total, u0 + run);
+    int4 mine = make_int4(0, 0, 0, 0);   // the tile that begins here and ends later
+    int r = 0;
+    long long at = 0;                    // items before request r
+    TreeRequest q = {};
+    if (u0 < u1) {
+        for (int base = 0;; base += 32) {
+            long long n = 0;
+            if (base + lane < R) {
+                const TreeRequest t = tree_request<ROWS>(p, base + lane, cap);
+                n = static_cast<long long>(t.tiles) * t.blocks * H;
+            }
+            long long scan = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long up = __shfl_up_sync(0xffffffffu, scan, o);
+                if (lane >= o) scan += up;
+            }
+            const uint32_t hit = __ballot_sync(0xffffffffu, at + scan > u0);
+            if (hit) {
+                const int who = __ffs(hit) - 1;
+                r = base + who;
+                at += __shfl_sync(0xffffffffu, scan - n, who);
+                break;
+            }
+            at += __shfl_sync(0xffffffffu, scan, 31);   // u0 < total: some request is hit before the requests end
+        }
+        q = tree_request<ROWS>(p, r, cap);
+    }
+
+    const int page_blocks = p.pages.page_tokens / kPgTokens;
+    uint32_t phases = 0;                 // parity of each stage's barrier
+    bool failed = false;
+    for (long long u = u0; u < u1 && !failed;) {
+        while (u - at >= static_cast<long long>(q.tiles) * q.blocks * H) {   // on to the request of this item
+            at += static_cast<long long>(q.tiles) * q.blocks * H;
+            q = tree_request<ROWS>(p, ++r, cap);
+        }
+        const long long inner = u - at;
+        const int tile_of = static_cast<int>(inner / q.blocks), b0 = static_cast<int>(inner - static_cast<long long>(tile_of) * q.blocks);
+        const int h = tile_of / q.tiles, tile = tile_of - h * q.tiles;
+        const int b1 = static_cast<int>(min(static_cast<long long>(q.blocks), b0 + (u1 - u)));
+        const int begin = p.rows.begin(r);
+
+        // ring: stage s holds block b0 + s, b0 + s + ST, ...; a block without a page is skipped (bit of `there` not set)
+        const size_t head = static_cast<size_t>(page_blocks) * kPgBlock;
+        const int32_t* table = p.pages.table + static_cast<size_t>(r) * p.pages.max_pages;
+        int table_base = b0 / page_blocks, pages32 = table_base + lane < p.pages.max_pages ? table[table_base + lane] : -1;
+        int next = b0, next_slot = table_base, next_inner = b0 - table_base * page_blocks;
+        uint32_t there = 0;
+        auto issue = [&](int stage) {    // requests block `next` into a stage that nobody reads any more
+            if (next_slot - table_base >= 32) {
+                table_base = next_slot;
+                pages32 = table_base + lane < p.pages.max_pages ? table[table_base + lane] : -1;
+            }
+            const int page = __shfl_sync(0xffffffffu, pages32, next_slot - table_base);
+            const bool have = static_cast<unsigned>(page) < static_cast<unsigned>(p.pages.num_pages) && next * kPgTokens < q.len;
+            if (have) {
+                if (lane == 0) {
+                    mbar_expect_tx(&bars[stage], kPgBlock);
+                    bulk_g2s(ring + stage * kPgBlock, p.pages.pool + (static_cast<size_t>(page) * H + h) * head + static_cast<size_t>(next_inner) * kPgBlock,
+                             kPgBlock, &bars[stage]);
+                }
+                there |= 1u << stage;
+            } else {
+                there &= ~(1u << stage);
+            }
+            ++next;
+            if (++next_inner == page_blocks) next_inner = 0, ++next_slot;
+        };
+        __syncwarp();
+#pragma unroll
+        for (int s = 0; s < ST; ++s)
+            if (next < b1) issue(s);
+
+        tree_load_query<BF16, ROWS>(p, begin, q.n, h, tile, operands, fact);
+        __syncwarp();
+        uint32_t qz[MT][2];
+        float factor[MT][LR];
+        int row_of[MT][LR], token_of[MT][LR];   // row of the call and drafted token of a logical row; -1: none
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const uint4 fa = fact[m * 16 + g];
+            const uint4 fb = S::kHalf ? make_uint4(0u, 0u, 0u, 0u) : fact[m * 16 + g + 8];
+            qz[m][0] = cq == 0 ? fa.x : cq == 1 ? fa.y : 0u, qz[m][1] = cq == 0 ? fb.x : cq == 1 ? fb.y : 0u;
+#pragma unroll
+            for (int i = 0; i < LR; ++i) {
+                factor[m][i] = __uint_as_float(i ? fb.z : fa.z);
+                const int rho = tile * ROWS + (S::kSplit ? 8 * m + g : 16 * m + g + 8 * i);
+                token_of[m][i] = rho < q.n * p.G ? rho / p.G : -1;
+                row_of[m][i] = begin + token_of[m][i];
+            }
+        }
+
+        const uint32_t query = smem_u32(operands);
+        float o[MT][16][4], z[MT][4], m_run[MT][LR], l_run[MT][LR];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+            for (int nt = 0; nt < 16; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[m][i] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < LR; ++i) m_run[m][i] = -INFINITY, l_run[m][i] = 0.0f;
+        }
+        int vexp = 8;                    // exponent field of the power of two that value scales are measured against
+
+        int stage = 0;
+        for (int b = b0; b < b1; ++b, stage = stage + 1 == ST ? 0 : stage + 1) {
+            if (there >> stage & 1) {
+                if (!mbar_wait(&bars[stage], phases >> stage & 1, kTreeSite)) {
+                    failed = true;
+                    break;
+                }
+                phases ^= 1u << stage;
+                const uint32_t base = smem_u32(ring + stage * kPgBlock);
+                const uint32_t piece = static_cast<uint32_t>(cq * 8 + (g ^ (2 * cq))) * 16;
+
+                // ---- scores
+                uint4 kw[4];
+                uint32_t kz[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    kw[n] = lds128(base + n * 512 + piece);
+                    kz[n] = ring[stage * kPgBlock + kPgKz + 8 * n + g] * (cq == 0 ? 0x00010001u : cq == 1 ? 1u : 0u);
+                }
+                float2 ks[4], vs[4];
+                uint32_t vz[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    ks[n] = *reinterpret_cast<const float2*>(ring + stage * kPgBlock + kPgKs + (8 * n + 2 * cq) * 4);
+                    vs[n] = *reinterpret_cast<const float2*>(ring + stage * kPgBlock + kPgVs + (8 * n + 2 * cq) * 4);
+                    vz[n] = __byte_perm(*reinterpret_cast<const uint16_t*>(ring + stage * kPgBlock + kPgVz + 8 * n + 2 * cq), 0u, 0x4140u);
+                    if (S::kSplit) vz[n] = lessened(vz[n] | 0x64006400u, 0xe408e408u);   // - 1032
+                }
+                float sc[MT][4][4];
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sc[m][n][i] = 0.0f;
+                        mma_f16(sc[m][n], qz[m][0], qz[m][1], 0u, 0u, kz[n], 0u);
+                    }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint4 a[MT], a8[MT];   // query operands come from shared memory every time: registers go to the sums
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        a[m] = lds128(query + tree_operand(m * 16 + g, cq, c));
+                        a8[m] = S::kHalf ? make_uint4(0u, 0u, 0u, 0u) : lds128(query + tree_operand(m * 16 + g + 8, cq, c));
+                    }
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        const uint32_t w = c == 0 ? kw[n].x : c == 1 ? kw[n].y : c == 2 ? kw[n].z : kw[n].w, y = w >> 8;
+                        const uint32_t r0 = w & 0x000f000fu, r1 = w & 0x00f000f0u, r2 = y & 0x000f000fu, r3 = y & 0x00f000f0u;
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) {
+                            mma_f16(sc[m][n], a[m].x, a8[m].x, a[m].y, a8[m].y, r0, r1);
+                            mma_f16(sc[m][n], a[m].z, a8[m].z, a[m].w, a8[m].w, r2, r3);
+                        }
+                    }
+                }
+                uint4 vw[4];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) vw[w] = lds128(base + kPgV + w * 512 + piece);
+                // the stage has been read: its next block may come
+                __syncwarp();
+                if (next < b1) issue(stage);
+
+                // ---- which tokens are seen; slots that hold nothing may hold anything, NaN included
+                const bool plain = (b + 1) * kPgTokens <= q.first && (b + 1) * kPgTokens <= q.len;   // the whole block is context
+                uint32_t seen[MT][LR];
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < LR; ++i) seen[m][i] = 0xffffffffu;
+                if (!plain) {
+                    const int left = q.len - b * kPgTokens;
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int i = 0; i < LR; ++i)
+                            seen[m][i] = token_of[m][i] >= 0 ? tree_seen(p, row_of[m][i], token_of[m][i], b, q.first, q.len) : 0u;
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        if (8 * n + 2 * cq >= left) vs[n].x = 0.0f;
+                        if (8 * n + 2 * cq + 1 >= left) vs[n].y = 0.0f;
+                    }
+                }
+                // ---- reference points: the power of two of the value scales, then each row's
+                uint32_t vtop = 0;
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const uint32_t a = __float_as_uint(vs[n].x), c = __float_as_uint(vs[n].y);
+                    vtop = max(vtop, max(a < 0x7f800000u ? a : 0u, c < 0x7f800000u ? c : 0u));
+                }
+                if (__any_sync(0xffffffffu, static_cast<int>(vtop >> 23) > vexp)) {
+                    const int to = max(vexp, static_cast<int>(__reduce_max_sync(0xffffffffu, vtop) >> 23));
+                    // 2^(vexp - to); what is 2^126 smaller is gone
+                    const float corr = __uint_as_float(static_cast<uint32_t>(max(1, 127 + vexp - to)) << 23);
+                    vexp = to;
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+                        for (int nt = 0; nt < 16; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[m][nt][i] *= corr;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) z[m][i] *= corr;
+                    }
+                }
+                const float vinv = __uint_as_float(static_cast<uint32_t>(261 - vexp) << 23);   // 2^8 / 2^(vexp - 126): scales become < 2^8
+                uint32_t wa[MT][2][4];   // weights as A operands of the two k-steps
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+#pragma unroll
+                    for (int i = 0; i < LR; ++i) {
+                        float s[8], top = -INFINITY;
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float x = S::kSplit ? sc[m][n][e] + sc[m][n][2 + e] : sc[m][n][2 * i + e];
+                                float y = x * ((e ? ks[n].y : ks[n].x) * factor[m][i]);
+                                if (!plain && !(seen[m][i] >> (8 * n + 2 * cq + e) & 1)) y = -INFINITY;
+                                s[2 * n + e] = y, top = fmaxf(top, y);
+                            }
+                        if (__any_sync(0xffffffffu, top > m_run[m][i] + kTreeSlack)) {
+                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                            const float to = fmaxf(top, m_run[m][i]);
+                            const float corr = to > m_run[m][i] ? ex2(m_run[m][i] - to) : 1.0f;   // from -inf: 0
+                            m_run[m][i] = to, l_run[m][i] *= corr;
+#pragma unroll
+                            for (int nt = 0; nt < 16; ++nt) {
+                                if (S::kSplit) o[m][nt][0] *= corr, o[m][nt][1] *= corr, o[m][nt][2] *= corr, o[m][nt][3] *= corr;
+                                else o[m][nt][2 * i] *= corr, o[m][nt][2 * i + 1] *= corr;
+                            }
+                            if (S::kSplit) z[m][0] *= corr, z[m][1] *= corr, z[m][2] *= corr, z[m][3] *= corr;
+                            else z[m][2 * i] *= corr, z[m][2 * i + 1] *= corr;
+                        }
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) {
+                            float w[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const bool on = plain || (seen[m][i] >> (8 * n + 2 * cq + e) & 1);
+                                const float pr = on ? ex2(s[2 * n + e] - m_run[m][i]) : 0.0f;
+                                l_run[m][i] += pr;
+                                w[e] = on ? pr * ((e ? vs[n].y : vs[n].x) * vinv) : 0.0f;
+                            }
+                            // A registers of k-step n / 2: rows g, g + 8 for tokens of n-tile 2k, then of 2k + 1
+                            if (S::kSplit) {
+                                split_half2(w[0], w[1], wa[m][n >> 1][2 * (n & 1)], wa[m][n >> 1][2 * (n & 1) + 1]);
+                            } else {
+                                const __half2 hw = __floats2half2_rn(w[0], w[1]);
+                                wa[m][n >> 1][2 * (n & 1) + i] = *reinterpret_cast<const uint32_t*>(&hw);
+                                if (S::kHalf) wa[m][n >> 1][2 * (n & 1) + 1] = 0u;
+                            }
+                        }
+                    }
+                }
+                // ---- O += w . codes
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) mma_f16(z[m], wa[m][k][0], wa[m][k][1], wa[m][k][2], wa[m][k][3], vz[2 * k], vz[2 * k + 1]);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t x[4] = {vw[w].x, vw[w].y, vw[w].z, vw[w].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t select = (j & 1) ? 0x00f000f0u : 0x000f000fu;
+                        const int down = j < 2 ? 0 : 8;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            uint32_t v0 = (x[2 * k] >> down) & select, v1 = (x[2 * k + 1] >> down) & select;
+                            if (S::kSplit) {
+                                v0 = lessened(v0 | 0x64006400u, (j & 1) ? 0xe480e480u : 0xe408e408u);   // - 1152 : - 1032
+                                v1 = lessened(v1 | 0x64006400u, (j & 1) ? 0xe480e480u : 0xe408e408u);
+                            }
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) mma_f16(o[m][4 * w + j], wa[m][k][0], wa[m][k][1], wa[m][k][2], wa[m][k][3], v0, v1);
+                        }
+                    }
+                }
+            } else if (next < b1) {
+                __syncwarp();
+                issue(stage);
+            }
+        }
+        if (failed) break;
+
+        // ---- the tile, or this warp's piece of it
+        const bool whole = b0 == 0 && b1 == q.blocks;
+        const float c1 = __uint_as_float(static_cast<uint32_t>(vexp) << 23);   // 2^(vexp - 127), times 2 / 2^8 and the codes' 2^24 below
+        float* piece_at = p.partial + static_cast<size_t>(2 * me + (u == u0 ? 0 : 1)) * ROWS * kTreeRow;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < LR; ++i) {
+                float l = l_run[m][i];
+                l += __shfl_xor_sync(0xffffffffu, l, 1), l += __shfl_xor_sync(0xffffffffu, l, 2);
+                if (token_of[m][i] < 0) continue;
+                const int rho = tile * ROWS + (S::kSplit ? 8 * m + g : 16 * m + g + 8 * i);
+                const int hq = h * p.G + rho - token_of[m][i] * p.G;
+                const float inv = whole ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    float y[8];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float* a = o[m][4 * w + j];
+                            const float x = S::kSplit ? a[c] + a[2 + c] : a[2 * i + c];
+                            const float zz = S::kSplit ? z[m][c] + z[m][2 + c] : z[m][2 * i + c];
+                            y[4 * c + j] = (fmaf(x, (j & 1) ? 0.0625f : 1.0f, -zz) * (S::kSplit ? 0x1p-7f : 0x1p17f)) * c1 * inv;
+                        }
+                    const int d = 32 * w + 8 * cq;
+                    if (!whole) {
+                        float4* dst = reinterpret_cast<float4*>(piece_at + (rho - tile * ROWS) * kTreeRow + d);
+                        dst[0] = make_float4(y[0], y[1], y[2], y[3]), dst[1] = make_float4(y[4], y[5], y[6], y[7]);
+                    } else if constexpr (BF16) {
+                        uint32_t bits[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const __nv_bfloat162 t = __floats2bfloat162_rn(y[2 * e], y[2 * e + 1]);
+                            bits[e] = *reinterpret_cast<const uint32_t*>(&t);
+                        }
+                        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + (static_cast<size_t>(row_of[m][i]) * p.Hq + hq) * kKvD + d) =
+                            make_uint4(bits[0], bits[1], bits[2], bits[3]);
+                    } else {
+                        float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.out) + (static_cast<size_t>(row_of[m][i]) * p.Hq + hq) * kKvD + d);
+                        dst[0] = make_float4(y[0], y[1], y[2], y[3]), dst[1] = make_float4(y[4], y[5], y[6], y[7]);
+                    }
+                }
+                if (!whole && cq == 0)
+                    *reinterpret_cast<float2*>(piece_at + (rho - tile * ROWS) * kTreeRow + kKvD) = make_float2(m_run[m][i], l);
+            }
+        if (b0 == 0 && !whole) {
+            // the tile's later pieces: one in every warp until its last item
+            const long long last = u + q.blocks - 1;
+            mine = make_int4(r, h, tile, static_cast<int>(last / run) - me + 1);
+            if (u != u0) mine.y |= 1 << 24;   // its first piece is this warp's second
+        }
+        u += b1 - b0;
+    }
+    if (failed) {   // copies in flight end (or are given up) before the shared memory does; whoever waits for this run's piece skips it
+        mine = make_int4(0, 0, 0, 0);
+        for (int s = 0; s < ST; ++s) mbar_wait(&bars[s], phases >> s & 1, kTreeSite, 1000000ull);
+    }
+    if (lane == 0) p.desc[me] = mine;
+}
+
+// Joins the pieces of the tile that begins in run blockIdx.x and ends in a later one.  The CTA's warps are shared out over the
+// tile's rows; the warps of a row take its pieces in turn and meet in shared memory.
+constexpr int kTreeJoinWarps = 8;
+template <bool BF16, int ROWS>
+__global__ void __launch_bounds__(32 * kTreeJoinWarps)
+kv4_tree_join_kernel(const KvTreeParams p) {
+    __shared__ float4 num[kTreeJoinWarps][32];
+    __shared__ float2 ml[kTreeJoinWarps];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int4 d = p.desc[blockIdx.x];
+    if (d.w == 0) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int r = d.x, h = d.y & 0xffffff, tile = d.z, pieces = d.w;
+    const int begin = p.rows.begin(r), n = p.rows.count(r);
+    const int valid = min(ROWS, n * p.G - tile * ROWS);
+    int share = kTreeJoinWarps;          // warps of a row: a power of two
+    while (share > 1 && (kTreeJoinWarps / share < valid || share > pieces)) share >>= 1;
+    const int rows_at_once = kTreeJoinWarps / share, sub = warp % share;
+    const size_t step = static_cast<size_t>(2) * ROWS * kTreeRow;
+    const float* first = p.partial + static_cast<size_t>(2 * blockIdx.x + (d.y >> 24)) * ROWS * kTreeRow;
+    const float* rest = p.partial + static_cast<size_t>(blockIdx.x) * step;   // piece s > 0: rest + s * step
+    for (int base = 0; base < valid; base += rows_at_once) {
+        const int row = base + warp / share;
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float m = -INFINITY, l = 0.0f;
+        if (row < valid) {
+            constexpr int kAhead = 4;
+            for (int s0 = sub; s0 < pieces; s0 += share * kAhead) {
+                float4 x[kAhead];
+                float2 t[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int s = s0 + i * share;
+                    const float* at = (s == 0 ? first : rest + s * step) + row * kTreeRow;
+                    t[i] = make_float2(-INFINITY, 0.0f), x[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (s < pieces) x[i] = *reinterpret_cast<const float4*>(at + 4 * lane), t[i] = *reinterpret_cast<const float2*>(at + kKvD);
+                }
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    if (!(t[i].x > -INFINITY)) continue;
+                    const float to = fmaxf(m, t[i].x), a = ex2(m - to), c = ex2(t[i].x - to);
+                    acc.x = fmaf(acc.x, a, x[i].x * c), acc.y = fmaf(acc.y, a, x[i].y * c);
+                    acc.z = fmaf(acc.z, a, x[i].z * c), acc.w = fmaf(acc.w, a, x[i].w * c);
+                    l = fmaf(l, a, t[i].y * c), m = to;
+                }
+            }
+        }
+        if (share > 1) {
+            __syncthreads();
+            num[warp][lane] = acc;
+            if (lane == 0) ml[warp] = make_float2(m, l);
+            __syncthreads();
+            if (sub == 0) {
+                for (int s = 1; s < share; ++s) {
+                    const float2 t = ml[warp + s];
+                    if (!(t.x > -INFINITY)) continue;
+                    const float4 x = num[warp + s][lane];
+                    const float to = fmaxf(m, t.x), a = ex2(m - to), c = ex2(t.x - to);
+                    acc.x = fmaf(acc.x, a, x.x * c), acc.y = fmaf(acc.y, a, x.y * c);
+                    acc.z = fmaf(acc.z, a, x.z * c), acc.w = fmaf(acc.w, a, x.w * c);
+                    l = fmaf(l, a, t.y * c), m = to;
+                }
+            }
+        }
+        if (row < valid && sub == 0) {
+            const int rho = tile * ROWS + row, i = rho / p.G, hq = h * p.G + rho - i * p.G;
+            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            const size_t at = (static_cast<size_t>(begin + i) * p.Hq + hq) * kKvD + 4 * lane;
+            if constexpr (BF16) {
+                const __nv_bfloat162 a = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), c = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) =
+                    make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&c));
+            } else {
+                *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+            }
+        }
+    }
+}
+
+}  // namespace qift

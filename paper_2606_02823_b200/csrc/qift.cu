@@ -13,6 +13,9 @@
 #include "diag.cuh"
 #include "grouped.cuh"
 #include "kv4.cuh"
+#include "kv4_paged.cuh"
+#include "kv4_tree.cuh"
+#include "lora.cuh"
 #include "pack.cuh"
 #include "prefill.cuh"
 #include "prefill_2cta.cuh"
@@ -1682,6 +1685,184 @@ int qift_kv4_attention_decode(const float* q, const uint8_t* k_codes, const floa
     const int rc = cuda_status(launch_pdl(kv4_attention_partial_kernel, dim3(p.splits, p.Hkv), dim3(32 * kKvWarps), 0, st, p));
     if (rc != QIFT_OK) return rc;
     return cuda_status(launch_pdl(kv4_attention_combine_kernel, dim3(p.Hq), dim3(kKvCombineThreads), 0, st, p));
+}
+
+}  // extern "C"
+
+namespace {
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+// A row of H * D elements of a type, whole 16-byte units from row to row.
+inline bool row_stride_ok(long long stride, int H, int dtype) {
+    return stride >= static_cast<long long>(H) * kKvD && stride % (dtype == QIFT_BF16 ? 8 : 4) == 0;
+}
+inline bool had_ok(int b) { return b >= 0 && (b <= 1 || (is_pow2(b) && b <= kKvD)); }
+
+// What the paged calls have in common; fills the structures when it returns QIFT_OK.
+int check_paged(int total, int H, int D, const int32_t* row_start, const int32_t* first, int R, const int32_t* page_table, int max_pages,
+                const void* pool, int num_pages, int page_tokens, KvPages* pages, KvRows* rows) {
+    if (!row_start || !first || !page_table || !pool) return QIFT_ERR_INVALID_ARG;
+    if (total <= 0 || H <= 0 || R <= 0 || max_pages <= 0 || num_pages <= 0) return QIFT_ERR_INVALID_ARG;
+    if (qift_kv4_page_bytes(page_tokens, H, D) == 0) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(pool) || !aligned4(row_start) || !aligned4(first) || !aligned4(page_table)) return QIFT_ERR_ALIGNMENT;
+    pages->pool = static_cast<uint8_t*>(const_cast<void*>(pool)), pages->table = page_table;
+    pages->num_pages = num_pages, pages->max_pages = max_pages, pages->page_tokens = page_tokens, pages->H = H;
+    rows->row_start = row_start, rows->first = first, rows->R = R, rows->total = total;
+    return QIFT_OK;
+}
+// Blocks that the rows of a call can fall into: a request with n > 0 rows touches at most min(n, (n + 62) / 32) of them.
+inline long long most_blocks(int total, int R) {
+    const long long b = (static_cast<long long>(total) + 62ll * R) / kPgTokens;
+    return b < total ? b : total;
+}
+// KV heads of a CTA of the write and the read: one for prompts (a block is work enough for its 32 groups); for rows that come by
+// the few, as many as give the groups a vector each.
+inline int move_heads(int total, int R, int H) {
+    const long long rows = (total + R - 1) / R;
+    const int h = rows >= 16 ? 1 : rows >= 4 ? 4 : kPgMaxHeads;
+    return h < H ? h : H;
+}
+template <typename Kernel>
+int run_move(Kernel f32, Kernel bf16, int x_dtype, const KvMoveParams& p, cudaStream_t st) {
+    const dim3 grid(static_cast<unsigned>(most_blocks(p.rows.total, p.rows.R)), static_cast<unsigned>((p.pages.H + p.heads - 1) / p.heads));
+    return cuda_status(launch_pdl(x_dtype == QIFT_BF16 ? bf16 : f32, grid, dim3(kPgThreads), 0, st, p));
+}
+// Attention of trees: rows of a tile, by the mean of a request's rows for one KV head.
+inline int tree_rows(int total, int R, int G, bool bf16) {
+    const long long mean = (static_cast<long long>(total) * G + R - 1) / R;
+    return mean <= 8 ? 8 : (!bf16 || mean <= 16) ? 16 : 32;
+}
+inline int tree_runs(int rows, bool bf16) { return sm_count() * ((bf16 ? rows <= 16 : rows <= 8) ? 12 : 8); }   // warps of the grid
+// descriptors of the runs, then two pieces of a tile for each
+inline size_t tree_workspace(int rows, bool bf16) {
+    const size_t warps = static_cast<size_t>(tree_runs(rows, bf16));
+    return warps * sizeof(int4) + 2 * warps * rows * kTreeRow * sizeof(float);
+}
+template <bool BF16, int ROWS>
+int run_tree(KvTreeParams p, void* workspace, cudaStream_t st) {
+    using S = TreeShape<BF16, ROWS>;
+    const int runs = tree_runs(ROWS, BF16);
+    p.desc = static_cast<int4*>(workspace);
+    p.partial = reinterpret_cast<float*>(p.desc + runs);
+    const cudaError_t e = allow_smem(kv4_tree_mma_kernel<BF16, ROWS>, S::kSmem);
+    if (e != cudaSuccess) return cuda_status(e);
+    const int rc = cuda_status(launch_pdl(kv4_tree_mma_kernel<BF16, ROWS>, dim3(runs / S::kWarps), dim3(32 * S::kWarps), S::kSmem, st, p));
+    if (rc != QIFT_OK) return rc;
+    return cuda_status(launch_pdl(kv4_tree_join_kernel<BF16, ROWS>, dim3(runs), dim3(32 * kTreeJoinWarps), 0, st, p));
+}
+}  // namespace
+
+extern "C" {
+
+size_t qift_kv4_page_bytes(int page_tokens, int H, int D) {
+    if (H <= 0 || H > 65535 || D != kKvD || page_tokens < kPgTokens || page_tokens > 1024 || page_tokens % kPgTokens != 0) return 0;
+    return static_cast<size_t>(H) * (page_tokens / kPgTokens) * kPgBlock;
+}
+
+int qift_kv4_paged_write(const void* K, const void* V, int x_dtype, long long k_stride, long long v_stride, int total, int H, int D,
+                         int k_had_block, int v_had_block, float clip_ratio, const int32_t* row_start, const int32_t* first, int R,
+                         const int32_t* page_table, int max_pages, void* pool, int num_pages, int page_tokens, void* stream) {
+    if (!K || !V || (x_dtype != QIFT_F32 && x_dtype != QIFT_BF16)) return QIFT_ERR_INVALID_ARG;
+    if (!(clip_ratio > 0.0f && clip_ratio <= 1.0f)) return QIFT_ERR_INVALID_ARG;
+    KvMoveParams p{};
+    const int rc = check_paged(total, H, D, row_start, first, R, page_table, max_pages, pool, num_pages, page_tokens, &p.pages, &p.rows);
+    if (rc != QIFT_OK) return rc;
+    if (!had_ok(k_had_block) || !had_ok(v_had_block)) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!row_stride_ok(k_stride, H, x_dtype) || !row_stride_ok(v_stride, H, x_dtype)) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(K) || !aligned16(V)) return QIFT_ERR_ALIGNMENT;
+    p.K = const_cast<void*>(K), p.V = const_cast<void*>(V), p.k_stride = k_stride, p.v_stride = v_stride;
+    p.k_had = k_had_block, p.v_had = v_had_block, p.clip = clip_ratio;
+    p.k_inv_sqrt = k_had_block > 1 ? inv_sqrt_block(k_had_block) : 1.0f;
+    p.v_inv_sqrt = v_had_block > 1 ? inv_sqrt_block(v_had_block) : 1.0f;
+    p.heads = move_heads(total, R, H);
+    return run_move(kv4_paged_write_kernel<false>, kv4_paged_write_kernel<true>, x_dtype, p, static_cast<cudaStream_t>(stream));
+}
+
+int qift_kv4_paged_read(void* K, void* V, int x_dtype, long long k_stride, long long v_stride, int total, int H, int D,
+                        int k_had_block, int v_had_block, const int32_t* row_start, const int32_t* first, int R,
+                        const int32_t* page_table, int max_pages, const void* pool, int num_pages, int page_tokens, void* stream) {
+    if ((!K && !V) || (x_dtype != QIFT_F32 && x_dtype != QIFT_BF16)) return QIFT_ERR_INVALID_ARG;
+    KvMoveParams p{};
+    const int rc = check_paged(total, H, D, row_start, first, R, page_table, max_pages, pool, num_pages, page_tokens, &p.pages, &p.rows);
+    if (rc != QIFT_OK) return rc;
+    if (!had_ok(k_had_block) || !had_ok(v_had_block)) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if ((K && !row_stride_ok(k_stride, H, x_dtype)) || (V && !row_stride_ok(v_stride, H, x_dtype))) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(K) || !aligned16(V)) return QIFT_ERR_ALIGNMENT;
+    p.K = K, p.V = V, p.k_stride = k_stride, p.v_stride = v_stride, p.k_had = k_had_block, p.v_had = v_had_block, p.clip = 1.0f;
+    p.k_inv_sqrt = k_had_block > 1 ? inv_sqrt_block(k_had_block) : 1.0f;
+    p.v_inv_sqrt = v_had_block > 1 ? inv_sqrt_block(v_had_block) : 1.0f;
+    p.heads = move_heads(total, R, H);
+    return run_move(kv4_paged_read_kernel<false>, kv4_paged_read_kernel<true>, x_dtype, p, static_cast<cudaStream_t>(stream));
+}
+
+int qift_kv4_paged_keep(const int32_t* keep, const int32_t* kept_start, int total, int H, int D, const int32_t* row_start,
+                        const int32_t* first, int R, const int32_t* page_table, int max_pages, void* pool, int num_pages,
+                        int page_tokens, void* stream) {
+    if (!keep || !kept_start) return QIFT_ERR_INVALID_ARG;
+    KvPages pages;
+    KvRows rows;
+    const int rc = check_paged(total, H, D, row_start, first, R, page_table, max_pages, pool, num_pages, page_tokens, &pages, &rows);
+    if (rc != QIFT_OK) return rc;
+    if (!aligned4(keep) || !aligned4(kept_start)) return QIFT_ERR_ALIGNMENT;
+    const long long ctas = (static_cast<long long>(R) * H + kPgThreads / 32 - 1) / (kPgThreads / 32);
+    if (ctas > 0x7fffffffll) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    return cuda_status(launch_pdl(kv4_paged_keep_kernel, dim3(static_cast<unsigned>(ctas)), dim3(kPgThreads), 0,
+                                  static_cast<cudaStream_t>(stream), pages, rows, keep, kept_start));
+}
+
+size_t qift_kv4_paged_attention_workspace_bytes(int total, int R, int Hq, int H) {
+    if (total <= 0 || R <= 0 || Hq <= 0 || H <= 0 || Hq % H != 0) return 0;
+    const size_t f = tree_workspace(tree_rows(total, R, Hq / H, false), false), b = tree_workspace(tree_rows(total, R, Hq / H, true), true);
+    return f > b ? f : b;
+}
+
+int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int total, int Hq, int H, int D, int q_had_block,
+                             float scale, const int32_t* mask, int mask_words, const int32_t* row_start, const int32_t* first, int R,
+                             const int32_t* page_table, int max_pages, const void* pool, int num_pages, int page_tokens, void* out,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+    if (!q || !out || (q_dtype != QIFT_F32 && q_dtype != QIFT_BF16) || Hq <= 0) return QIFT_ERR_INVALID_ARG;
+    if (mask && (mask_words <= 0 || mask_words > 32)) return QIFT_ERR_INVALID_ARG;
+    if (!(scale >= 0.0f) || std::isinf(scale)) return QIFT_ERR_INVALID_ARG;
+    KvTreeParams p{};
+    const int rc = check_paged(total, H, D, row_start, first, R, page_table, max_pages, pool, num_pages, page_tokens, &p.pages, &p.rows);
+    if (rc != QIFT_OK) return rc;
+    if (!had_ok(q_had_block) || Hq % H != 0 || Hq / H > 64) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!row_stride_ok(q_stride, Hq, q_dtype)) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || !aligned4(mask)) return QIFT_ERR_ALIGNMENT;
+    if (!workspace || workspace_bytes < qift_kv4_paged_attention_workspace_bytes(total, R, Hq, H)) return QIFT_ERR_WORKSPACE;
+    p.q = q, p.out = out, p.mask = mask, p.mask_words = mask_words, p.q_stride = q_stride, p.Hq = Hq, p.G = Hq / H;
+    p.q_had = q_had_block, p.q_inv_sqrt = q_had_block > 1 ? inv_sqrt_block(q_had_block) : 1.0f;
+    p.scale_log2 = static_cast<float>((scale > 0.0f ? static_cast<double>(scale) : 1.0 / std::sqrt(static_cast<double>(D))) * 1.4426950408889634);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int rows = tree_rows(total, R, p.G, q_dtype == QIFT_BF16);
+    if (q_dtype == QIFT_BF16)
+        return rows == 8 ? run_tree<true, 8>(p, workspace, st) : rows == 16 ? run_tree<true, 16>(p, workspace, st) : run_tree<true, 32>(p, workspace, st);
+    return rows == 8 ? run_tree<false, 8>(p, workspace, st) : run_tree<false, 16>(p, workspace, st);
+}
+
+size_t qift_lora_workspace_bytes(int M, int rank, int K) {
+    if (M <= 0 || rank <= 0 || K <= 0) return 0;
+    return (static_cast<size_t>(M) * rank * sizeof(float) + 15) & ~static_cast<size_t>(15);
+}
+
+int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16_t* B, const float* scaling, int adapters, int rank,
+                     int M, int N, int K, const int32_t* row_start, const int32_t* adapter, int R, const void* y, void* out,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+    if (!X || !A || !B || !scaling || !row_start || !adapter || !out) return QIFT_ERR_INVALID_ARG;
+    if (adapters <= 0 || rank <= 0 || M <= 0 || N <= 0 || K <= 0 || R <= 0) return QIFT_ERR_INVALID_ARG;
+    if (x_dtype != QIFT_F32 && x_dtype != QIFT_BF16) return QIFT_ERR_INVALID_ARG;
+    if (K % 8 != 0 || N % 8 != 0 || rank % 8 != 0 || rank > 128) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(X) || !aligned16(A) || !aligned16(B) || !aligned16(y) || !aligned16(out) || !aligned16(workspace) ||
+        !aligned4(scaling) || !aligned4(row_start) || !aligned4(adapter))
+        return QIFT_ERR_ALIGNMENT;
+    if (!workspace || workspace_bytes < qift_lora_workspace_bytes(M, rank, K)) return QIFT_ERR_WORKSPACE;
+    LoraParams p{};
+    p.x = X, p.A = A, p.B = B, p.scaling = scaling, p.row_start = row_start, p.adapter = adapter, p.y = y, p.out = out;
+    p.t = static_cast<float*>(workspace), p.M = M, p.N = N, p.K = K, p.rank = rank, p.adapters = adapters, p.R = R;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool b = x_dtype == QIFT_BF16;
+    const int rc = cuda_status(launch_pdl(b ? lora_down_kernel<true> : lora_down_kernel<false>, dim3(M), dim3(256), 0, st, p));
+    if (rc != QIFT_OK) return rc;
+    return cuda_status(launch_pdl(b ? lora_up_kernel<true> : lora_up_kernel<false>, dim3(M), dim3(256), 0, st, p));
 }
 
 }  // extern "C"

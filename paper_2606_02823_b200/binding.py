@@ -581,20 +581,33 @@ def qift_kv4_attention_decode(q, K: Kv4Cache, V: Kv4Cache, T: int, out=None, wor
 KV_BLOCK_TOKENS, KV_BLOCK_BYTES = 32, 4416
 
 
-def _call(t, name, *args):
+def _call(t, fn, *args):
     """Calls an entry point on the current stream of the tensors' device (which need not be the current one)."""
-    if t.device.index == torch.cuda.current_device():
-        rc = getattr(_lib or lib(), name)(*args, _stream())
+    device = t.get_device()
+    if device == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(device))
     else:
-        with torch.cuda.device(t.device):
-            rc = getattr(_lib or lib(), name)(*args, _stream())
+        with torch.cuda.device(device):
+            rc = fn(*args, _raw_stream(device))
     if rc != OK:
-        raise QiftError(rc, name)
+        raise QiftError(rc, fn.__name__)
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _on(t, dtype, *shape):
+    """The address of a contiguous CUDA tensor; dtype and (where given) shape are checked."""
+    assert t.is_cuda and t.is_contiguous(), "expected a contiguous CUDA tensor"
+    assert t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
+    assert not shape or t.shape == shape, f"expected shape {shape}, got {tuple(t.shape)}"
+    return t.data_ptr()
 
 
 def _same_device(t, *others):
+    device = t.get_device()
     for o in others:
-        assert o is None or o.device == t.device, f"tensors on {t.device} and {o.device}"
+        assert o is None or o.get_device() == device, f"tensors on {t.device} and {o.device}"
 
 
 def _float_type(t):
@@ -615,12 +628,12 @@ class Kv4Pages:
     requests of a batch (the layout is described in include/qift.h)."""
 
     def __init__(self, pool, page_table, page_tokens: int):
-        _dev(pool, torch.uint8), _dev(page_table, torch.int32), _same_device(pool, page_table)
-        assert pool.dim() == 3 and page_table.dim() == 2
-        assert pool.shape[2] * KV_BLOCK_TOKENS == page_tokens * KV_BLOCK_BYTES, "the pool's last dimension is page_tokens / 32 * 4416 bytes"
-        self.pool, self.page_table, self.page_tokens = pool, page_table, page_tokens
-        self.num_pages, self.H = pool.shape[0], pool.shape[1]
+        _on(pool, torch.uint8), _on(page_table, torch.int32)
+        _same_device(pool, page_table)
+        self.num_pages, self.H, page_bytes = pool.shape
         self.R, self.max_pages = page_table.shape
+        assert page_bytes * KV_BLOCK_TOKENS == page_tokens * KV_BLOCK_BYTES, "the pool's last dimension is page_tokens / 32 * 4416 bytes"
+        self.pool, self.page_table, self.page_tokens = pool, page_table, page_tokens
 
     @classmethod
     def empty(cls, num_pages: int, H: int, page_tokens: int, page_table):
@@ -628,10 +641,9 @@ class Kv4Pages:
         return cls(pool, page_table, page_tokens)
 
     def _batch(self, row_start, first):
-        _dev(row_start, torch.int32), _dev(first, torch.int32), _same_device(self.pool, row_start, first)
-        assert row_start.numel() == self.R + 1 and first.numel() == self.R, "row_start has R + 1 entries, first R, like the page table"
-        return (_ptr(row_start), _ptr(first), self.R, _ptr(self.page_table), self.max_pages, _ptr(self.pool), self.num_pages,
-                self.page_tokens)
+        _same_device(self.pool, row_start, first)
+        return (_on(row_start, torch.int32, self.R + 1), _on(first, torch.int32, self.R), self.R, _on(self.page_table, torch.int32, self.R, self.max_pages),
+                self.max_pages, _on(self.pool, torch.uint8), self.num_pages, self.page_tokens)
 
 
 def qift_kv4_page_bytes(page_tokens: int, H: int, D: int = 128) -> int:
@@ -642,9 +654,10 @@ def qift_kv4_paged_write(K, V, pages: Kv4Pages, row_start, first, k_had_block: i
     """K, V fp32 or bf16 [total, H, D] -> quantized into positions first[r] .. of each request's pages."""
     _same_device(pages.pool, K, V)
     assert K.dtype == V.dtype and K.shape == V.shape
+    total, H, D = K.shape
     ks, vs = _rows(K, pages.H), _rows(V, pages.H)
-    _call(K, "qift_kv4_paged_write", _ptr(K), _ptr(V), _float_type(K), ks, vs, K.shape[0], pages.H, K.shape[2], k_had_block,
-          v_had_block, clip_ratio, *pages._batch(row_start, first))
+    _call(K, lib().qift_kv4_paged_write, K.data_ptr(), V.data_ptr(), _float_type(K), ks, vs, total, H, D, k_had_block, v_had_block,
+          clip_ratio, *pages._batch(row_start, first))
 
 
 def qift_kv4_paged_read(pages: Kv4Pages, row_start, first, total: int, dtype=torch.float32, k_had_block: int = 0, v_had_block: int = 0,
@@ -652,23 +665,23 @@ def qift_kv4_paged_read(pages: Kv4Pages, row_start, first, total: int, dtype=tor
     """-> (K, V) [total, H, 128]: what positions first[r] .. of each request hold, rotated back.  Rows of no request (and
     positions without a page) are left as they are in K and V where those are given."""
     if K is None:
-        K = torch.empty((total, pages.H, 128), dtype=dtype, device=pages.pool.device)
+        K = torch.empty((total, pages.H, 128), dtype=dtype if V is None else V.dtype, device=pages.pool.device)
     if V is None:
-        V = torch.empty((total, pages.H, 128), dtype=dtype, device=pages.pool.device)
+        V = torch.empty(K.shape, dtype=K.dtype, device=K.device)
     _same_device(pages.pool, K, V)
     assert K.dtype == V.dtype and K.shape == V.shape and K.shape[0] == total
     ks, vs = _rows(K, pages.H), _rows(V, pages.H)
-    _call(K, "qift_kv4_paged_read", _ptr(K), _ptr(V), _float_type(K), ks, vs, total, pages.H, K.shape[2], k_had_block, v_had_block,
-          *pages._batch(row_start, first))
+    _call(K, lib().qift_kv4_paged_read, K.data_ptr(), V.data_ptr(), _float_type(K), ks, vs, total, pages.H, K.shape[2], k_had_block,
+          v_had_block, *pages._batch(row_start, first))
     return K, V
 
 
 def qift_kv4_paged_keep(pages: Kv4Pages, row_start, first, keep, kept_start):
     """After the check of drafted trees at first[r] ..: position first[r] + i takes the token at first[r] + keep[row_start[r] + i]
     for the kept_start[r + 1] - kept_start[r] accepted tokens of each request (ascending indices)."""
-    _dev(keep, torch.int32), _dev(kept_start, torch.int32), _same_device(pages.pool, keep, kept_start)
-    assert kept_start.numel() == pages.R + 1
-    _call(keep, "qift_kv4_paged_keep", _ptr(keep), _ptr(kept_start), keep.numel(), pages.H, 128, *pages._batch(row_start, first))
+    _same_device(pages.pool, keep, kept_start)
+    _call(keep, lib().qift_kv4_paged_keep, _on(keep, torch.int32), _on(kept_start, torch.int32, pages.R + 1), keep.numel(), pages.H, 128,
+          *pages._batch(row_start, first))
 
 
 def qift_kv4_paged_attention_workspace_bytes(total: int, R: int, Hq: int, H: int) -> int:
@@ -680,23 +693,19 @@ def qift_kv4_paged_attention(q, pages: Kv4Pages, row_start, first, mask=None, q_
     """q fp32 or bf16 [total, Hq, D] -> out of the same shape and type: the attention of each row over its request's cached tokens
     before first[r] and the drafted ones that mask (int32 [total, words], bit j: drafted token j) lets it see; without a mask,
     those up to itself."""
-    Hq, D = q.shape[1], q.shape[2]
+    L = lib()
+    total, Hq, D = q.shape
+    qs = _rows(q)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    qs = _rows(q)
-    _dev(out, q.dtype), _same_device(pages.pool, q, out, mask)
-    assert out.shape == q.shape
-    words = 0
-    if mask is not None:
-        _dev(mask, torch.int32)
-        assert mask.dim() == 2 and mask.shape[0] == q.shape[0]
-        words = mask.shape[1]
     if workspace is None:
-        need = (_lib or lib()).qift_kv4_paged_attention_workspace_bytes(q.shape[0], pages.R, Hq, pages.H)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
-    _same_device(q, workspace)
-    _call(q, "qift_kv4_paged_attention", _ptr(q), _float_type(q), qs, q.shape[0], Hq, pages.H, D, q_had_block, scale, _ptr(mask),
-          words, *pages._batch(row_start, first), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size())
+        need = L.qift_kv4_paged_attention_workspace_bytes(total, pages.R, Hq, pages.H)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _same_device(pages.pool, q, out, mask, workspace)
+    words = 0 if mask is None else mask.shape[1]
+    _call(q, L.qift_kv4_paged_attention, q.data_ptr(), _float_type(q), qs, total, Hq, pages.H, D, q_had_block, scale,
+          None if mask is None else _on(mask, torch.int32, total, words), words, *pages._batch(row_start, first),
+          _on(out, q.dtype, total, Hq, D), workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return out
 
 
@@ -709,28 +718,19 @@ def qift_lora_linear(x, A, B, scaling, row_start, adapter, y=None, out=None, wor
     """x fp32 or bf16 [M, K], A bf16 [adapters, rank, K], B bf16 [adapters, N, rank], scaling fp32 [adapters], adapter int32 [R] ->
     out [M, N] of x's type: y + scaling[a] * B[a] (A[a] x) for the rows row_start[r] .. of each request and its adapter a (none
     where it is negative).  y (None: zeros) is the shared projection's product; out may be y."""
-    _dev(x), _dev(A, torch.bfloat16), _dev(B, torch.bfloat16), _dev(scaling, torch.float32)
-    _dev(row_start, torch.int32), _dev(adapter, torch.int32)
+    L = lib()
     M, K = x.shape
     n, rank = A.shape[0], A.shape[1]
-    N = B.shape[1]
-    assert A.shape == (n, rank, K) and B.shape == (n, N, rank) and scaling.numel() == n
-    R = adapter.numel()
-    assert row_start.numel() == R + 1
-    if y is not None:
-        _dev(y, x.dtype)
-        assert y.shape == (M, N)
+    N, R = B.shape[1], adapter.numel()
     if out is None:
         out = torch.empty((M, N), dtype=x.dtype, device=x.device)
-    else:
-        _dev(out, x.dtype)
-        assert out.shape == (M, N)
     if workspace is None:
-        need = (_lib or lib()).qift_lora_workspace_bytes(M, rank, K)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=x.device)
+        workspace = torch.empty(L.qift_lora_workspace_bytes(M, rank, K), dtype=torch.uint8, device=x.device)
     _same_device(x, A, B, scaling, row_start, adapter, y, out, workspace)
-    _call(x, "qift_lora_linear", _ptr(x), _float_type(x), _ptr(A), _ptr(B), _ptr(scaling), n, rank, M, N, K, _ptr(row_start),
-          _ptr(adapter), R, _ptr(y), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size())
+    _call(x, L.qift_lora_linear, _on(x, x.dtype), _float_type(x), _on(A, torch.bfloat16, n, rank, K), _on(B, torch.bfloat16, n, N, rank),
+          _on(scaling, torch.float32, n), n, rank, M, N, K, _on(row_start, torch.int32, R + 1), _on(adapter, torch.int32, R), R,
+          None if y is None else _on(y, x.dtype, M, N), _on(out, x.dtype, M, N), workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())
     return out
 
 

@@ -15,8 +15,8 @@
 // against the same rounded operands.
 //   q is scaled by a power of two per row (largest value 2^7 .. 2^8) and held in fp16: exact for bf16 queries that are not
 //   rotated, else off by 2^-12.  fp32 calls hold q and w in two fp16 parts each (residual 2^-22), rows g and g + 8 of the same
-//   instruction, and their value codes lessened by 8 (1024 + c - 1032 in fp16, exact): the sums of an average over many tokens
-//   would otherwise be far larger than the result and lose what the zero-points take away.  w is normalised by the largest value scale seen so far (a power of two, one for the warp) and by the row's
+//   instruction, and all codes lessened by 8 (1024 + c - 1032 in fp16, exact): the sums of an average over many tokens would
+//   otherwise be far larger than the result and lose what the zero-points take away.  w is normalised by the largest value scale seen so far (a power of two, one for the warp) and by the row's
 //   reference point, which moves only when a score exceeds it by more than kTreeSlack.
 #pragma once
 
@@ -148,7 +148,7 @@ __device__ __forceinline__ void tree_load_query(const KvTreeParams& p, int begin
                     const __half lo = __float2half_rn(-sum - __half2float(hi));
                     const __half third = __float2half_rn((-sum - __half2float(hi)) - __half2float(lo));
                     fact[op] = make_uint4(static_cast<uint32_t>(__half_as_ushort(hi)) | static_cast<uint32_t>(__half_as_ushort(lo)) << 16,
-                                          __half_as_ushort(third), __float_as_uint(down * 0x1p24f * p.scale_log2), 0u);
+                                          __half_as_ushort(third), __float_as_uint(down * (S::kSplit ? 1.0f : 0x1p24f) * p.scale_log2), 0u);
                 }
             }
         }
@@ -342,7 +342,9 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
 #pragma unroll
                 for (int n = 0; n < 4; ++n) {
                     kw[n] = lds128(base + n * 512 + piece);
-                    kz[n] = ring[stage * kPgBlock + kPgKz + 8 * n + g] * (cq == 0 ? 0x00010001u : cq == 1 ? 1u : 0u);
+                    kz[n] = ring[stage * kPgBlock + kPgKz + 8 * n + g] * 0x00010001u;
+                    if (S::kSplit) kz[n] = lessened(kz[n] | 0x64006400u, 0xe408e408u);   // - 1032
+                    kz[n] &= cq == 0 ? 0xffffffffu : cq == 1 ? 0x0000ffffu : 0u;
                 }
                 float2 ks[4], vs[4];
                 uint32_t vz[4];
@@ -373,7 +375,11 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
 #pragma unroll
                     for (int n = 0; n < 4; ++n) {
                         const uint32_t w = c == 0 ? kw[n].x : c == 1 ? kw[n].y : c == 2 ? kw[n].z : kw[n].w, y = w >> 8;
-                        const uint32_t r0 = w & 0x000f000fu, r1 = w & 0x00f000f0u, r2 = y & 0x000f000fu, r3 = y & 0x00f000f0u;
+                        uint32_t r0 = w & 0x000f000fu, r1 = w & 0x00f000f0u, r2 = y & 0x000f000fu, r3 = y & 0x00f000f0u;
+                        if (S::kSplit) {
+                            r0 = lessened(r0 | 0x64006400u, 0xe408e408u), r1 = lessened(r1 | 0x64006400u, 0xe480e480u);   // - 1032, - 1152
+                            r2 = lessened(r2 | 0x64006400u, 0xe408e408u), r3 = lessened(r3 | 0x64006400u, 0xe480e480u);
+                        }
 #pragma unroll
                         for (int m = 0; m < MT; ++m) {
                             mma_f16(sc[m][n], a[m].x, a8[m].x, a[m].y, a8[m].y, r0, r1);

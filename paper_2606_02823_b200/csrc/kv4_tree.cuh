@@ -7,18 +7,22 @@
 // is finished there; the pieces of the others go to the workspace -- a warp has at most two, its first and its last -- and the
 // second kernel joins them, one CTA for the tile that begins in a warp and ends in a later one.
 //
-// Both products run on mma.sync.m16n8k16 (fp16, fp32 sums) with the query rows as A:
-//   S[row][token] = sum_d q[row][d] kc[token][d],        O[row][d] += sum_t w[row][t] vc[t][d],  w = p * vs.
+// Both products run on mma.sync.m16n8k16 (fp16, fp32 sums) with the codes as A and eight query rows as the columns:
+//   S[token][row] = sum_d kc[token][d] q[row][d],        O[d][row] += sum_t vc[t][d] w[t][row],  w = p * vs.
 // A code c in the low mantissa bits of an fp16 number is the subnormal c * 2^-24, exactly: `word & 0x000f000f` IS a pair of
-// operands, `word & 0x00f000f0` one of 16 c * 2^-24 (the 16 is taken out of the query, and out of the result).  Zero-points enter
-// as one more k-step (query sums against key zeros) and one more column tile (weights against value zeros), so they cancel
-// against the same rounded operands.
+// operands, `word & 0x00f000f0` one of 16 c * 2^-24 (the 16 is taken out of the query, and out of the result).  Scores come out
+// with a lane holding four tokens of two rows, and movmatrix turns the packed weights into the columns of the second product.
+// Zero-points enter as one more k-step (key zeros against query sums) and one more row tile (value zeros against weights), so they
+// cancel against the same rounded operands.
 //   q is scaled by a power of two per row (largest value 2^7 .. 2^8) and held in fp16: exact for bf16 queries that are not
-//   rotated, else off by 2^-12.  fp32 calls hold q and w in two fp16 parts each (residual 2^-22), rows g and g + 8 of the same
-//   instruction, and all codes lessened by 8 (1024 + c - 1032 in fp16, exact): the sums of an average over many tokens would
-//   otherwise be far larger than the result and lose what the zero-points take away.  w is normalised by the largest value scale seen so far (a power of two, one for the warp) and by the row's
-//   reference point, which moves only when a score exceeds it by more than kTreeSlack.
+//   rotated, else off by 2^-12.  fp32 calls hold q and w in two fp16 parts each (residual 2^-22), multiplied one after the other
+//   into the same sums, and all codes lessened by 8 (1024 + c - 1032 in fp16, exact): the sums of an average over many tokens
+//   would otherwise be far larger than the result and lose what the zero-points take away.  w is normalised by the largest value
+//   scale seen so far (a power of two, one for the warp) and by the row's reference point, which moves only when a score exceeds
+//   it by more than kTreeSlack.
 #pragma once
+
+#include <type_traits>
 
 #include "kv4_paged.cuh"
 
@@ -42,6 +46,7 @@ struct KvTreeParams {
 constexpr int kTreeRow = 132;        // floats of a row's piece: numerator, reference point, sum, two unused
 constexpr int kTreeMinRun = 2;       // items of a warp's run at least
 constexpr float kTreeSlack = 6.0f;   // binary orders that a weight may exceed its reference by: w * 2^8 stays below 2^14
+constexpr int kTreeVexp = 40;           // exponent field of the smallest power of two that value scales are measured against
 constexpr int kTreeSite = 48;        // site of an expired wait
 
 __device__ __forceinline__ float ex2(float x) {
@@ -73,24 +78,20 @@ __device__ __forceinline__ TreeRequest tree_request(const KvTreeParams& p, int r
 
 template <bool BF16, int ROWS>
 struct TreeShape {
-    static constexpr bool kSplit = !BF16;                      // operands in two parts, rows g and g + 8
-    static constexpr int kMT = kSplit ? ROWS / 8 : (ROWS + 15) / 16;
-    static constexpr bool kHalf = BF16 && ROWS == 8;           // rows g + 8 unused
-    static constexpr int kLR = (kSplit || kHalf) ? 1 : 2;      // logical rows of a lane per m-tile
-    static constexpr int kWarps = kMT == 1 ? 12 : 8;           // one CTA per SM: 168 and 255 registers a thread
-    static constexpr int kStages = kMT == 1 ? 3 : 4;
-    static constexpr int kOpRows = kMT * 16;
-    static constexpr int kWarpBytes = kStages * kPgBlock + kOpRows * 256 + kOpRows * 16 + 64;   // ring, query operands, row facts, barriers
+    static constexpr bool kSplit = !BF16;                      // operands in two parts
+    static constexpr int kParts = kSplit ? 2 : 1;
+    static constexpr int kNT = ROWS / 8;                       // column tiles
+    static constexpr int kWarps = kNT == 1 ? 16 : 12;          // one CTA per SM: 128 and 168 registers a thread
+    static constexpr int kStages = kNT == 1 ? 2 : 3;
+    static constexpr int kQuery = kNT * kParts * 4 * 512;      // query operands: tile, part, two k-steps, lane, their four registers
+    static constexpr int kWarpBytes = kStages * kPgBlock + kQuery + ROWS * kParts * 16 + 64;   // ring, query, row facts, barriers
     static constexpr int kSmem = kWarps * kWarpBytes;
+    static_assert(ROWS == 8 || (BF16 && ROWS == 16), "rows of a tile");
 };
 
-// Where the operands of dimensions 32cq + 8c .. + 7 of an operand row stand: 16 bytes, spread so that a warp's 128-bit reads (rows
-// g, pieces cq) meet no bank twice.
-__device__ __forceinline__ uint32_t tree_operand(int row, int cq, int c) {
-    return static_cast<uint32_t>(row * 256 + (((c * 4 + cq) ^ ((row & 1) * 4)) << 4));
-}
-// Query rows of a tile -> fp16 operands in fragment order: row, then 16 bytes for dimensions 8c .. 8c + 7 as pairs (0,4) (1,5)/16
-// (2,6) (3,7)/16.  fact[row] = {-sum of the row's operands in three fp16 parts, factor from an accumulated product to a score}.
+// Query rows of a tile -> fp16 B operands.  Dimensions 8c .. 8c + 7 of a row (c = 4 cq + i) are the pairs (0,4) (1,5)/16 of k-step
+// 2i and (2,6) (3,7)/16 of k-step 2i + 1.  fact[part][row] = {-sum of the row's operands in three fp16 parts, factor from an
+// accumulated product to a score}.
 template <bool BF16, int ROWS>
 __device__ __forceinline__ void tree_load_query(const KvTreeParams& p, int begin, int n, int h, int tile, uint8_t* operands, uint4* fact) {
     using S = TreeShape<BF16, ROWS>;
@@ -117,14 +118,12 @@ __device__ __forceinline__ void tree_load_query(const KvTreeParams& p, int begin
         const int field = max(16, min(254, static_cast<int>(__float_as_uint(top) >> 23)));
         const float up = __uint_as_float(static_cast<uint32_t>(min(254, 261 - field)) << 23);
         const float down = __uint_as_float(static_cast<uint32_t>(max(1, field - 7)) << 23);   // 1 / up
-        const bool ok = row < ROWS;              // ROWS is a multiple of 4
 #pragma unroll
-        for (int part = 0; part < (S::kSplit ? 2 : 1); ++part) {
+        for (int part = 0; part < S::kParts; ++part) {
             float sum = 0.0f;
-            uint4 w[2];
-            uint32_t* ww = reinterpret_cast<uint32_t*>(w);
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+            for (int c = 0; c < 2; ++c) {
+                uint32_t w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float a = v[8 * c + e] * (part ? 1.0f : up), b = v[8 * c + e + 4] * (part ? 1.0f : up);
@@ -134,25 +133,29 @@ __device__ __forceinline__ void tree_load_query(const KvTreeParams& p, int begin
                     const float ra = back.x * ((e & 1) ? 16.0f : 1.0f), rb = back.y * ((e & 1) ? 16.0f : 1.0f);
                     sum += ra + rb;
                     if (S::kSplit && part == 0) v[8 * c + e] = a - ra, v[8 * c + e + 4] = b - rb;   // the residual is the second part
-                    ww[4 * c + e] = *reinterpret_cast<const uint32_t*>(&hh);
+                    w[e] = *reinterpret_cast<const uint32_t*>(&hh);
                 }
+                const int at = (((row >> 3) * S::kParts + part) * 4 + 2 * (l & 1) + c) * 512 + ((row & 7) * 4 + (l >> 1)) * 16;
+                *reinterpret_cast<uint4*>(operands + at) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
 #pragma unroll
             for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            // operand row: m-tile, then g (first part or rows 0..7) or g + 8 (second part or rows 8..15)
-            const int op = S::kSplit ? (row >> 3) * 16 + (row & 7) + 8 * part : row;
-            if (ok) {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) *reinterpret_cast<uint4*>(operands + tree_operand(op, l >> 1, 2 * (l & 1) + c)) = w[c];
-                if (l == 0) {
-                    const __half hi = __float2half_rn(-sum);
-                    const __half lo = __float2half_rn(-sum - __half2float(hi));
-                    const __half third = __float2half_rn((-sum - __half2float(hi)) - __half2float(lo));
-                    fact[op] = make_uint4(static_cast<uint32_t>(__half_as_ushort(hi)) | static_cast<uint32_t>(__half_as_ushort(lo)) << 16,
-                                          __half_as_ushort(third), __float_as_uint(down * (S::kSplit ? 1.0f : 0x1p24f) * p.scale_log2), 0u);
-                }
+            if (l == 0) {
+                const __half hi = __float2half_rn(-sum);
+                const __half lo = __float2half_rn(-sum - __half2float(hi));
+                const __half third = __float2half_rn((-sum - __half2float(hi)) - __half2float(lo));
+                fact[part * ROWS + row] = make_uint4(static_cast<uint32_t>(__half_as_ushort(hi)) | static_cast<uint32_t>(__half_as_ushort(lo)) << 16,
+                                                     __half_as_ushort(third), __float_as_uint(down * (S::kSplit ? 1.0f : 0x1p24f) * p.scale_log2), 0u);
             }
         }
     }
+}
+
+// The transpose of an 8 x 8 matrix of 16-bit values, two of them (neighbours in a row) per lane.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 
 // Which tokens of block b a drafted token sees: bit k for position 32 b + k.
@@ -188,14 +191,14 @@ template <bool BF16, int ROWS>
 __global__ void __launch_bounds__(32 * TreeShape<BF16, ROWS>::kWarps, 1)
 kv4_tree_mma_kernel(const KvTreeParams p) {
     using S = TreeShape<BF16, ROWS>;
-    constexpr int MT = S::kMT, LR = S::kLR, ST = S::kStages;
+    constexpr int NT = S::kNT, ST = S::kStages;
     extern __shared__ __align__(16) uint8_t smem[];
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, cq = lane & 3;
     uint8_t* ring = smem + warp * S::kWarpBytes;
     uint8_t* operands = ring + ST * kPgBlock;
-    uint4* fact = reinterpret_cast<uint4*>(operands + S::kOpRows * 256);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(fact + S::kOpRows);
+    uint4* fact = reinterpret_cast<uint4*>(operands + S::kQuery);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(fact + ROWS * S::kParts);
     if (lane < ST) mbar_init(&bars[lane], 1);
     mbar_fence_init();
     __syncwarp();
@@ -247,6 +250,8 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
     }
 
     const int page_blocks = p.pages.page_tokens / kPgTokens;
+    const uint32_t ring_at = smem_u32(ring), query = smem_u32(operands) + lane * 16;
+    const uint32_t piece = static_cast<uint32_t>(cq * 8 + (g ^ (2 * cq))) * 16;
     uint32_t phases = 0;                 // parity of each stage's barrier
     bool failed = false;
     for (long long u = u0; u < u1 && !failed;) {
@@ -261,30 +266,36 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
         const int begin = p.rows.begin(r);
 
         // ring: stage s holds block b0 + s, b0 + s + ST, ...; a block without a page is skipped (bit of `there` not set)
-        const size_t head = static_cast<size_t>(page_blocks) * kPgBlock;
         const int32_t* table = p.pages.table + static_cast<size_t>(r) * p.pages.max_pages;
-        int table_base = b0 / page_blocks, pages32 = table_base + lane < p.pages.max_pages ? table[table_base + lane] : -1;
-        int next = b0, next_slot = table_base, next_inner = b0 - table_base * page_blocks;
+        int slot = b0 / page_blocks, in_page = b0 - slot * page_blocks, table_base = slot, next = b0;
+        int pages32 = table_base + lane < p.pages.max_pages ? table[table_base + lane] : -1;
         uint32_t there = 0;
+        const uint8_t* src = nullptr;    // next block's bytes
+        auto page_of_slot = [&]() {
+            const int page = __shfl_sync(0xffffffffu, pages32, slot - table_base);
+            src = static_cast<unsigned>(page) < static_cast<unsigned>(p.pages.num_pages) && q.len > 0
+                      ? p.pages.pool + ((static_cast<size_t>(page) * H + h) * page_blocks + in_page) * kPgBlock : nullptr;
+        };
+        page_of_slot();
         auto issue = [&](int stage) {    // requests block `next` into a stage that nobody reads any more
-            if (next_slot - table_base >= 32) {
-                table_base = next_slot;
-                pages32 = table_base + lane < p.pages.max_pages ? table[table_base + lane] : -1;
+            if (in_page == page_blocks) {
+                in_page = 0, ++slot;
+                if (slot - table_base == 32) {
+                    table_base = slot;
+                    pages32 = table_base + lane < p.pages.max_pages ? table[table_base + lane] : -1;
+                }
+                page_of_slot();
             }
-            const int page = __shfl_sync(0xffffffffu, pages32, next_slot - table_base);
-            const bool have = static_cast<unsigned>(page) < static_cast<unsigned>(p.pages.num_pages) && next * kPgTokens < q.len;
-            if (have) {
+            there &= ~(1u << stage);
+            if (src) {
                 if (lane == 0) {
                     mbar_expect_tx(&bars[stage], kPgBlock);
-                    bulk_g2s(ring + stage * kPgBlock, p.pages.pool + (static_cast<size_t>(page) * H + h) * head + static_cast<size_t>(next_inner) * kPgBlock,
-                             kPgBlock, &bars[stage]);
+                    bulk_g2s(ring + stage * kPgBlock, src, kPgBlock, &bars[stage]);
                 }
                 there |= 1u << stage;
-            } else {
-                there &= ~(1u << stage);
+                src += kPgBlock;
             }
-            ++next;
-            if (++next_inner == page_blocks) next_inner = 0, ++next_slot;
+            ++next, ++in_page;
         };
         __syncwarp();
 #pragma unroll
@@ -293,228 +304,225 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
 
         tree_load_query<BF16, ROWS>(p, begin, q.n, h, tile, operands, fact);
         __syncwarp();
-        uint32_t qz[MT][2];
-        float factor[MT][LR];
-        int row_of[MT][LR], token_of[MT][LR];   // row of the call and drafted token of a logical row; -1: none
+        uint32_t qz[NT][S::kParts];      // B operands of the k-step of the zero-points: the sums of row g of a tile
+        float factor[NT][2];             // of the lane's two rows of a tile, 2 cq and 2 cq + 1
+        int token_of[NT][2];             // their drafted tokens; -1: none
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const uint4 fa = fact[m * 16 + g];
-            const uint4 fb = S::kHalf ? make_uint4(0u, 0u, 0u, 0u) : fact[m * 16 + g + 8];
-            qz[m][0] = cq == 0 ? fa.x : cq == 1 ? fa.y : 0u, qz[m][1] = cq == 0 ? fb.x : cq == 1 ? fb.y : 0u;
+        for (int t = 0; t < NT; ++t) {
 #pragma unroll
-            for (int i = 0; i < LR; ++i) {
-                factor[m][i] = __uint_as_float(i ? fb.z : fa.z);
-                const int rho = tile * ROWS + (S::kSplit ? 8 * m + g : 16 * m + g + 8 * i);
-                token_of[m][i] = rho < q.n * p.G ? rho / p.G : -1;
-                row_of[m][i] = begin + token_of[m][i];
+            for (int part = 0; part < S::kParts; ++part) {
+                const uint4 f = fact[part * ROWS + 8 * t + g];
+                qz[t][part] = cq == 0 ? f.x : cq == 1 ? f.y : 0u;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                factor[t][e] = __uint_as_float(fact[8 * t + 2 * cq + e].z);
+                const int rho = tile * ROWS + 8 * t + 2 * cq + e;
+                token_of[t][e] = rho < q.n * p.G ? rho / p.G : -1;
             }
         }
 
-        const uint32_t query = smem_u32(operands);
-        float o[MT][16][4], z[MT][4], m_run[MT][LR], l_run[MT][LR];
+        float o[NT][8][4], z[NT][4], m_run[NT][2], l_run[NT][2];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
+        for (int t = 0; t < NT; ++t) {
 #pragma unroll
-            for (int nt = 0; nt < 16; ++nt)
+            for (int x = 0; x < 8; ++x)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.0f;
+                for (int i = 0; i < 4; ++i) o[t][x][i] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[m][i] = 0.0f;
+            for (int i = 0; i < 4; ++i) z[t][i] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < LR; ++i) m_run[m][i] = -INFINITY, l_run[m][i] = 0.0f;
+            for (int e = 0; e < 2; ++e) m_run[t][e] = -INFINITY, l_run[t][e] = 0.0f;
         }
-        int vexp = 8;                    // exponent field of the power of two that value scales are measured against
+        // value scales are measured against 2^(vexp - 126), the first power of two above them: weights carry 2^8 over it
+        int vexp = kTreeVexp;
+        const int plain_blocks = min(q.first, q.len) / kPgTokens;   // blocks that are context altogether
 
         int stage = 0;
-        for (int b = b0; b < b1; ++b, stage = stage + 1 == ST ? 0 : stage + 1) {
-            if (there >> stage & 1) {
-                if (!mbar_wait(&bars[stage], phases >> stage & 1, kTreeSite)) {
-                    failed = true;
-                    break;
+        auto process = [&](int b, auto plain_tag) {
+            constexpr bool kPlain = decltype(plain_tag)::value;
+            const uint8_t* blk = ring + stage * kPgBlock;
+            const uint32_t base = ring_at + stage * kPgBlock;
+            // ---- scores: row tiles of 16 tokens (8n + g and 8(n + 1) + g), column tiles of eight query rows
+            uint4 kw[4];
+            uint32_t kz[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                kw[n] = lds128(base + n * 512 + piece);
+                kz[n] = blk[kPgKz + 8 * n + g] * 0x00010001u;
+                if (S::kSplit) kz[n] = lessened(kz[n] | 0x64006400u, 0xe408e408u);   // - 1032
+                kz[n] &= cq == 0 ? 0xffffffffu : cq == 1 ? 0x0000ffffu : 0u;
+            }
+            float sc[NT][2][4];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sc[t][n][i] = 0.0f;
+#pragma unroll
+                    for (int part = 0; part < S::kParts; ++part) mma_f16(sc[t][n], kz[2 * n], kz[2 * n + 1], 0u, 0u, qz[t][part], 0u);
                 }
-                phases ^= 1u << stage;
-                const uint32_t base = smem_u32(ring + stage * kPgBlock);
-                const uint32_t piece = static_cast<uint32_t>(cq * 8 + (g ^ (2 * cq))) * 16;
-
-                // ---- scores
-                uint4 kw[4];
-                uint32_t kz[4];
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    kw[n] = lds128(base + n * 512 + piece);
-                    kz[n] = ring[stage * kPgBlock + kPgKz + 8 * n + g] * 0x00010001u;
-                    if (S::kSplit) kz[n] = lessened(kz[n] | 0x64006400u, 0xe408e408u);   // - 1032
-                    kz[n] &= cq == 0 ? 0xffffffffu : cq == 1 ? 0x0000ffffu : 0u;
-                }
-                float2 ks[4], vs[4];
-                uint32_t vz[4];
+            for (int c = 0; c < 4; ++c) {
+                uint4 qb[NT][S::kParts];   // query operands come from shared memory every time: the registers go to the sums
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    ks[n] = *reinterpret_cast<const float2*>(ring + stage * kPgBlock + kPgKs + (8 * n + 2 * cq) * 4);
-                    vs[n] = *reinterpret_cast<const float2*>(ring + stage * kPgBlock + kPgVs + (8 * n + 2 * cq) * 4);
-                    vz[n] = __byte_perm(*reinterpret_cast<const uint16_t*>(ring + stage * kPgBlock + kPgVz + 8 * n + 2 * cq), 0u, 0x4140u);
-                    if (S::kSplit) vz[n] = lessened(vz[n] | 0x64006400u, 0xe408e408u);   // - 1032
-                }
-                float sc[MT][4][4];
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
+                    for (int part = 0; part < S::kParts; ++part) qb[t][part] = lds128(query + ((t * S::kParts + part) * 4 + c) * 512);
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
+                for (int n = 0; n < 2; ++n) {
+                    uint32_t r[2][4];      // the lane's word of two 8-token groups as four operand pairs each
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) sc[m][n][i] = 0.0f;
-                        mma_f16(sc[m][n], qz[m][0], qz[m][1], 0u, 0u, kz[n], 0u);
-                    }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint4 a[MT], a8[MT];   // query operands come from shared memory every time: registers go to the sums
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        a[m] = lds128(query + tree_operand(m * 16 + g, cq, c));
-                        a8[m] = S::kHalf ? make_uint4(0u, 0u, 0u, 0u) : lds128(query + tree_operand(m * 16 + g + 8, cq, c));
-                    }
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const uint32_t w = c == 0 ? kw[n].x : c == 1 ? kw[n].y : c == 2 ? kw[n].z : kw[n].w, y = w >> 8;
-                        uint32_t r0 = w & 0x000f000fu, r1 = w & 0x00f000f0u, r2 = y & 0x000f000fu, r3 = y & 0x00f000f0u;
+                    for (int i = 0; i < 2; ++i) {
+                        const uint4& x = kw[2 * n + i];
+                        const uint32_t w = c == 0 ? x.x : c == 1 ? x.y : c == 2 ? x.z : x.w, y = w >> 8;
+                        r[i][0] = w & 0x000f000fu, r[i][1] = w & 0x00f000f0u, r[i][2] = y & 0x000f000fu, r[i][3] = y & 0x00f000f0u;
                         if (S::kSplit) {
-                            r0 = lessened(r0 | 0x64006400u, 0xe408e408u), r1 = lessened(r1 | 0x64006400u, 0xe480e480u);   // - 1032, - 1152
-                            r2 = lessened(r2 | 0x64006400u, 0xe408e408u), r3 = lessened(r3 | 0x64006400u, 0xe480e480u);
-                        }
 #pragma unroll
-                        for (int m = 0; m < MT; ++m) {
-                            mma_f16(sc[m][n], a[m].x, a8[m].x, a[m].y, a8[m].y, r0, r1);
-                            mma_f16(sc[m][n], a[m].z, a8[m].z, a[m].w, a8[m].w, r2, r3);
+                            for (int e = 0; e < 4; ++e) r[i][e] = lessened(r[i][e] | 0x64006400u, (e & 1) ? 0xe480e480u : 0xe408e408u);   // - 1152 : - 1032
                         }
                     }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int part = 0; part < S::kParts; ++part) {
+                            mma_f16(sc[t][n], r[0][0], r[1][0], r[0][1], r[1][1], qb[t][part].x, qb[t][part].y);
+                            mma_f16(sc[t][n], r[0][2], r[1][2], r[0][3], r[1][3], qb[t][part].z, qb[t][part].w);
+                        }
                 }
-                uint4 vw[4];
+            }
+            float ks[4], vs[4];            // of the lane's tokens 8n + g
+            uint32_t vz[4];
+            uint4 vw[4];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) vw[w] = lds128(base + kPgV + w * 512 + piece);
-                // the stage has been read: its next block may come
-                __syncwarp();
-                if (next < b1) issue(stage);
+            for (int n = 0; n < 4; ++n) {
+                ks[n] = *reinterpret_cast<const float*>(blk + kPgKs + (8 * n + g) * 4);
+                vs[n] = *reinterpret_cast<const float*>(blk + kPgVs + (8 * n + g) * 4);
+                vz[n] = __byte_perm(*reinterpret_cast<const uint16_t*>(blk + kPgVz + 8 * n + 2 * cq), 0u, 0x4140u);
+                if (S::kSplit) vz[n] = lessened(vz[n] | 0x64006400u, 0xe408e408u);   // - 1032
+                vw[n] = lds128(base + kPgV + n * 512 + piece);
+            }
+            __syncwarp();                 // the stage has been read: its next block may come
+            if (next < b1) issue(stage);
 
-                // ---- which tokens are seen; slots that hold nothing may hold anything, NaN included
-                const bool plain = (b + 1) * kPgTokens <= q.first && (b + 1) * kPgTokens <= q.len;   // the whole block is context
-                uint32_t seen[MT][LR];
+            // ---- which tokens are seen; slots that hold nothing may hold anything, NaN included
+            uint32_t seen[NT][2];
+            if (!kPlain) {
+                const int left = q.len - b * kPgTokens;
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int i = 0; i < LR; ++i) seen[m][i] = 0xffffffffu;
-                if (!plain) {
-                    const int left = q.len - b * kPgTokens;
+                    for (int e = 0; e < 2; ++e)
+                        seen[t][e] = token_of[t][e] >= 0 ? tree_seen(p, begin + token_of[t][e], token_of[t][e], b, q.first, q.len) >> g : 0u;
 #pragma unroll
-                    for (int m = 0; m < MT; ++m)
+                for (int n = 0; n < 4; ++n)
+                    if (8 * n + g >= left) vs[n] = 0.0f;
+            }
+            // ---- the power of two of the value scales
+            const float vtop = fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3]));
+            if (__any_sync(0xffffffffu, vtop >= __uint_as_float(static_cast<uint32_t>(vexp + 1) << 23))) {
+                uint32_t top = 0;         // the largest finite one
 #pragma unroll
-                        for (int i = 0; i < LR; ++i)
-                            seen[m][i] = token_of[m][i] >= 0 ? tree_seen(p, row_of[m][i], token_of[m][i], b, q.first, q.len) : 0u;
+                for (int n = 0; n < 4; ++n) top = max(top, __float_as_uint(vs[n]) < 0x7f800000u ? __float_as_uint(vs[n]) : 0u);
+                const int to = max(vexp, static_cast<int>(__reduce_max_sync(0xffffffffu, top) >> 23));
+                const float corr = __uint_as_float(static_cast<uint32_t>(max(1, 127 + vexp - to)) << 23);   // what is 2^126 smaller is gone
+                vexp = to;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[t][x][i] *= corr;
+                    z[t][0] *= corr, z[t][1] *= corr;
+                    l_run[t][0] *= corr, l_run[t][1] *= corr;
+                }
+            }
+            const float vshift = static_cast<float>(134 - vexp);   // weights and their sum carry 2^8 / 2^(vexp - 126)
+            uint32_t wb[NT][S::kParts][4];   // weights as B operands: tokens of group n, columns = rows
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float w[2][4];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float s[4], top = -INFINITY;
 #pragma unroll
                     for (int n = 0; n < 4; ++n) {
-                        if (8 * n + 2 * cq >= left) vs[n].x = 0.0f;
-                        if (8 * n + 2 * cq + 1 >= left) vs[n].y = 0.0f;
+                        s[n] = sc[t][n >> 1][2 * (n & 1) + e] * ks[n];
+                        if (!kPlain && !(seen[t][e] >> (8 * n) & 1)) s[n] = -INFINITY;
+                        top = fmaxf(top, s[n]);
+                    }
+                    top *= factor[t][e];
+                    if (__any_sync(0xffffffffu, top > m_run[t][e] + kTreeSlack)) {
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                        const float to = fmaxf(top, m_run[t][e]);
+                        const float corr = to > m_run[t][e] ? ex2(m_run[t][e] - to) : 1.0f;   // from -inf: 0
+                        m_run[t][e] = to, l_run[t][e] *= corr, z[t][e] *= corr;
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) o[t][x][e] *= corr, o[t][x][2 + e] *= corr;
+                    }
+                    const float ref = vshift - m_run[t][e];
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        const bool on = kPlain || (seen[t][e] >> (8 * n) & 1);
+                        const float pr = on ? ex2(fmaf(s[n], factor[t][e], ref)) : 0.0f;
+                        l_run[t][e] += pr;
+                        w[e][n] = on ? pr * vs[n] : 0.0f;
                     }
                 }
-                // ---- reference points: the power of two of the value scales, then each row's
-                uint32_t vtop = 0;
 #pragma unroll
                 for (int n = 0; n < 4; ++n) {
-                    const uint32_t a = __float_as_uint(vs[n].x), c = __float_as_uint(vs[n].y);
-                    vtop = max(vtop, max(a < 0x7f800000u ? a : 0u, c < 0x7f800000u ? c : 0u));
-                }
-                if (__any_sync(0xffffffffu, static_cast<int>(vtop >> 23) > vexp)) {
-                    const int to = max(vexp, static_cast<int>(__reduce_max_sync(0xffffffffu, vtop) >> 23));
-                    // 2^(vexp - to); what is 2^126 smaller is gone
-                    const float corr = __uint_as_float(static_cast<uint32_t>(max(1, 127 + vexp - to)) << 23);
-                    vexp = to;
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-#pragma unroll
-                        for (int nt = 0; nt < 16; ++nt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[m][nt][i] *= corr;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) z[m][i] *= corr;
+                    if constexpr (S::kSplit) {
+                        uint32_t hi, lo;
+                        split_half2(w[0][n], w[1][n], hi, lo);
+                        wb[t][0][n] = transpose8(hi), wb[t][1][n] = transpose8(lo);
+                    } else {
+                        const __half2 hw = __floats2half2_rn(w[0][n], w[1][n]);
+                        wb[t][0][n] = transpose8(*reinterpret_cast<const uint32_t*>(&hw));
                     }
                 }
-                const float vinv = __uint_as_float(static_cast<uint32_t>(261 - vexp) << 23);   // 2^8 / 2^(vexp - 126): scales become < 2^8
-                uint32_t wa[MT][2][4];   // weights as A operands of the two k-steps
+            }
+            // ---- O += codes . w: row tile 2w + j of dimensions 32w + 4g + {j, j + 2}
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int i = 0; i < LR; ++i) {
-                        float s[8], top = -INFINITY;
+                for (int part = 0; part < S::kParts; ++part)
 #pragma unroll
-                        for (int n = 0; n < 4; ++n)
+                    for (int k = 0; k < 2; ++k) mma_f16(z[t], vz[2 * k], 0u, vz[2 * k + 1], 0u, wb[t][part][2 * k], wb[t][part][2 * k + 1]);
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const float x = S::kSplit ? sc[m][n][e] + sc[m][n][2 + e] : sc[m][n][2 * i + e];
-                                float y = x * ((e ? ks[n].y : ks[n].x) * factor[m][i]);
-                                if (!plain && !(seen[m][i] >> (8 * n + 2 * cq + e) & 1)) y = -INFINITY;
-                                s[2 * n + e] = y, top = fmaxf(top, y);
-                            }
-                        if (__any_sync(0xffffffffu, top > m_run[m][i] + kTreeSlack)) {
-                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                            const float to = fmaxf(top, m_run[m][i]);
-                            const float corr = to > m_run[m][i] ? ex2(m_run[m][i] - to) : 1.0f;   // from -inf: 0
-                            m_run[m][i] = to, l_run[m][i] *= corr;
-#pragma unroll
-                            for (int nt = 0; nt < 16; ++nt) {
-                                if (S::kSplit) o[m][nt][0] *= corr, o[m][nt][1] *= corr, o[m][nt][2] *= corr, o[m][nt][3] *= corr;
-                                else o[m][nt][2 * i] *= corr, o[m][nt][2 * i + 1] *= corr;
-                            }
-                            if (S::kSplit) z[m][0] *= corr, z[m][1] *= corr, z[m][2] *= corr, z[m][3] *= corr;
-                            else z[m][2 * i] *= corr, z[m][2 * i + 1] *= corr;
-                        }
-#pragma unroll
-                        for (int n = 0; n < 4; ++n) {
-                            float w[2];
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const bool on = plain || (seen[m][i] >> (8 * n + 2 * cq + e) & 1);
-                                const float pr = on ? ex2(s[2 * n + e] - m_run[m][i]) : 0.0f;
-                                l_run[m][i] += pr;
-                                w[e] = on ? pr * ((e ? vs[n].y : vs[n].x) * vinv) : 0.0f;
-                            }
-                            // A registers of k-step n / 2: rows g, g + 8 for tokens of n-tile 2k, then of 2k + 1
-                            if (S::kSplit) {
-                                split_half2(w[0], w[1], wa[m][n >> 1][2 * (n & 1)], wa[m][n >> 1][2 * (n & 1) + 1]);
-                            } else {
-                                const __half2 hw = __floats2half2_rn(w[0], w[1]);
-                                wa[m][n >> 1][2 * (n & 1) + i] = *reinterpret_cast<const uint32_t*>(&hw);
-                                if (S::kHalf) wa[m][n >> 1][2 * (n & 1) + 1] = 0u;
-                            }
-                        }
-                    }
-                }
-                // ---- O += w . codes
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t x[4] = {vw[w].x, vw[w].y, vw[w].z, vw[w].w};
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) mma_f16(z[m], wa[m][k][0], wa[m][k][1], wa[m][k][2], wa[m][k][3], vz[2 * k], vz[2 * k + 1]);
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t select = j ? 0x00f000f0u : 0x000f000fu;
+                        uint32_t v[4] = {x[2 * k] & select, (x[2 * k] >> 8) & select, x[2 * k + 1] & select, (x[2 * k + 1] >> 8) & select};
+                        if (S::kSplit) {
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t x[4] = {vw[w].x, vw[w].y, vw[w].z, vw[w].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t select = (j & 1) ? 0x00f000f0u : 0x000f000fu;
-                        const int down = j < 2 ? 0 : 8;
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            uint32_t v0 = (x[2 * k] >> down) & select, v1 = (x[2 * k + 1] >> down) & select;
-                            if (S::kSplit) {
-                                v0 = lessened(v0 | 0x64006400u, (j & 1) ? 0xe480e480u : 0xe408e408u);   // - 1152 : - 1032
-                                v1 = lessened(v1 | 0x64006400u, (j & 1) ? 0xe480e480u : 0xe408e408u);
-                            }
-#pragma unroll
-                            for (int m = 0; m < MT; ++m) mma_f16(o[m][4 * w + j], wa[m][k][0], wa[m][k][1], wa[m][k][2], wa[m][k][3], v0, v1);
+                            for (int e = 0; e < 4; ++e) v[e] = lessened(v[e] | 0x64006400u, j ? 0xe480e480u : 0xe408e408u);   // - 1152 : - 1032
                         }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int part = 0; part < S::kParts; ++part)
+                                mma_f16(o[t][2 * w + j], v[0], v[1], v[2], v[3], wb[t][part][2 * k], wb[t][part][2 * k + 1]);
                     }
-                }
-            } else if (next < b1) {
-                __syncwarp();
-                issue(stage);
             }
+        };
+        for (int b = b0; b < b1; ++b, stage = stage + 1 == ST ? 0 : stage + 1) {
+            if (!(there >> stage & 1)) {
+                if (next < b1) issue(stage);
+                continue;
+            }
+            if (!mbar_wait(&bars[stage], phases >> stage & 1, kTreeSite)) {
+                failed = true;
+                break;
+            }
+            phases ^= 1u << stage;
+            if (b < plain_blocks) process(b, std::true_type{});
+            else process(b, std::false_type{});
         }
         if (failed) break;
 
@@ -523,47 +531,35 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
         const float c1 = __uint_as_float(static_cast<uint32_t>(vexp) << 23);   // 2^(vexp - 127), times 2 / 2^8 and the codes' 2^24 below
         float* piece_at = p.partial + static_cast<size_t>(2 * me + (u == u0 ? 0 : 1)) * ROWS * kTreeRow;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < LR; ++i) {
-                float l = l_run[m][i];
-                l += __shfl_xor_sync(0xffffffffu, l, 1), l += __shfl_xor_sync(0xffffffffu, l, 2);
-                if (token_of[m][i] < 0) continue;
-                const int rho = tile * ROWS + (S::kSplit ? 8 * m + g : 16 * m + g + 8 * i);
-                const int hq = h * p.G + rho - token_of[m][i] * p.G;
+            for (int e = 0; e < 2; ++e) {
+                float l = l_run[t][e];
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+                l = (l * 0x1p-7f) * c1;      // the weights' own power of two
+                if (token_of[t][e] < 0) continue;
+                const int row = 8 * t + 2 * cq + e, hq = h * p.G + tile * ROWS + row - token_of[t][e] * p.G;
+                const size_t out_at = (static_cast<size_t>(begin + token_of[t][e]) * p.Hq + hq) * kKvD;
                 const float inv = whole ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    float y[8];
+                    float y[4];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float* a = o[m][4 * w + j];
-                            const float x = S::kSplit ? a[c] + a[2 + c] : a[2 * i + c];
-                            const float zz = S::kSplit ? z[m][c] + z[m][2 + c] : z[m][2 * i + c];
-                            y[4 * c + j] = (fmaf(x, (j & 1) ? 0.0625f : 1.0f, -zz) * (S::kSplit ? 0x1p-7f : 0x1p17f)) * c1 * inv;
-                        }
-                    const int d = 32 * w + 8 * cq;
+                    for (int j = 0; j < 4; ++j)
+                        y[j] = (fmaf(o[t][2 * w + (j & 1)][(j & 2) + e], (j & 1) ? 0.0625f : 1.0f, -z[t][e]) * (S::kSplit ? 0x1p-7f : 0x1p17f)) * c1 * inv;
+                    const int d = 32 * w + 4 * g;
                     if (!whole) {
-                        float4* dst = reinterpret_cast<float4*>(piece_at + (rho - tile * ROWS) * kTreeRow + d);
-                        dst[0] = make_float4(y[0], y[1], y[2], y[3]), dst[1] = make_float4(y[4], y[5], y[6], y[7]);
+                        *reinterpret_cast<float4*>(piece_at + row * kTreeRow + d) = make_float4(y[0], y[1], y[2], y[3]);
                     } else if constexpr (BF16) {
-                        uint32_t bits[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const __nv_bfloat162 t = __floats2bfloat162_rn(y[2 * e], y[2 * e + 1]);
-                            bits[e] = *reinterpret_cast<const uint32_t*>(&t);
-                        }
-                        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + (static_cast<size_t>(row_of[m][i]) * p.Hq + hq) * kKvD + d) =
-                            make_uint4(bits[0], bits[1], bits[2], bits[3]);
+                        const __nv_bfloat162 u0 = __floats2bfloat162_rn(y[0], y[1]), u1 = __floats2bfloat162_rn(y[2], y[3]);
+                        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + out_at + d) =
+                            make_uint2(*reinterpret_cast<const uint32_t*>(&u0), *reinterpret_cast<const uint32_t*>(&u1));
                     } else {
-                        float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.out) + (static_cast<size_t>(row_of[m][i]) * p.Hq + hq) * kKvD + d);
-                        dst[0] = make_float4(y[0], y[1], y[2], y[3]), dst[1] = make_float4(y[4], y[5], y[6], y[7]);
+                        *reinterpret_cast<float4*>(static_cast<float*>(p.out) + out_at + d) = make_float4(y[0], y[1], y[2], y[3]);
                     }
                 }
-                if (!whole && cq == 0)
-                    *reinterpret_cast<float2*>(piece_at + (rho - tile * ROWS) * kTreeRow + kKvD) = make_float2(m_run[m][i], l);
+                if (!whole && g == 0) *reinterpret_cast<float2*>(piece_at + row * kTreeRow + kKvD) = make_float2(m_run[t][e], l);
             }
         if (b0 == 0 && !whole) {
             // the tile's later pieces: one in every warp until its last item

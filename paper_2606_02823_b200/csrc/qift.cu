@@ -1729,18 +1729,18 @@ int run_move(Kernel f32, Kernel bf16, int x_dtype, const KvMoveParams& p, cudaSt
 // Attention of trees: rows of a tile, by the mean of a request's rows for one KV head.
 inline int tree_rows(int total, int R, int G, bool bf16) {
     const long long mean = (static_cast<long long>(total) * G + R - 1) / R;
-    return mean <= 8 ? 8 : (!bf16 || mean <= 16) ? 16 : 32;
+    return mean <= 8 || !bf16 ? 8 : 16;
 }
-inline int tree_runs(int rows, bool bf16) { return sm_count() * ((bf16 ? rows <= 16 : rows <= 8) ? 12 : 8); }   // warps of the grid
+inline int tree_runs(int rows) { return sm_count() * (rows == 8 ? TreeShape<true, 8>::kWarps : TreeShape<true, 16>::kWarps); }   // warps of the grid
 // descriptors of the runs, then two pieces of a tile for each
-inline size_t tree_workspace(int rows, bool bf16) {
-    const size_t warps = static_cast<size_t>(tree_runs(rows, bf16));
+inline size_t tree_workspace(int rows) {
+    const size_t warps = static_cast<size_t>(tree_runs(rows));
     return warps * sizeof(int4) + 2 * warps * rows * kTreeRow * sizeof(float);
 }
 template <bool BF16, int ROWS>
 int run_tree(KvTreeParams p, void* workspace, cudaStream_t st) {
     using S = TreeShape<BF16, ROWS>;
-    const int runs = tree_runs(ROWS, BF16);
+    const int runs = tree_runs(ROWS);
     p.desc = static_cast<int4*>(workspace);
     p.partial = reinterpret_cast<float*>(p.desc + runs);
     const cudaError_t e = allow_smem(kv4_tree_mma_kernel<BF16, ROWS>, S::kSmem);
@@ -1811,7 +1811,7 @@ int qift_kv4_paged_keep(const int32_t* keep, const int32_t* kept_start, int tota
 
 size_t qift_kv4_paged_attention_workspace_bytes(int total, int R, int Hq, int H) {
     if (total <= 0 || R <= 0 || Hq <= 0 || H <= 0 || Hq % H != 0) return 0;
-    const size_t f = tree_workspace(tree_rows(total, R, Hq / H, false), false), b = tree_workspace(tree_rows(total, R, Hq / H, true), true);
+    const size_t f = tree_workspace(tree_rows(total, R, Hq / H, false)), b = tree_workspace(tree_rows(total, R, Hq / H, true));
     return f > b ? f : b;
 }
 
@@ -1835,8 +1835,8 @@ int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int rows = tree_rows(total, R, p.G, q_dtype == QIFT_BF16);
     if (q_dtype == QIFT_BF16)
-        return rows == 8 ? run_tree<true, 8>(p, workspace, st) : rows == 16 ? run_tree<true, 16>(p, workspace, st) : run_tree<true, 32>(p, workspace, st);
-    return rows == 8 ? run_tree<false, 8>(p, workspace, st) : run_tree<false, 16>(p, workspace, st);
+        return rows == 8 ? run_tree<true, 8>(p, workspace, st) : run_tree<true, 16>(p, workspace, st);
+    return run_tree<false, 8>(p, workspace, st);
 }
 
 size_t qift_lora_workspace_bytes(int M, int rank, int K) {

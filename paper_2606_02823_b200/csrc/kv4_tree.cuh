@@ -61,20 +61,89 @@ __device__ __forceinline__ uint32_t lessened(uint32_t x, uint32_t by) {   // fp1
     return y;
 }
 
-// What a call makes of a request.
+// What a call makes of a request, in row tiles of ROWS and units of UNIT tokens.
 struct TreeRequest {
-    int n, first, len, blocks, tiles;   // drafted tokens, cached before them, positions in all, blocks and row tiles (0 without rows)
+    int n, first, len, units, tiles;   // drafted tokens, cached before them, positions in all, units and row tiles (0 without rows)
 };
-template <int ROWS>
+template <int ROWS, int UNIT>
 __device__ __forceinline__ TreeRequest tree_request(const KvTreeParams& p, int r, int capacity) {
     TreeRequest q;
     q.n = p.rows.count(r), q.first = p.rows.first[r];
     const long long end = static_cast<long long>(q.first) + q.n;
     q.len = static_cast<int>(max(0ll, min(end, static_cast<long long>(capacity))));
-    q.blocks = q.n > 0 ? max(1, (q.len + kPgTokens - 1) / kPgTokens) : 0;   // rows over nothing still get their zeros
+    q.units = q.n > 0 ? max(1, (q.len + UNIT - 1) / UNIT) : 0;   // rows over nothing still get their zeros
     q.tiles = (q.n * p.G + ROWS - 1) / ROWS;
     return q;
 }
+
+// A run of the call's items (request, KV head, row tile, unit of tokens; in that order), tile by tile.
+template <int ROWS, int UNIT>
+struct TreeWalk {
+    long long u0, u1, run, u, at;   // the run's items, items of a run, the current item, items before request r
+    int r, capacity;
+    TreeRequest q;
+    int h, tile, b0, b1, begin;     // the current tile: KV head, row tile, units of it in this run, the request's first row
+    // executed by whole warps
+    __device__ __forceinline__ void start(const KvTreeParams& p, int me, int runs) {
+        const int lane = threadIdx.x & 31, R = p.rows.R;
+        capacity = p.pages.capacity();
+        auto items = [&](int i) {
+            if (i >= R) return 0ll;
+            const TreeRequest t = tree_request<ROWS, UNIT>(p, i, capacity);
+            return static_cast<long long>(t.tiles) * t.units * p.pages.H;
+        };
+        long long total = 0;
+        for (int base = 0; base < R; base += 32) total += items(base + lane);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        run = max(static_cast<long long>(kTreeMinRun), (total + runs - 1) / runs);
+        u0 = min(total, me * run), u1 = min(total, u0 + run), u = u0;
+        r = 0, at = 0, q = {};
+        if (u0 >= u1) return;
+        for (int base = 0;; base += 32) {
+            const long long n = items(base + lane);
+            long long scan = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long up = __shfl_up_sync(0xffffffffu, scan, o);
+                if (lane >= o) scan += up;
+            }
+            const uint32_t hit = __ballot_sync(0xffffffffu, at + scan > u0);
+            if (hit) {
+                const int who = __ffs(hit) - 1;
+                r = base + who;
+                at += __shfl_sync(0xffffffffu, scan - n, who);
+                break;
+            }
+            at += __shfl_sync(0xffffffffu, scan, 31);   // u0 < total: some request is hit before the requests end
+        }
+        q = tree_request<ROWS, UNIT>(p, r, capacity);
+    }
+    // The tile of item u; false at the run's end.
+    __device__ __forceinline__ bool tile_here(const KvTreeParams& p) {
+        if (u >= u1) return false;
+        for (;;) {
+            const long long n = static_cast<long long>(q.tiles) * q.units * p.pages.H;
+            if (u - at < n) break;
+            at += n;
+            q = tree_request<ROWS, UNIT>(p, ++r, capacity);
+        }
+        const long long inner = u - at;
+        const int tile_of = static_cast<int>(inner / q.units);
+        b0 = static_cast<int>(inner - static_cast<long long>(tile_of) * q.units);
+        b1 = static_cast<int>(min(static_cast<long long>(q.units), b0 + (u1 - u)));
+        h = tile_of / q.tiles, tile = tile_of - h * q.tiles;
+        begin = p.rows.begin(r);
+        return true;
+    }
+    __device__ __forceinline__ void next() { u += b1 - b0; }
+    __device__ __forceinline__ bool whole() const { return b0 == 0 && b1 == q.units; }
+    // What the join needs of a tile that begins in this run and ends in a later one: request, head (and whether its first piece
+    // is this run's second), row tile, pieces.
+    __device__ __forceinline__ int4 unfinished(int me) const {
+        return make_int4(r, h | (u != u0 ? 1 << 24 : 0), tile, static_cast<int>((u + q.units - 1) / run) - me + 1);
+    }
+};
 
 template <bool BF16, int ROWS>
 struct TreeShape {
@@ -204,66 +273,18 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
     __syncwarp();
     pdl_wait();
 
-    // this warp's run of items
-    const int cap = p.pages.capacity(), H = p.pages.H, R = p.rows.R;
-    const int warps = gridDim.x * S::kWarps, me = blockIdx.x * S::kWarps + warp;
-    long long total = 0;
-    for (int base = 0; base < R; base += 32) {
-        long long n = 0;
-        if (base + lane < R) {
-            const TreeRequest q = tree_request<ROWS>(p, base + lane, cap);
-            n = static_cast<long long>(q.tiles) * q.blocks * H;
-        }
-        total += n;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    const long long run = max(static_cast<long long>(kTreeMinRun), (total + warps - 1) / warps);
-    const long long u0 = min(total, me * run), u1 = min(total, u0 + run);
+    const int me = blockIdx.x * S::kWarps + warp;
+    TreeWalk<ROWS, kPgTokens> walk;
+    walk.start(p, me, gridDim.x * S::kWarps);
     int4 mine = make_int4(0, 0, 0, 0);   // the tile that begins here and ends later
-    int r = 0;
-    long long at = 0;                    // items before request r
-    TreeRequest q = {};
-    if (u0 < u1) {
-        for (int base = 0;; base += 32) {
-            long long n = 0;
-            if (base + lane < R) {
-                const TreeRequest t = tree_request<ROWS>(p, base + lane, cap);
-                n = static_cast<long long>(t.tiles) * t.blocks * H;
-            }
-            long long scan = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long up = __shfl_up_sync(0xffffffffu, scan, o);
-                if (lane >= o) scan += up;
-            }
-            const uint32_t hit = __ballot_sync(0xffffffffu, at + scan > u0);
-            if (hit) {
-                const int who = __ffs(hit) - 1;
-                r = base + who;
-                at += __shfl_sync(0xffffffffu, scan - n, who);
-                break;
-            }
-            at += __shfl_sync(0xffffffffu, scan, 31);   // u0 < total: some request is hit before the requests end
-        }
-        q = tree_request<ROWS>(p, r, cap);
-    }
-
     const int page_blocks = p.pages.page_tokens / kPgTokens;
     const uint32_t ring_at = smem_u32(ring), query = smem_u32(operands) + lane * 16;
     const uint32_t piece = static_cast<uint32_t>(cq * 8 + (g ^ (2 * cq))) * 16;
     uint32_t phases = 0;                 // parity of each stage's barrier
     bool failed = false;
-    for (long long u = u0; u < u1 && !failed;) {
-        while (u - at >= static_cast<long long>(q.tiles) * q.blocks * H) {   // on to the request of this item
-            at += static_cast<long long>(q.tiles) * q.blocks * H;
-            q = tree_request<ROWS>(p, ++r, cap);
-        }
-        const long long inner = u - at;
-        const int tile_of = static_cast<int>(inner / q.blocks), b0 = static_cast<int>(inner - static_cast<long long>(tile_of) * q.blocks);
-        const int h = tile_of / q.tiles, tile = tile_of - h * q.tiles;
-        const int b1 = static_cast<int>(min(static_cast<long long>(q.blocks), b0 + (u1 - u)));
-        const int begin = p.rows.begin(r);
+    for (; !failed && walk.tile_here(p); walk.next()) {
+        const TreeRequest q = walk.q;
+        const int r = walk.r, h = walk.h, tile = walk.tile, b0 = walk.b0, b1 = walk.b1, begin = walk.begin;
 
         // ring: stage s holds block b0 + s, b0 + s + ST, ...; a block without a page is skipped (bit of `there` not set)
         const int32_t* table = p.pages.table + static_cast<size_t>(r) * p.pages.max_pages;
@@ -274,7 +295,7 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
         auto page_of_slot = [&]() {
             const int page = __shfl_sync(0xffffffffu, pages32, slot - table_base);
             src = static_cast<unsigned>(page) < static_cast<unsigned>(p.pages.num_pages) && q.len > 0
-                      ? p.pages.pool + ((static_cast<size_t>(page) * H + h) * page_blocks + in_page) * kPgBlock : nullptr;
+                      ? p.pages.pool + ((static_cast<size_t>(page) * p.pages.H + h) * page_blocks + in_page) * kPgBlock : nullptr;
         };
         page_of_slot();
         auto issue = [&](int stage) {    // requests block `next` into a stage that nobody reads any more
@@ -527,9 +548,9 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
         if (failed) break;
 
         // ---- the tile, or this warp's piece of it
-        const bool whole = b0 == 0 && b1 == q.blocks;
+        const bool whole = walk.whole();
         const float c1 = __uint_as_float(static_cast<uint32_t>(vexp) << 23);   // 2^(vexp - 127), times 2 / 2^8 and the codes' 2^24 below
-        float* piece_at = p.partial + static_cast<size_t>(2 * me + (u == u0 ? 0 : 1)) * ROWS * kTreeRow;
+        float* piece_at = p.partial + static_cast<size_t>(2 * me + (walk.u == walk.u0 ? 0 : 1)) * ROWS * kTreeRow;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -561,13 +582,7 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
                 }
                 if (!whole && g == 0) *reinterpret_cast<float2*>(piece_at + row * kTreeRow + kKvD) = make_float2(m_run[t][e], l);
             }
-        if (b0 == 0 && !whole) {
-            // the tile's later pieces: one in every warp until its last item
-            const long long last = u + q.blocks - 1;
-            mine = make_int4(r, h, tile, static_cast<int>(last / run) - me + 1);
-            if (u != u0) mine.y |= 1 << 24;   // its first piece is this warp's second
-        }
-        u += b1 - b0;
+        if (b0 == 0 && !whole) mine = walk.unfinished(me);
     }
     if (failed) {   // copies in flight end (or are given up) before the shared memory does; whoever waits for this run's piece skips it
         mine = make_int4(0, 0, 0, 0);
@@ -591,7 +606,9 @@ kv4_tree_join_kernel(const KvTreeParams p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int r = d.x, h = d.y & 0xffffff, tile = d.z, pieces = d.w;
     const int begin = p.rows.begin(r), n = p.rows.count(r);
-    const int valid = min(ROWS, n * p.G - tile * ROWS);
+    const int row0 = 8 * blockIdx.y;     // rows of the tile for this CTA: eight
+    const int valid = min(8, min(ROWS, n * p.G - tile * ROWS) - row0);
+    if (valid <= 0) return;
     int share = kTreeJoinWarps;          // warps of a row: a power of two
     while (share > 1 && (kTreeJoinWarps / share < valid || share > pieces)) share >>= 1;
     const int rows_at_once = kTreeJoinWarps / share, sub = warp % share;
@@ -599,10 +616,10 @@ kv4_tree_join_kernel(const KvTreeParams p) {
     const float* first = p.partial + static_cast<size_t>(2 * blockIdx.x + (d.y >> 24)) * ROWS * kTreeRow;
     const float* rest = p.partial + static_cast<size_t>(blockIdx.x) * step;   // piece s > 0: rest + s * step
     for (int base = 0; base < valid; base += rows_at_once) {
-        const int row = base + warp / share;
+        const int local = base + warp / share, row = row0 + local;
         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         float m = -INFINITY, l = 0.0f;
-        if (row < valid) {
+        if (local < valid) {
             constexpr int kAhead = 4;
             for (int s0 = sub; s0 < pieces; s0 += share * kAhead) {
                 float4 x[kAhead];
@@ -641,7 +658,7 @@ kv4_tree_join_kernel(const KvTreeParams p) {
                 }
             }
         }
-        if (row < valid && sub == 0) {
+        if (local < valid && sub == 0) {
             const int rho = tile * ROWS + row, i = rho / p.G, hq = h * p.G + rho - i * p.G;
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;
             const size_t at = (static_cast<size_t>(begin + i) * p.Hq + hq) * kKvD + 4 * lane;

@@ -15,6 +15,7 @@
 #include "kv4.cuh"
 #include "kv4_paged.cuh"
 #include "kv4_tree.cuh"
+#include "kv4_tree_tc.cuh"
 #include "lora.cuh"
 #include "pack.cuh"
 #include "prefill.cuh"
@@ -1726,28 +1727,38 @@ int run_move(Kernel f32, Kernel bf16, int x_dtype, const KvMoveParams& p, cudaSt
     const dim3 grid(static_cast<unsigned>(most_blocks(p.rows.total, p.rows.R)), static_cast<unsigned>((p.pages.H + p.heads - 1) / p.heads));
     return cuda_status(launch_pdl(x_dtype == QIFT_BF16 ? bf16 : f32, grid, dim3(kPgThreads), 0, st, p));
 }
-// Attention of trees: rows of a tile, by the mean of a request's rows for one KV head.
+// Attention of trees: rows of a tile, by the mean of a request's rows for one KV head.  8 and 16: kv4_tree.cuh, 64 and 128: the tcgen05
+// kernel of kv4_tree_tc.cuh (bf16 calls).
 inline int tree_rows(int total, int R, int G, bool bf16) {
     const long long mean = (static_cast<long long>(total) * G + R - 1) / R;
-    return mean <= 8 || !bf16 ? 8 : 16;
+    return mean <= 8 || !bf16 ? 8 : mean <= 16 ? 16 : mean <= 64 ? 64 : 128;
 }
-inline int tree_runs(int rows) { return sm_count() * (rows == 8 ? TreeShape<true, 8>::kWarps : TreeShape<true, 16>::kWarps); }   // warps of the grid
+// runs that the items are dealt to: warps of the one kernel, CTAs of the other
+inline int tree_runs(int rows) { return sm_count() * (rows == 8 ? TreeShape<true, 8>::kWarps : rows == 16 ? TreeShape<true, 16>::kWarps : 1); }
 // descriptors of the runs, then two pieces of a tile for each
 inline size_t tree_workspace(int rows) {
-    const size_t warps = static_cast<size_t>(tree_runs(rows));
-    return warps * sizeof(int4) + 2 * warps * rows * kTreeRow * sizeof(float);
+    const size_t runs = static_cast<size_t>(tree_runs(rows));
+    return runs * sizeof(int4) + 2 * runs * rows * kTreeRow * sizeof(float);
 }
 template <bool BF16, int ROWS>
 int run_tree(KvTreeParams p, void* workspace, cudaStream_t st) {
-    using S = TreeShape<BF16, ROWS>;
     const int runs = tree_runs(ROWS);
     p.desc = static_cast<int4*>(workspace);
     p.partial = reinterpret_cast<float*>(p.desc + runs);
-    const cudaError_t e = allow_smem(kv4_tree_mma_kernel<BF16, ROWS>, S::kSmem);
-    if (e != cudaSuccess) return cuda_status(e);
-    const int rc = cuda_status(launch_pdl(kv4_tree_mma_kernel<BF16, ROWS>, dim3(runs / S::kWarps), dim3(32 * S::kWarps), S::kSmem, st, p));
+    int rc;
+    if constexpr (ROWS >= 64) {
+        auto kernel = kv4_tree_tc_kernel<128 / ROWS>;
+        const cudaError_t e = allow_smem(kernel, TtShape<128 / ROWS>::kSmem);
+        if (e != cudaSuccess) return cuda_status(e);
+        rc = cuda_status(launch_pdl(kernel, dim3(runs), dim3(kTtThreads), TtShape<128 / ROWS>::kSmem, st, p));
+    } else {
+        using S = TreeShape<BF16, ROWS>;
+        const cudaError_t e = allow_smem(kv4_tree_mma_kernel<BF16, ROWS>, S::kSmem);
+        if (e != cudaSuccess) return cuda_status(e);
+        rc = cuda_status(launch_pdl(kv4_tree_mma_kernel<BF16, ROWS>, dim3(runs / S::kWarps), dim3(32 * S::kWarps), S::kSmem, st, p));
+    }
     if (rc != QIFT_OK) return rc;
-    return cuda_status(launch_pdl(kv4_tree_join_kernel<BF16, ROWS>, dim3(runs), dim3(32 * kTreeJoinWarps), 0, st, p));
+    return cuda_status(launch_pdl(kv4_tree_join_kernel<BF16, ROWS>, dim3(runs, ROWS / 8), dim3(32 * kTreeJoinWarps), 0, st, p));
 }
 }  // namespace
 
@@ -1835,7 +1846,10 @@ int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int rows = tree_rows(total, R, p.G, q_dtype == QIFT_BF16);
     if (q_dtype == QIFT_BF16)
-        return rows == 8 ? run_tree<true, 8>(p, workspace, st) : run_tree<true, 16>(p, workspace, st);
+        return rows == 8    ? run_tree<true, 8>(p, workspace, st)
+               : rows == 16 ? run_tree<true, 16>(p, workspace, st)
+               : rows == 64 ? run_tree<true, 64>(p, workspace, st)
+                            : run_tree<true, 128>(p, workspace, st);
     return run_tree<false, 8>(p, workspace, st);
 }
 

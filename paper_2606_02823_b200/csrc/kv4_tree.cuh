@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(32 * TreeShape<BF16, ROWS>::kWarps, 1)
 kv4_tree_mma_kernel(const KvTreeParams p) {
     using S = TreeShape<BF16, ROWS>;
     constexpr int NT = S::kNT, ST = S::kStages;
-    extern __shared__ __align__(16) uint8_t smem[];
+    extern __shared__ __align__(128) uint8_t smem[];
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, cq = lane & 3;
     uint8_t* ring = smem + warp * S::kWarpBytes;

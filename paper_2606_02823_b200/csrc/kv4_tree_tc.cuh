@@ -2,15 +2,14 @@
 // items and the same pieces, joined by the same kernel.  An item is 128 tokens (four blocks) of one row tile.
 //
 //   S[128 rows][128 tokens] = Q (tensor memory) x K^T (shared memory),     O[128 rows][128 dims] += P (tensor memory) x V
-// Rows are the lanes of tensor memory, so a thread owns a row: maximum, sum and rescaling stay in it.
-//   warps 0-3    softmax, one thread per lane: scores from tensor memory in two halves of 64 tokens, weights back as fp16
-//   warps 4-11   conversion: every warp has one of the four blocks of every other item; codes less their zero-points become fp16
-//                (exactly: (c - z) * 2^-24, odd dimensions * 2^-20) in the 128-byte-swizzled tiles that the products read.  A warp
-//                fetches its own blocks two items ahead, 4416-byte bulk copies
-//   warp 12      tensor memory and the two products: S of the next item is issued before O of this one, so the tensor cores
+// Rows are the lanes of tensor memory, so a thread has a row: maximum, sum and rescaling stay in it.
+//   warps 0-7    softmax, two warps for 32 rows: scores of 64 of the item's tokens each, weights back as fp16.  The two agree on the
+//                row's reference point through shared memory, once per item
+//   warps 8-14   conversion, block by block in turn: codes less their zero-points become fp16 (exactly: (c - z) * 2^-24, odd
+//                dimensions * 2^-20) in the 128-byte-swizzled tiles that the products read.  A warp fetches its own blocks two
+//                ahead, 4416-byte bulk copies
+//   warp 15      tensor memory and the two products: S of the next item is issued before O of this one, so the tensor cores
 //                work while the softmax does
-// REP = 2 serves tiles of up to 64 rows: lanes 64 .. 127 hold the same rows as 0 .. 63 and take the second 64 tokens of an item (the
-// other half of their P stays zero), which halves the softmax per warp; the two halves of O meet in shared memory at the end.
 // What bounds it, per item of 128 tokens: the tensor cores (2 x 8 instructions of 64 cycles), the exponentials (128 rows x 128 at 16
 // a cycle) and shared memory (64 KB of tiles written, 64 KB read) each take about 1024 cycles.
 #pragma once
@@ -21,18 +20,37 @@
 
 namespace qift {
 
+constexpr int kTtRows = 128;                 // rows of a tile
 constexpr int kTtUnit = 128;                 // tokens of an item
-constexpr int kTtThreads = 32 * 13;
+constexpr int kTtConvert = 7;                // conversion warps
+constexpr int kTtThreads = 32 * (8 + kTtConvert + 1);
 constexpr int kTtRing = 2;                   // raw blocks of a conversion warp
 constexpr int kTtScaleBytes = 2 * kTtUnit * 4 + 32;   // scales of keys and values; per block: largest value scale, whether it is there
-constexpr int kTtMeet = 68;                  // floats of a row where the halves meet (64 of a numerator, reference point, sum)
+constexpr int kTtStage = 4 * 16 * 256;       // query operands on their way to tensor memory: 16 rows of each lane quarter
+constexpr int kTtSmem = 1024 + 4 * 32768 + kTtConvert * kTtRing * kPgBlock + 4 * kTtScaleBytes + kTtStage + 2 * 8 * 32 * 4 + 512;
 constexpr uint32_t kTtS = 0, kTtO = 256, kTtP = 384, kTtQ = 448;   // tensor-memory columns: two S, O, P, Q
 
-template <int REP>
-struct TtShape {
-    static constexpr int kRows = 128 / REP;
-    static constexpr int kSmem = 1024 + 4 * 32768 + 8 * kTtRing * kPgBlock + 4 * kTtScaleBytes + (REP == 2 ? 64 * kTtMeet * 4 : 0) + 512;
-};
+// As mbar_wait, polling without a time hint: these waits are short and mostly over when they begin.
+__device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, unsigned int site) {
+    const uint32_t at = smem_u32(bar);
+    uint64_t t0 = 0;
+    for (uint32_t tries = 0;; ++tries) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done) : "r"(at), "r"(parity) : "memory");
+        if (done) return true;
+        if ((tries & 63) == 63) {
+            const uint64_t t = global_timer_ns();
+            if (t0 == 0) t0 = t;
+            else if (t - t0 > kWaitLimitNs) break;
+        }
+    }
+    report_timeout(site);
+    return false;
+}
 
 // D[tmem] (+)= A[tmem] * B[smem descriptor], fp16 operands, fp32 sums
 __device__ __forceinline__ void tc_mma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -47,30 +65,30 @@ __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.a
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-// Pairs of fp32 values in one instruction.
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 d;
-    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+        "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
 }
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 d;
-    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
+// Pairs of fp32 values (bit patterns, neighbouring registers) in one instruction, in place: x = x * y, x = x * y + z.
+__device__ __forceinline__ void mul2(uint32_t& x0, uint32_t& x1, uint32_t y0, uint32_t y1) {
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+r"(x0), "+r"(x1) : "r"(y0), "r"(y1));
 }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
+__device__ __forceinline__ void fma2(uint32_t& x0, uint32_t& x1, uint64_t y, uint64_t z) {
+    asm("{\n\t.reg .b64 x;\n\tmov.b64 x, {%0, %1};\n\tfma.rn.f32x2 x, x, %2, %3;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+r"(x0), "+r"(x1) : "l"(y), "l"(z));
 }
+__device__ __forceinline__ void add2(uint64_t& sum, uint32_t x0, uint32_t x1) {
+    asm("{\n\t.reg .b64 x;\n\tmov.b64 x, {%1, %2};\n\tadd.rn.f32x2 %0, %0, x;\n\t}" : "+l"(sum) : "r"(x0), "r"(x1));
+}
+__device__ __forceinline__ uint64_t both(float x) { return static_cast<uint64_t>(__float_as_uint(x)) << 32 | __float_as_uint(x); }
+__device__ __forceinline__ float sum2(uint64_t x) { return __uint_as_float(static_cast<uint32_t>(x)) + __uint_as_float(static_cast<uint32_t>(x >> 32)); }
 
 // Items of a run one by one: a tile's units are consecutive.
-template <int ROWS>
 struct TtItems {
-    TreeWalk<ROWS, kTtUnit> w;
+    TreeWalk<kTtRows, kTtUnit> w;
     int unit;          // the item's unit within its tile
     uint32_t n;        // items of this run before it
     bool valid;
@@ -78,32 +96,32 @@ struct TtItems {
         w.start(p, blockIdx.x, gridDim.x);
         n = 0, valid = w.tile_here(p), unit = valid ? w.b0 : 0;
     }
-    __device__ __forceinline__ void next(const KvTreeParams& p) {
-        ++n;
-        if (++unit == w.b1) {
-            w.next();
-            valid = w.tile_here(p);
-            if (valid) unit = w.b0;
+    __device__ __forceinline__ void to(const KvTreeParams& p, uint32_t item) {
+        while (valid && n < item) {
+            ++n;
+            if (++unit == w.b1) {
+                w.next();
+                valid = w.tile_here(p);
+                if (valid) unit = w.b0;
+            }
         }
     }
 };
 
-template <int REP>
 __global__ void __launch_bounds__(kTtThreads, 1)
 kv4_tree_tc_kernel(const KvTreeParams p) {
-    using S = TtShape<REP>;
-    constexpr int ROWS = S::kRows;
     constexpr uint32_t IDESC = (1u << 4) | ((128u / 8) << 17) | ((128u / 16) << 24);   // fp32 sums, fp16 operands, K-major, N = M = 128
-    extern __shared__ uint8_t smem_raw[];
+    extern __shared__ __align__(128) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     uint8_t* k_tiles = smem;                       // two, 32 KB each: two halves of 64 dimensions, 128 rows (tokens) of 128 bytes
     uint8_t* v_tiles = smem + 2 * 32768;           // two: two halves of 64 tokens, 128 rows (dimensions) of 128 bytes
     uint8_t* raw = smem + 4 * 32768;               // conversion warp, slot
-    uint8_t* scales = raw + 8 * kTtRing * kPgBlock;   // four items
-    float* meet = reinterpret_cast<float*>(scales + 4 * kTtScaleBytes);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(meet) + (REP == 2 ? 64 * kTtMeet * 4 : 0));
-    uint64_t* raw_full = bars;                     // [8 * kTtRing]
-    uint64_t* k_full = raw_full + 8 * kTtRing;     // [2] conversion -> products
+    uint8_t* scales = raw + kTtConvert * kTtRing * kPgBlock;   // four items
+    uint8_t* stage = scales + 4 * kTtScaleBytes;
+    float* tops = reinterpret_cast<float*>(stage + kTtStage);   // [item parity][softmax warp][lane]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(tops + 2 * 8 * 32);
+    uint64_t* raw_full = bars;                     // [kTtConvert * kTtRing]
+    uint64_t* k_full = raw_full + kTtConvert * kTtRing;   // [2] conversion -> products
     uint64_t* k_free = k_full + 2;                 // [2] products -> conversion
     uint64_t* v_full = k_free + 2;
     uint64_t* v_free = v_full + 2;
@@ -114,20 +132,21 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
     uint64_t* o_done = p_full + 1;                 // products -> softmax
     uint64_t* q_full = o_done + 1;                 // softmax -> products
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_full + 1);
+    static_assert((kTtConvert * kTtRing + 19) * 8 + 4 <= 512, "barriers");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_launch_dependents();
     if (tid == 0) {
-        for (int i = 0; i < 8 * kTtRing; ++i) mbar_init(&raw_full[i], 1);
+        for (int i = 0; i < kTtConvert * kTtRing; ++i) mbar_init(&raw_full[i], 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&k_full[i], 4), mbar_init(&v_full[i], 4), mbar_init(&s_free[i], 4);
+            mbar_init(&k_full[i], 4), mbar_init(&v_full[i], 4), mbar_init(&s_free[i], 8);
             mbar_init(&k_free[i], 1), mbar_init(&v_free[i], 1), mbar_init(&s_full[i], 1);
         }
         for (int i = 0; i < 4; ++i) mbar_init(&scale_full[i], 4);
-        mbar_init(p_full, 4), mbar_init(o_done, 1), mbar_init(q_full, 4);
+        mbar_init(p_full, 8), mbar_init(o_done, 1), mbar_init(q_full, 8);
         mbar_fence_init();
     }
-    if (warp == 12) {
+    if (warp == 15) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -137,363 +156,319 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
     const uint32_t tmem = *tmem_slot;
     pdl_wait();
 
-    if (warp < 4) {
-        // ------------------------------------------------------------------ softmax: a thread per lane
-        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp * 32) << 16);
-        const int row = (warp * 32 + lane) & (ROWS - 1);      // row of the tile
-        const int half = REP == 2 ? warp >> 1 : 0;            // REP = 2: the 64 tokens of an item that these lanes take
-        if (REP == 2) {                                       // the others' weights stay zero
-            tc_zero16(lanes + kTtP + 32 * (1 - half)), tc_zero16(lanes + kTtP + 32 * (1 - half) + 16);
-            tc_wait_st();
-        }
-        TreeWalk<ROWS, kTtUnit> walk;
+    // registers move to the softmax: 128 a thread at the launch, then 2 x 168 + 2 x 88 = 4 x 128 in the four warpgroups
+    if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp < 8) {
+        // ------------------------------------------------------------------ softmax: a thread per row and half of the tokens
+        const int quarter = warp & 3, half = warp >> 2;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+        const int row = quarter * 32 + lane;                  // row of the tile
+        // the two warps of a lane quarter meet here; a warp that has given up waiting still comes
+        auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory"); };
+        TreeWalk<kTtRows, kTtUnit> walk;
         walk.start(p, blockIdx.x, gridDim.x);
         int4 mine = make_int4(0, 0, 0, 0);
         uint32_t n = 0;                                       // items done
-        bool ok = true;   // once false the warp only keeps the barriers that the four share
+        bool ok = true;
         for (; walk.tile_here(p); walk.next()) {
             const TreeRequest q = walk.q;
-            const int begin = walk.begin, rho = walk.tile * ROWS + row;
-            const bool have = rho < q.n * p.G;                // this row exists
-            const bool active = walk.tile * ROWS + (warp * 32 & (ROWS - 1)) < q.n * p.G;   // some row of the warp does
-            const int token = have ? rho / p.G : -1, hq = have ? walk.h * p.G + rho - token * p.G : 0;
+            const int begin = walk.begin, rows = q.n * p.G - walk.tile * kTtRows;   // rows from this tile on
+            const bool have = row < rows;                     // this row exists
+            const bool active = quarter * 32 < rows;          // some row of the warp does
+            const int token = have ? (walk.tile * kTtRows + row) / p.G : -1;
+            const int hq = have ? walk.h * p.G + walk.tile * kTtRows + row - token * p.G : 0;
+            // ---- the query rows: rotated, scaled by a power of two each (largest value 2^7 .. 2^8), fp16, pairs (0,4) (1,5)/16 (2,6)
+            // (3,7)/16 of every eight dimensions -- the order of the codes in a word of the cache.  Eight lanes make a row; sixteen
+            // rows of the quarter at a time meet in shared memory and go to the lanes that own them, half of the columns per warp
             float factor = 0.0f;
-            if (ok) {   // the query row: rotated, scaled by a power of two (largest value 2^7 .. 2^8), fp16, pairs (0,4) (1,5)/16 (2,6) (3,7)/16
-                // of every eight dimensions -- the order of the codes in a word of the cache
-                float v[128];
+            if (active) {
+                uint8_t* here = stage + quarter * 16 * 256;
+                const int l = lane & 7, sub = lane >> 3;
+                uint32_t w[32];
 #pragma unroll
-                for (int i = 0; i < 128; ++i) v[i] = 0.0f;
-                if (have) {
-                    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q) +
-                                                                      static_cast<size_t>((static_cast<long long>(begin) + token) * p.q_stride) + hq * kKvD);
+                for (int i = 0; i < 32; ++i) w[i] = 0u;
+#pragma unroll 1
+                for (int round = 0; round < 2; ++round) {
+#pragma unroll 1
+                    for (int pass = 0; pass < 2; ++pass) {
+                        const int row16 = 8 * half + 4 * pass + sub, at = quarter * 32 + 16 * round + row16;
+                        float v[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const uint4 x = src[i];
-                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                        for (int e = 0; e < 16; ++e) v[e] = 0.0f;
+                        if (at < rows) {
+                            const int rho = walk.tile * kTtRows + at, t = rho / p.G;
+                            kv_load16<true>(p.q, static_cast<size_t>((static_cast<long long>(begin) + t) * p.q_stride) + (walk.h * p.G + rho - t * p.G) * kKvD + 16 * l, v);
+                        }
+                        kv_rotate16(v, l, p.q_had, p.q_inv_sqrt);
+                        float top = 0.0f;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            v[8 * i + 2 * k] = __uint_as_float(w[k] << 16), v[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-                    }
-                }
+                        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(v[e]));
 #pragma unroll
-                for (int h = 1; h < kKvD; h <<= 1) {
-                    if (h < p.q_had) {
+                        for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        const int field = max(16, min(254, static_cast<int>(__float_as_uint(top) >> 23)));
+                        const float up = __uint_as_float(static_cast<uint32_t>(min(254, 261 - field)) << 23);
+                        if (l == 0) tops[(4 * round + quarter) * 32 + row16] = __uint_as_float(static_cast<uint32_t>(max(1, field - 7)) << 23) * 0x1p24f * p.scale_log2;
 #pragma unroll
-                        for (int i = 0; i < 128; ++i)
-                            if (!(i & h)) {
-                                const float a = v[i], b = v[i + h];
-                                v[i] = a + b, v[i + h] = a - b;
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t x[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float f = (e & 1) ? 0.0625f * up : up;
+                                const __half2 hh = __floats2half2_rn(v[8 * c + e] * f, v[8 * c + e + 4] * f);
+                                x[e] = *reinterpret_cast<const uint32_t*>(&hh);
                             }
+                            *reinterpret_cast<uint4*>(here + row16 * 256 + (((2 * l + c) ^ row16) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+                        }
                     }
-                }
-                float top = 0.0f;
+                    meet();
+                    if ((lane >> 4) == round) {
+                        factor = tops[(4 * round + quarter) * 32 + (lane & 15)];
 #pragma unroll
-                for (int i = 0; i < 128; ++i) v[i] *= p.q_inv_sqrt, top = fmaxf(top, fabsf(v[i]));
-                const int field = max(16, min(254, static_cast<int>(__float_as_uint(top) >> 23)));
-                const float up = __uint_as_float(static_cast<uint32_t>(min(254, 261 - field)) << 23);
-                factor = __uint_as_float(static_cast<uint32_t>(max(1, field - 7)) << 23) * 0x1p24f * p.scale_log2;
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    uint32_t w[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int d = 64 * part + 8 * (i >> 2) + (i & 3);
-                        const float f = (i & 1) ? 0.0625f * up : up;
-                        const __half2 hh = __floats2half2_rn(v[d] * f, v[d + 4] * f);
-                        w[i] = *reinterpret_cast<const uint32_t*>(&hh);
+                        for (int c = 0; c < 8; ++c) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(here + (lane & 15) * 256 + (((8 * half + c) ^ (lane & 15)) << 4));
+                            w[4 * c] = x.x, w[4 * c + 1] = x.y, w[4 * c + 2] = x.z, w[4 * c + 3] = x.w;
+                        }
                     }
-                    tc_st32(lanes + kTtQ + 32 * part, w);
+                    meet();
                 }
+                tc_st32(lanes + kTtQ + 32 * half, w);
                 tc_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(q_full);
             }
-            float m = -INFINITY, vexp_f = 0.0f;
-            float2 l2 = make_float2(0.0f, 0.0f);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full);
+
+            float m = -INFINITY;
+            uint64_t l2 = 0;                                  // two sums of weights
             int vexp = kTreeVexp;
-            for (int unit = walk.b0; unit < walk.b1 && ok; ++unit, ++n) {
+            for (int unit = walk.b0; unit < walk.b1; ++unit, ++n) {
                 const bool fresh = unit == walk.b0;           // O holds nothing of this tile yet
-                if (!mbar_wait(&s_full[n & 1], (n >> 1) & 1, kTreeSite + 1) || !mbar_wait(&scale_full[n & 3], (n >> 2) & 1, kTreeSite + 2)) {
-                    ok = false;
-                    break;
-                }
+                if (ok) ok = mbar_wait_near(&s_full[n & 1], (n >> 1) & 1, kTreeSite + 1) && mbar_wait_near(&scale_full[n & 3], (n >> 2) & 1, kTreeSite + 2);
                 tc_fence_after();
-                bool o_waited = n == 0;                       // O of the item before is done
-                const uint8_t* sl = scales + (n & 3) * kTtScaleBytes;
-                const uint32_t* info = reinterpret_cast<const uint32_t*>(sl + 2 * kTtUnit * 4);
-                const uint32_t s_at = lanes + kTtS + (n & 1) * 128;
-                auto rescale = [&](float corr, int p_done) {  // O (and the weights of this item already given) times corr, row by row
-                    if (!fresh) {
-                        if (!o_waited) {
-                            if (!mbar_wait(o_done, (n - 1) & 1, kTreeSite + 3)) ok = false;
-                            o_waited = true;
-                            tc_fence_after();
-                        }
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t x[32];
-                            tc_ld32(lanes + kTtO + 32 * c, x);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * corr);
-                            tc_st32(lanes + kTtO + 32 * c, x);
-                        }
-                    }
-                    if (p_done) {
-                        uint32_t x[32];
-                        tc_ld32(lanes + kTtP, x);
-                        tc_wait_ld();
-                        const __half2 c2 = __float2half2_rn(corr);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&x[i]), c2);
-                            x[i] = *reinterpret_cast<const uint32_t*>(&y);
-                        }
-                        tc_st32(lanes + kTtP, x);
-                    }
-                    tc_wait_st();
-                    l2.x *= corr, l2.y *= corr;
+                bool o_waited = n == 0;                       // O of the item before is done, and its P has been read
+                auto wait_o = [&]() {
+                    if (!o_waited && ok) ok = mbar_wait_near(o_done, (n - 1) & 1, kTreeSite + 3);
+                    o_waited = true;
+                    tc_fence_after();
                 };
                 if (active) {
-                    // the power of two of the value scales, over the four blocks
-                    const uint32_t vt = max(max(info[0], info[1]), max(info[2], info[3]));
-                    if (static_cast<int>(vt >> 23) > vexp) {   // the same for all rows
-                        const int to = static_cast<int>(vt >> 23);
-                        rescale(__uint_as_float(static_cast<uint32_t>(max(1, 127 + vexp - to)) << 23), 0);
-                        vexp = to;
-                    }
-                    vexp_f = static_cast<float>(134 - vexp);
-                    const bool plain = (unit + 1) * kTtUnit <= min(q.first, q.len) && (info[4] & info[5] & info[6] & info[7]);
-#pragma unroll
-                    for (int sub = 0; sub < (REP == 2 ? 1 : 2); ++sub) {
-                        const int c0 = 64 * (REP == 2 ? half : sub);   // tokens of the item
-                        float2 s[32];
-                        {
-                            uint32_t x[32], y[32];
-                            tc_ld32(s_at + c0, x);
-                            tc_ld32(s_at + c0 + 32, y);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                s[i] = make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
-                                s[16 + i] = make_float2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1]));
-                            }
+                    const uint32_t sl = smem_u32(scales + (n & 3) * kTtScaleBytes);
+                    const uint4 vtops = lds128(sl + 2 * kTtUnit * 4), info = lds128(sl + 2 * kTtUnit * 4 + 16);
+                    const uint32_t vt = max(max(vtops.x, vtops.y), max(vtops.z, vtops.w));
+                    const bool plain = (unit + 1) * kTtUnit <= min(q.first, q.len) && (info.x & info.y & info.z & info.w);
+                    auto weigh = [&](auto plain_tag) {        // 64 tokens: scores -> weights
+                        constexpr bool kPlain = decltype(plain_tag)::value;
+                        uint32_t x[2][32];                    // scores, then weights, of tokens 32 i + 0 .. 31
+                        tc_ld32(lanes + kTtS + (n & 1) * 128 + 64 * half, x[0]);
+                        tc_ld32(lanes + kTtS + (n & 1) * 128 + 64 * half + 32, x[1]);
+                        tc_wait_ld();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&s_free[n & 1]);   // S may be written again
+                        uint32_t seen[2];
+                        if (!kPlain) {
+                            const uint32_t i0 = half ? info.z : info.x, i1 = half ? info.w : info.y;
+                            seen[0] = have && i0 ? tree_seen(p, begin + token, token, 4 * unit + 2 * half, q.first, q.len) : 0u;
+                            seen[1] = have && i1 ? tree_seen(p, begin + token, token, 4 * unit + 2 * half + 1, q.first, q.len) : 0u;
                         }
-                        if (REP == 2 || sub == 1) {            // S may be written again
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&s_free[n & 1]);
-                        }
-                        const float4* ks = reinterpret_cast<const float4*>(sl) + c0 / 4;
-                        const float4* vs = reinterpret_cast<const float4*>(sl + kTtUnit * 4) + c0 / 4;
-                        uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
-                        if (!plain) {
-#pragma unroll
-                            for (int b = 0; b < 2; ++b)
-                                seen[b] = have && info[4 + c0 / 32 + b] ? tree_seen(p, begin + token, token, 4 * unit + c0 / 32 + b, q.first, q.len) : 0u;
-                        }
-                        float top = -INFINITY;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float4 k4 = ks[i];
-                            s[2 * i] = mul2(s[2 * i], make_float2(k4.x, k4.y));
-                            s[2 * i + 1] = mul2(s[2 * i + 1], make_float2(k4.z, k4.w));
+                            const uint4 k4 = lds128(sl + 256 * half + 16 * i);
+                            uint32_t* y = &x[i >> 3][4 * (i & 7)];
+                            mul2(y[0], y[1], k4.x, k4.y), mul2(y[2], y[3], k4.z, k4.w);
                         }
-                        if (!plain) {
+                        if (!kPlain) {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                if (!(seen[i >> 4] >> (2 * (i & 15)) & 1)) s[i].x = -INFINITY;
-                                if (!(seen[i >> 4] >> (2 * (i & 15) + 1) & 1)) s[i].y = -INFINITY;
-                            }
+                            for (int i = 0; i < 64; ++i)
+                                if (!(seen[i >> 5] >> (i & 31) & 1)) x[i >> 5][i & 31] = 0xff800000u;   // -inf
                         }
+                        float best[4];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) top = fmaxf(top, fmaxf(s[i].x, s[i].y));
-                        top *= factor;
-                        if (__any_sync(0xffffffffu, top > m + kTreeSlack)) {
-                            const float to = top > m ? ceilf(top) : m;   // whole binary orders: the correction is exact
-                            const float corr = to > m ? ex2(m - to) : 1.0f;
-                            rescale(corr, sub);
+                        for (int c = 0; c < 4; ++c) best[c] = __uint_as_float(x[0][c]);
+#pragma unroll
+                        for (int i = 4; i < 64; i += 2)
+                            best[(i >> 1) & 3] = fmaxf(best[(i >> 1) & 3], fmaxf(__uint_as_float(x[i >> 5][i & 31]), __uint_as_float(x[i >> 5][(i & 31) + 1])));
+                        float top = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])) * factor;
+                        // the row's reference point, the same in both warps
+                        float* told = tops + (n & 1) * 256;
+                        told[warp * 32 + lane] = top;
+                        meet();
+                        top = fmaxf(top, told[(warp ^ 4) * 32 + lane]);
+                        const bool vgrew = static_cast<int>(vt >> 23) > vexp;   // the same for all rows
+                        if (vgrew || __any_sync(0xffffffffu, top > m + kTreeSlack)) {
+                            const float to = top > m + kTreeSlack ? ceilf(top) : m;
+                            float corr = to > m ? ex2(m - to) : 1.0f;
                             m = to;
-                        }
-                        const float2 f2 = make_float2(factor, factor);
-                        const float ref = vexp_f - m;
-                        const float2 r2 = make_float2(ref, ref);
-                        uint32_t out[32];
+                            if (vgrew) {
+                                const int v = static_cast<int>(vt >> 23);
+                                corr *= __uint_as_float(static_cast<uint32_t>(max(1, 127 + vexp - v)) << 23);
+                                vexp = v;
+                            }
+                            l2 = both(0.0f) | __float_as_uint(sum2(l2) * corr);
+                            if (!fresh) {
+                                wait_o();
+#pragma unroll 1
+                                for (int c = 0; c < 4; ++c) {   // O times corr, row by row; half of the columns per warp
+                                    uint32_t x[16];
+                                    tc_ld16(lanes + kTtO + 64 * half + 16 * c, x);
+                                    tc_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float4 v4 = vs[i];
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int j = 2 * i + e;       // tokens 2 j, 2 j + 1 of the 64
-                                const float2 a = fma2(s[j], f2, r2);
-                                float2 pr = make_float2(ex2(a.x), ex2(a.y));
-                                if (!plain) {
-                                    if (!(seen[j >> 4] >> (2 * (j & 15)) & 1)) pr.x = 0.0f;
-                                    if (!(seen[j >> 4] >> (2 * (j & 15) + 1) & 1)) pr.y = 0.0f;
+                                    for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * corr);
+                                    tc_st16(lanes + kTtO + 64 * half + 16 * c, x);
                                 }
-                                l2 = add2(l2, pr);
-                                float2 w = mul2(pr, e ? make_float2(v4.z, v4.w) : make_float2(v4.x, v4.y));
-                                if (!plain) {                  // a slot that is not seen may hold anything
-                                    if (!(seen[j >> 4] >> (2 * (j & 15)) & 1)) w.x = 0.0f;
-                                    if (!(seen[j >> 4] >> (2 * (j & 15) + 1) & 1)) w.y = 0.0f;
-                                }
-                                const __half2 hw = __floats2half2_rn(w.x, w.y);
-                                // token 32 b + 8 n + 2 cq + h stands at position 32 b + 8 cq + 2 n + h of the second product
-                                out[(j >> 4) * 16 + (j & 3) * 4 + ((j >> 2) & 3)] = *reinterpret_cast<const uint32_t*>(&hw);
+                                tc_wait_st();
                             }
                         }
-                        if (!o_waited) {                       // P of the item before has been read
-                            if (!mbar_wait(o_done, (n - 1) & 1, kTreeSite + 3)) ok = false;
-                            o_waited = true;
-                            tc_fence_after();
+                        const uint64_t f2 = both(factor);
+                        const uint64_t r2 = both(static_cast<float>(134 - vexp) - m);   // weights and their sum carry 2^8 / 2^(vexp - 126)
+                        uint64_t l3 = 0;
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            uint32_t out[16];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const uint4 v4 = lds128(sl + kTtUnit * 4 + 256 * half + 128 * b + 16 * i);
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const int j = 2 * i + e;   // tokens 2 j, 2 j + 1 of the 32
+                                    uint32_t &y0 = x[b][2 * j], &y1 = x[b][2 * j + 1];
+                                    fma2(y0, y1, f2, r2);
+                                    y0 = __float_as_uint(ex2(__uint_as_float(y0))), y1 = __float_as_uint(ex2(__uint_as_float(y1)));
+                                    if (!kPlain) {
+                                        if (!(seen[b] >> (2 * j) & 1)) y0 = 0u;
+                                        if (!(seen[b] >> (2 * j + 1) & 1)) y1 = 0u;
+                                    }
+                                    add2(e ? l3 : l2, y0, y1);
+                                    mul2(y0, y1, e ? v4.z : v4.x, e ? v4.w : v4.y);
+                                    if (!kPlain) {             // a slot that is not seen may hold anything
+                                        if (!(seen[b] >> (2 * j) & 1)) y0 = 0u;
+                                        if (!(seen[b] >> (2 * j + 1) & 1)) y1 = 0u;
+                                    }
+                                    const __half2 hw = __floats2half2_rn(__uint_as_float(y0), __uint_as_float(y1));
+                                    // token 32 b + 8 n + 2 cq + h stands at position 32 b + 8 cq + 2 n + h of the second product
+                                    out[(j & 3) * 4 + (j >> 2)] = *reinterpret_cast<const uint32_t*>(&hw);
+                                }
+                            }
+                            if (b == 0) wait_o();
+                            tc_st16(lanes + kTtP + 32 * half + 16 * b, out);
                         }
-                        tc_st32(lanes + kTtP + c0 / 2, out);
-                    }
-                    tc_wait_st();
+                        add2(l2, static_cast<uint32_t>(l3), static_cast<uint32_t>(l3 >> 32));
+                        tc_wait_st();
+                    };
+                    if (plain) weigh(std::true_type{});
+                    else weigh(std::false_type{});
                 } else {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&s_free[n & 1]);
-                    if (!o_waited && !mbar_wait(o_done, (n - 1) & 1, kTreeSite + 3)) ok = false;
+                    wait_o();
                 }
                 tc_fence_before();
-                __syncwarp();
                 ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
                 if (lane == 0) mbar_arrive(p_full);
             }
-            // ---- the tile, or this run's piece of it
-            if (ok && !mbar_wait(o_done, (n - 1) & 1, kTreeSite + 3)) ok = false;
+            // ---- the tile, or this run's piece of it: half of the columns per warp
+            if (ok) ok = mbar_wait_near(o_done, (n - 1) & 1, kTreeSite + 3);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
-            const bool whole = walk.whole();
-            const float c1 = __uint_as_float(static_cast<uint32_t>(vexp) << 23);
-            float l = ((l2.x + l2.y) * 0x1p-7f) * c1, own = 1.0f, other = 0.0f;
-            float* piece = p.partial + (static_cast<size_t>(2 * blockIdx.x + (walk.u == walk.u0 ? 0 : 1)) * ROWS + row) * kTreeRow;
-            if (REP == 2) {
-                // the second half hands over its numerator in two parts of 64 columns, its reference point and sum with each
-                m = l == 0.0f ? -INFINITY : m;
-            }
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                float y[64];
-                {
-                    uint32_t a[32], b[32];
-                    tc_ld32(lanes + kTtO + 64 * part, a);
-                    tc_ld32(lanes + kTtO + 64 * part + 32, b);
+            if (active) {
+                const bool whole = walk.whole();
+                const float c1 = __uint_as_float(static_cast<uint32_t>(vexp) << 23);
+                float l = (sum2(l2) * 0x1p-7f) * c1;
+                float* told = tops + (n & 1) * 256;
+                told[warp * 32 + lane] = l;
+                meet();
+                l += told[(warp ^ 4) * 32 + lane];
+                const float inv = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+                float* piece = p.partial + (static_cast<size_t>(2 * blockIdx.x + (walk.u == walk.u0 ? 0 : 1)) * kTtRows + row) * kTreeRow;
+                const size_t out_at = (static_cast<size_t>(begin + token) * p.Hq + hq) * kKvD;
+#pragma unroll 1
+                for (int part = 2 * half; part < 2 * half + 2; ++part) {
+                    uint32_t a[32];
+                    float y[32];
+                    tc_ld32(lanes + kTtO + 32 * part, a);
                     tc_wait_ld();
-                    // column 32 w + 8 j + g is dimension 32 w + 4 g + j; odd ones carry 16
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int at = 4 * (i & 7) + (i >> 3);
-                        const float f = ((i >> 3) & 1) ? 0.0625f : 1.0f;
-                        y[at] = (__uint_as_float(a[i]) * f * 0x1p17f) * c1;
-                        y[32 + at] = (__uint_as_float(b[i]) * f * 0x1p17f) * c1;
-                    }
-                }
-                if (REP == 2) {
-                    float* mt = meet + row * kTtMeet;
-                    if (half == 1) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) reinterpret_cast<float4*>(mt)[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-                        mt[64] = m, mt[65] = l;
-                    }
-                    asm volatile("bar.sync 1, 128;" ::: "memory");
-                    if (half == 0) {
-                        if (part == 0) {
-                            const float mo = mt[64], lo = mt[65], to = fmaxf(m, mo);
-                            own = m > -INFINITY ? ex2(m - to) : 0.0f, other = mo > -INFINITY ? ex2(mo - to) : 0.0f;
-                            l = l * own + lo * other, m = to;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float4 x = reinterpret_cast<const float4*>(mt)[i];
-                            const float xs[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) y[4 * i + e] = fmaf(y[4 * i + e], own, xs[e] * other);
-                        }
-                    }
-                    asm volatile("bar.sync 1, 128;" ::: "memory");
-                }
-                if (ok && have && half == 0) {
+                    for (int i = 0; i < 32; ++i)   // column 32 w + 8 j + g is dimension 32 w + 4 g + j; odd ones carry 16
+                        y[4 * (i & 7) + (i >> 3)] = (__uint_as_float(a[i]) * (((i >> 3) & 1) ? 0x1p13f : 0x1p17f)) * c1 * inv;
+                    if (!ok || !have) continue;
                     if (whole) {
-                        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-                        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + (static_cast<size_t>(begin + token) * p.Hq + hq) * kKvD + 64 * part);
+                        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + out_at + 32 * part);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
+                        for (int i = 0; i < 4; ++i) {
                             uint32_t bits[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const __nv_bfloat162 t = __floats2bfloat162_rn(l > 0.0f ? y[8 * i + 2 * e] * inv : 0.0f, l > 0.0f ? y[8 * i + 2 * e + 1] * inv : 0.0f);
+                                const __nv_bfloat162 t = __floats2bfloat162_rn(y[8 * i + 2 * e], y[8 * i + 2 * e + 1]);
                                 bits[e] = *reinterpret_cast<const uint32_t*>(&t);
                             }
                             dst[i] = make_uint4(bits[0], bits[1], bits[2], bits[3]);
                         }
                     } else {
-                        float4* dst = reinterpret_cast<float4*>(piece + 64 * part);
+                        float4* dst = reinterpret_cast<float4*>(piece + 32 * part);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) dst[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+                        for (int i = 0; i < 8; ++i) dst[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
                     }
                 }
+                if (ok && have && half == 0 && !whole) *reinterpret_cast<float2*>(piece + kKvD) = make_float2(m, l);
+                meet();              // the sums have been read before the next tile's factors come
             }
-            if (ok && have && half == 0 && !whole) *reinterpret_cast<float2*>(piece + kKvD) = make_float2(m, l);
-            tc_fence_before();   // O and Q have been read: the next tile's products may write
-            if (walk.b0 == 0 && !whole) mine = walk.unfinished(blockIdx.x);
+            tc_fence_before();       // O has been read: the next tile's products may write
+            if (walk.b0 == 0 && !walk.whole()) mine = walk.unfinished(blockIdx.x);
         }
         if (tid == 0) p.desc[blockIdx.x] = ok ? mine : make_int4(0, 0, 0, 0);
-    } else if (warp < 12) {
-        // ------------------------------------------------------------------ conversion: block `blk` of the items of one parity
-        const int k = warp - 4, blk = k & 3, par = k >> 2;
+    } else if (warp < 8 + kTtConvert) {
+        // ------------------------------------------------------------------ conversion: every seventh block
+        const int k = warp - 8;
         const int cq = lane >> 3, g = lane & 7;
         const int page_blocks = p.pages.page_tokens / kPgTokens;
         uint8_t* my_raw = raw + k * kTtRing * kPgBlock;
-        TtItems<ROWS> ahead, now;
+        TtItems ahead, now;
         now.start(p);
-        if (now.valid && par == 1) now.next(p);
         ahead = now;
-        uint32_t asked = 0, there = 0;                        // blocks asked for; which ring slots got one
-        int page = -1;
-        auto look_up = [&]() {                                // the page of `ahead`'s block: used when it is asked for, later
+        uint32_t want = k, block = k;                         // numbers of the next block to ask for and to convert
+        uint32_t there = 0;                                   // which ring slots got one
+        int slot_in = 0, slot = 0, page = -1;
+        auto look_up = [&]() {                                // the page of block `want`: used when it is asked for, later
+            ahead.to(p, want >> 2);
             page = -1;
             if (!ahead.valid) return;
-            const int b = 4 * ahead.unit + blk, slot = b / page_blocks;
-            if (b * kPgTokens < ahead.w.q.len) page = p.pages.table[static_cast<size_t>(ahead.w.r) * p.pages.max_pages + slot];
+            const int b = 4 * ahead.unit + (want & 3);
+            if (b * kPgTokens < ahead.w.q.len) page = p.pages.table[static_cast<size_t>(ahead.w.r) * p.pages.max_pages + b / page_blocks];
         };
         auto ask = [&]() {
-            const int slot = asked % kTtRing;
-            const int b = 4 * ahead.unit + blk;
+            const int b = 4 * ahead.unit + (want & 3);
             const bool have = ahead.valid && static_cast<unsigned>(page) < static_cast<unsigned>(p.pages.num_pages);
-            there = have ? there | (1u << slot) : there & ~(1u << slot);
+            there = have ? there | (1u << slot_in) : there & ~(1u << slot_in);
             if (have && lane == 0) {
-                mbar_expect_tx(&raw_full[k * kTtRing + slot], kPgBlock);
-                bulk_g2s(my_raw + slot * kPgBlock, p.pages.pool + ((static_cast<size_t>(page) * p.pages.H + ahead.w.h) * page_blocks + b % page_blocks) * kPgBlock,
-                         kPgBlock, &raw_full[k * kTtRing + slot]);
+                uint64_t* bar = &raw_full[k * kTtRing + slot_in];
+                mbar_expect_tx(bar, kPgBlock);
+                bulk_g2s(my_raw + slot_in * kPgBlock, p.pages.pool + ((static_cast<size_t>(page) * p.pages.H + ahead.w.h) * page_blocks + b % page_blocks) * kPgBlock,
+                         kPgBlock, bar);
             }
-            ++asked;
-            if (ahead.valid) ahead.next(p);
-            if (ahead.valid) ahead.next(p);
+            slot_in ^= 1, want += kTtConvert;
             look_up();
         };
+        static_assert(kTtRing == 2, "slots alternate");
         look_up();
-        for (int i = 0; i < kTtRing; ++i) ask();
-        uint32_t phases = 0, used = 0;
+        ask(), ask();
+        uint32_t phases = 0;
         bool ok = true;
-        while (now.valid && ok) {
-            const int buf = par;                              // items of one parity use one pair of tiles
-            const int slot = used % kTtRing;
+        for (now.to(p, block >> 2); now.valid; block += kTtConvert, now.to(p, block >> 2), slot ^= 1) {
+            const int buf = now.n & 1, blk = block & 3;
+            const uint32_t use = now.n >> 1;                  // how often this pair of tiles has been used before
             const bool have = there >> slot & 1;
             const uint8_t* src = my_raw + slot * kPgBlock;
             const uint32_t base = smem_u32(src);
-            const uint32_t use = now.n >> 1;                  // how often this pair of tiles has been used before
             if (have) {
-                if (!mbar_wait(&raw_full[k * kTtRing + slot], phases >> slot & 1, kTreeSite + 4)) {
+                if (!mbar_wait_near(&raw_full[k * kTtRing + slot], phases >> slot & 1, kTreeSite + 4)) {
                     ok = false;
                     break;
                 }
                 phases ^= 1u << slot;
                 there &= ~(1u << slot);
             }
-            if (use > 0 && !mbar_wait(&k_free[buf], (use - 1) & 1, kTreeSite + 5)) {
+            if (use > 0 && !mbar_wait_near(&k_free[buf], (use - 1) & 1, kTreeSite + 5)) {
                 ok = false;
                 break;
             }
@@ -530,7 +505,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
             __syncwarp();
             if (lane == 0) mbar_arrive(&k_full[buf]), mbar_arrive(&scale_full[now.n & 3]);
             // ---- values: row = dimension, 16-byte chunk = eight tokens
-            if (use > 0 && !mbar_wait(&v_free[buf], (use - 1) & 1, kTreeSite + 6)) {
+            if (use > 0 && !mbar_wait_near(&v_free[buf], (use - 1) & 1, kTreeSite + 6)) {
                 ok = false;
                 break;
             }
@@ -563,17 +538,14 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&v_full[buf]);
-            ++used;
             ask();
-            now.next(p);
-            if (now.valid) now.next(p);
         }
         if (!ok)   // copies in flight end (or are given up) before the shared memory does
             for (int s = 0; s < kTtRing; ++s)
                 if (there >> s & 1) mbar_wait(&raw_full[k * kTtRing + s], phases >> s & 1, kTreeSite + 4);
     } else {
         // ------------------------------------------------------------------ products
-        TreeWalk<ROWS, kTtUnit> walk;
+        TreeWalk<kTtRows, kTtUnit> walk;
         walk.start(p, blockIdx.x, gridDim.x);
         if (lane == 0) {
             const uint64_t kdesc = make_kmajor_sw128_desc(smem_u32(k_tiles)), vdesc = make_kmajor_sw128_desc(smem_u32(v_tiles));
@@ -581,8 +553,8 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
             bool ok = true;
             auto scores = [&](uint32_t i) {                   // S of item i
                 const uint32_t buf = i & 1, use = i >> 1;
-                if (!mbar_wait(&k_full[buf], use & 1, kTreeSite + 7)) return false;
-                if (use > 0 && !mbar_wait(&s_free[buf], (use - 1) & 1, kTreeSite + 8)) return false;
+                if (!mbar_wait_near(&k_full[buf], use & 1, kTreeSite + 7)) return false;
+                if (use > 0 && !mbar_wait_near(&s_free[buf], (use - 1) & 1, kTreeSite + 8)) return false;
                 tc_fence_after();
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
@@ -592,7 +564,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                 return true;
             };
             for (; ok && walk.tile_here(p); walk.next(), ++tiles) {
-                if (!mbar_wait(q_full, tiles & 1, kTreeSite + 9)) break;
+                if (!mbar_wait_near(q_full, tiles & 1, kTreeSite + 9)) break;
                 tc_fence_after();
                 if (!scores(n)) break;
                 for (int unit = walk.b0; unit < walk.b1; ++unit, ++n) {
@@ -601,7 +573,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                         ok = false;
                         break;
                     }
-                    if (!mbar_wait(p_full, n & 1, kTreeSite + 10) || !mbar_wait(&v_full[buf], use & 1, kTreeSite + 11)) {
+                    if (!mbar_wait_near(p_full, n & 1, kTreeSite + 10) || !mbar_wait_near(&v_full[buf], use & 1, kTreeSite + 11)) {
                         ok = false;
                         break;
                     }
@@ -619,7 +591,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 15) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }

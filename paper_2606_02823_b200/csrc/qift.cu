@@ -1727,11 +1727,11 @@ int run_move(Kernel f32, Kernel bf16, int x_dtype, const KvMoveParams& p, cudaSt
     const dim3 grid(static_cast<unsigned>(most_blocks(p.rows.total, p.rows.R)), static_cast<unsigned>((p.pages.H + p.heads - 1) / p.heads));
     return cuda_status(launch_pdl(x_dtype == QIFT_BF16 ? bf16 : f32, grid, dim3(kPgThreads), 0, st, p));
 }
-// Attention of trees: rows of a tile, by the mean of a request's rows for one KV head.  8 and 16: kv4_tree.cuh, 64 and 128: the tcgen05
-// kernel of kv4_tree_tc.cuh (bf16 calls).
+// Attention of trees: rows of a tile, by the mean of a request's rows for one KV head.  8 and 16: kv4_tree.cuh, 128: the tcgen05 kernel
+// of kv4_tree_tc.cuh (bf16 calls).
 inline int tree_rows(int total, int R, int G, bool bf16) {
     const long long mean = (static_cast<long long>(total) * G + R - 1) / R;
-    return mean <= 8 || !bf16 ? 8 : mean <= 16 ? 16 : mean <= 64 ? 64 : 128;
+    return mean <= 8 || !bf16 ? 8 : mean <= 16 ? 16 : kTtRows;
 }
 // runs that the items are dealt to: warps of the one kernel, CTAs of the other
 inline int tree_runs(int rows) { return sm_count() * (rows == 8 ? TreeShape<true, 8>::kWarps : rows == 16 ? TreeShape<true, 16>::kWarps : 1); }
@@ -1746,11 +1746,10 @@ int run_tree(KvTreeParams p, void* workspace, cudaStream_t st) {
     p.desc = static_cast<int4*>(workspace);
     p.partial = reinterpret_cast<float*>(p.desc + runs);
     int rc;
-    if constexpr (ROWS >= 64) {
-        auto kernel = kv4_tree_tc_kernel<128 / ROWS>;
-        const cudaError_t e = allow_smem(kernel, TtShape<128 / ROWS>::kSmem);
+    if constexpr (ROWS == kTtRows) {
+        const cudaError_t e = allow_smem(kv4_tree_tc_kernel, kTtSmem);
         if (e != cudaSuccess) return cuda_status(e);
-        rc = cuda_status(launch_pdl(kernel, dim3(runs), dim3(kTtThreads), TtShape<128 / ROWS>::kSmem, st, p));
+        rc = cuda_status(launch_pdl(kv4_tree_tc_kernel, dim3(runs), dim3(kTtThreads), kTtSmem, st, p));
     } else {
         using S = TreeShape<BF16, ROWS>;
         const cudaError_t e = allow_smem(kv4_tree_mma_kernel<BF16, ROWS>, S::kSmem);
@@ -1848,8 +1847,7 @@ int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int
     if (q_dtype == QIFT_BF16)
         return rows == 8    ? run_tree<true, 8>(p, workspace, st)
                : rows == 16 ? run_tree<true, 16>(p, workspace, st)
-               : rows == 64 ? run_tree<true, 64>(p, workspace, st)
-                            : run_tree<true, 128>(p, workspace, st);
+                            : run_tree<true, kTtRows>(p, workspace, st);
     return run_tree<false, 8>(p, workspace, st);
 }
 

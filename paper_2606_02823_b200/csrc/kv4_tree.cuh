@@ -49,6 +49,25 @@ constexpr float kTreeSlack = 6.0f;   // binary orders that a weight may exceed i
 constexpr int kTreeVexp = 40;           // exponent field of the smallest power of two that value scales are measured against
 constexpr int kTreeSite = 48;        // site of an expired wait
 
+// As mbar_wait, for waits that are short and mostly over when they begin: a loop of four instructions, bounded by its trips (a trip
+// is parked by the hardware for a while, so the limit is a good part of a second).
+constexpr uint32_t kNearTrips = 1u << 22;
+__device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, unsigned int site) {
+    uint32_t left = kNearTrips;
+    asm volatile(
+        "{\n\t.reg .pred p;\n"
+        "NEAR_AGAIN:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "@p bra NEAR_DONE;\n\t"
+        "add.u32 %0, %0, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %0, 0;\n\t"
+        "@p bra NEAR_AGAIN;\n"
+        "NEAR_DONE:\n\t}"
+        : "+r"(left) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    if (left == 0) report_timeout(site);
+    return left != 0;
+}
+
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -537,7 +556,7 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
                 if (next < b1) issue(stage);
                 continue;
             }
-            if (!mbar_wait(&bars[stage], phases >> stage & 1, kTreeSite)) {
+            if (!mbar_wait_near(&bars[stage], phases >> stage & 1, kTreeSite)) {
                 failed = true;
                 break;
             }

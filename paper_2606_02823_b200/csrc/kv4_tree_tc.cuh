@@ -1,17 +1,23 @@
 // Attention of drafted token trees with many rows per KV head (bf16 calls): the tcgen05 form of kv4_tree.cuh, on the same runs of
-// items and the same pieces, joined by the same kernel.  An item is 128 tokens (four blocks) of one row tile.
+// items and the same pieces, joined by the same kernel.  An item is 64 tokens (two blocks) of one row tile.
 //
-//   S[128 rows][128 tokens] = Q (tensor memory) x K^T (shared memory),     O[128 rows][128 dims] += P (tensor memory) x V
+//   S[128 rows][64 tokens] = Q (tensor memory) x K^T (shared memory),     O[128 rows][128 dims] += P (tensor memory) x V
 // Rows are the lanes of tensor memory, so a thread has a row: maximum, sum and rescaling stay in it.
-//   warps 0-7    softmax, two warps for 32 rows: scores of 64 of the item's tokens each, weights back as fp16.  The two agree on the
-//                row's reference point through shared memory, once per item
-//   warps 8-14   conversion, block by block in turn: codes less their zero-points become fp16 (exactly: (c - z) * 2^-24, odd
-//                dimensions * 2^-20) in the 128-byte-swizzled tiles that the products read.  A warp fetches its own blocks two
-//                ahead, 4416-byte bulk copies
-//   warp 15      tensor memory and the two products: S of the next item is issued before O of this one, so the tensor cores
-//                work while the softmax does
-// What bounds it, per item of 128 tokens: the tensor cores (2 x 8 instructions of 64 cycles), the exponentials (128 rows x 128 at 16
-// a cycle) and shared memory (64 KB of tiles written, 64 KB read) each take about 1024 cycles.
+//   warps 0-7    softmax, two warps for 32 rows, which take the items in turn: while one is at the exponentials of its item (the
+//                special-function pipe is the limit), the other scales the scores of the next and finds their maximum.  A row's
+//                reference point goes from item to item through shared memory
+//   warps 8-12   conversion: codes less their zero-points become fp16 (exactly: (c - z) * 2^-24, odd dimensions * 2^-20) in the
+//                128-byte-swizzled tiles that the products read.  A task is the keys or the values of one block; they are dealt out
+//                in the order in which the products need them (keys run three items ahead of values), so no task waits behind one
+//                that is needed later
+//   warp 13      fetches the blocks, one 4416-byte bulk copy each, up to twenty ahead (a lane looks up one block's page, 32 blocks at
+//                a time)
+//   warp 14      issues O as the weights and values of an item are there
+//   warp 15      tensor memory; issues S.  Two warps issue because a wait, the instructions and their commits take one several
+//                hundred cycles per item.  There are four S: a weight's way -- S, softmax, O -- takes about 2000 cycles, an item's
+//                share of the tensor cores 512.  The weights take the place of their S
+// What bounds it, per item: the tensor cores (8 instructions of 32 cycles, 4 of 64), the exponentials (128 rows x 64 at 16 a cycle) and
+// shared memory (32 KB of tiles written, 32 KB read) each take about 512 cycles.
 #pragma once
 
 #include "kv4_tree.cuh"
@@ -21,36 +27,17 @@
 namespace qift {
 
 constexpr int kTtRows = 128;                 // rows of a tile
-constexpr int kTtUnit = 128;                 // tokens of an item
-constexpr int kTtConvert = 7;                // conversion warps
-constexpr int kTtThreads = 32 * (8 + kTtConvert + 1);
-constexpr int kTtRing = 2;                   // raw blocks of a conversion warp
-constexpr int kTtScaleBytes = 2 * kTtUnit * 4 + 32;   // scales of keys and values; per block: largest value scale, whether it is there
-constexpr int kTtStage = 4 * 16 * 256;       // query operands on their way to tensor memory: 16 rows of each lane quarter
-constexpr int kTtSmem = 1024 + 4 * 32768 + kTtConvert * kTtRing * kPgBlock + 4 * kTtScaleBytes + kTtStage + 2 * 8 * 32 * 4 + 512;
-constexpr uint32_t kTtS = 0, kTtO = 256, kTtP = 384, kTtQ = 448;   // tensor-memory columns: two S, O, P, Q
-
-// As mbar_wait, polling without a time hint: these waits are short and mostly over when they begin.
-__device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, unsigned int site) {
-    const uint32_t at = smem_u32(bar);
-    uint64_t t0 = 0;
-    for (uint32_t tries = 0;; ++tries) {
-        uint32_t done;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done) : "r"(at), "r"(parity) : "memory");
-        if (done) return true;
-        if ((tries & 63) == 63) {
-            const uint64_t t = global_timer_ns();
-            if (t0 == 0) t0 = t;
-            else if (t - t0 > kWaitLimitNs) break;
-        }
-    }
-    report_timeout(site);
-    return false;
-}
+constexpr int kTtUnit = 64;                  // tokens of an item
+constexpr int kTtDepth = 4;                  // S under way
+constexpr int kTtTiles = 3;                  // tiles of keys, and of values
+constexpr int kTtTile = 16384;               // bytes of a tile
+constexpr int kTtConvert = 5;                // conversion warps
+constexpr int kTtThreads = 32 * (8 + kTtConvert + 3);
+constexpr int kTtRing = 20;                  // blocks on their way to the conversion; three items of them wait for their values to be due
+constexpr int kTtScaleBytes = 2 * kTtUnit * 4 + 16;   // scales of keys and values; per block: largest value scale, whether it is there
+constexpr int kTtStage = 8 * 4096;           // 4 KB of a softmax warp: query operands on their way in, results on their way out
+constexpr int kTtSmem = 1024 + 2 * kTtTiles * kTtTile + kTtRing * kPgBlock + 2 * kTtDepth * kTtScaleBytes + kTtStage + 2 * 128 * 8 + 768;
+constexpr uint32_t kTtS = 0, kTtO = 256, kTtQ = 384;   // tensor-memory columns: four S (the weights take the place of the first half), O, Q
 
 // D[tmem] (+)= A[tmem] * B[smem descriptor], fp16 operands, fp32 sums
 __device__ __forceinline__ void tc_mma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -60,6 +47,11 @@ __device__ __forceinline__ void tc_mma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, 
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d),
         "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -110,40 +102,44 @@ struct TtItems {
 
 __global__ void __launch_bounds__(kTtThreads, 1)
 kv4_tree_tc_kernel(const KvTreeParams p) {
-    constexpr uint32_t IDESC = (1u << 4) | ((128u / 8) << 17) | ((128u / 16) << 24);   // fp32 sums, fp16 operands, K-major, N = M = 128
+    // fp32 sums, fp16 operands, K-major, M = 128; N = 64 tokens or 128 dimensions
+    constexpr uint32_t S_IDESC = (1u << 4) | ((64u / 8) << 17) | ((128u / 16) << 24), O_IDESC = (1u << 4) | ((128u / 8) << 17) | ((128u / 16) << 24);
     extern __shared__ __align__(128) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    uint8_t* k_tiles = smem;                       // two, 32 KB each: two halves of 64 dimensions, 128 rows (tokens) of 128 bytes
-    uint8_t* v_tiles = smem + 2 * 32768;           // two: two halves of 64 tokens, 128 rows (dimensions) of 128 bytes
-    uint8_t* raw = smem + 4 * 32768;               // conversion warp, slot
-    uint8_t* scales = raw + kTtConvert * kTtRing * kPgBlock;   // four items
-    uint8_t* stage = scales + 4 * kTtScaleBytes;
-    float* tops = reinterpret_cast<float*>(stage + kTtStage);   // [item parity][softmax warp][lane]
-    uint64_t* bars = reinterpret_cast<uint64_t*>(tops + 2 * 8 * 32);
-    uint64_t* raw_full = bars;                     // [kTtConvert * kTtRing]
-    uint64_t* k_full = raw_full + kTtConvert * kTtRing;   // [2] conversion -> products
-    uint64_t* k_free = k_full + 2;                 // [2] products -> conversion
-    uint64_t* v_full = k_free + 2;
-    uint64_t* v_free = v_full + 2;
-    uint64_t* scale_full = v_free + 2;             // [4] conversion -> softmax
-    uint64_t* s_full = scale_full + 4;             // [2] products -> softmax
-    uint64_t* s_free = s_full + 2;                 // [2] softmax -> products
-    uint64_t* p_full = s_free + 2;                 // softmax -> products
-    uint64_t* o_done = p_full + 1;                 // products -> softmax
-    uint64_t* q_full = o_done + 1;                 // softmax -> products
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_full + 1);
-    static_assert((kTtConvert * kTtRing + 19) * 8 + 4 <= 512, "barriers");
+    uint8_t* k_tiles = smem;                       // [kTtTiles] two halves of 64 dimensions, 64 rows (tokens) of 128 bytes
+    uint8_t* v_tiles = smem + kTtTiles * kTtTile;  // [kTtTiles] 128 rows (dimensions) of 128 bytes, 64 tokens
+    uint8_t* raw = smem + 2 * kTtTiles * kTtTile;  // ring of blocks
+    uint8_t* scales = raw + kTtRing * kPgBlock;    // [2 * kTtDepth] items
+    uint8_t* stage = scales + 2 * kTtDepth * kTtScaleBytes;
+    float2* marks = reinterpret_cast<float2*>(stage + kTtStage);   // [item parity][row] reference points
+    uint64_t* bars = reinterpret_cast<uint64_t*>(marks + 2 * 128);
+    uint64_t* raw_full = bars;                     // [kTtRing] fetch -> conversion
+    uint64_t* raw_free = raw_full + kTtRing;       // [kTtRing] conversion -> fetch
+    uint64_t* k_full = raw_free + kTtRing;         // [kTtTiles] conversion -> products
+    uint64_t* k_free = k_full + kTtTiles;          // [2 * kTtTiles] products -> conversion, by item
+    uint64_t* v_free = k_free + 2 * kTtTiles;      // [2 * kTtTiles]
+    uint64_t* scale_full = v_free + 2 * kTtTiles;      // [2 * kTtDepth] conversion -> softmax
+    uint64_t* s_full = scale_full + 2 * kTtDepth;  // [kTtDepth] products -> softmax
+    uint64_t* p_full = s_full + kTtDepth;          // [kTtDepth] softmax (weights) and conversion (values) -> products
+    uint64_t* o_done = p_full + kTtDepth;          // [kTtDepth] products -> softmax
+    uint64_t* q_full = o_done + kTtDepth;          // softmax -> products
+    uint64_t* mark_full = q_full + 1;              // [2][4] reference points of an item, by lane quarter
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mark_full + 8);
+    int* raw_tokens = reinterpret_cast<int*>(tmem_slot + 1);   // [kTtRing] tokens of a block that hold something; 0: no such block
+    static_assert((2 * kTtRing + 5 * kTtTiles + 5 * kTtDepth + 9) * 8 + 4 + 4 * kTtRing <= 768, "barriers");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_launch_dependents();
     if (tid == 0) {
-        for (int i = 0; i < kTtConvert * kTtRing; ++i) mbar_init(&raw_full[i], 1);
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&k_full[i], 4), mbar_init(&v_full[i], 4), mbar_init(&s_free[i], 8);
-            mbar_init(&k_free[i], 1), mbar_init(&v_free[i], 1), mbar_init(&s_full[i], 1);
+        for (int i = 0; i < kTtRing; ++i) mbar_init(&raw_full[i], 1), mbar_init(&raw_free[i], 2);
+        for (int i = 0; i < kTtDepth; ++i) {
+            mbar_init(&p_full[i], 4 + 2), mbar_init(&s_full[i], 1), mbar_init(&o_done[i], 1);
         }
-        for (int i = 0; i < 4; ++i) mbar_init(&scale_full[i], 4);
-        mbar_init(p_full, 8), mbar_init(o_done, 1), mbar_init(q_full, 8);
+        for (int i = 0; i < kTtTiles; ++i) mbar_init(&k_full[i], 2);
+        for (int i = 0; i < 2 * kTtTiles; ++i) mbar_init(&k_free[i], 1), mbar_init(&v_free[i], 1);
+        for (int i = 0; i < 2 * kTtDepth; ++i) mbar_init(&scale_full[i], 2);
+        mbar_init(q_full, 8);
+        for (int i = 0; i < 8; ++i) mbar_init(&mark_full[i], 1);
         mbar_fence_init();
     }
     if (warp == 15) {
@@ -156,12 +152,12 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
     const uint32_t tmem = *tmem_slot;
     pdl_wait();
 
-    // registers move to the softmax: 128 a thread at the launch, then 2 x 168 + 2 x 88 = 4 x 128 in the four warpgroups
-    if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    // registers move to the softmax: 128 a thread at the launch, then 2 x 184 + 2 x 72 = 4 x 128 in the four warpgroups
+    if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp < 8) {
-        // ------------------------------------------------------------------ softmax: a thread per row and half of the tokens
-        const int quarter = warp & 3, half = warp >> 2;
+        // ------------------------------------------------------------------ softmax: a thread per row, items in turn
+        const int quarter = warp & 3, turn = warp >> 2;       // items n with (n & 1) == turn; half of the columns of Q and O
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
         const int row = quarter * 32 + lane;                  // row of the tile
         // the two warps of a lane quarter meet here; a warp that has given up waiting still comes
@@ -177,149 +173,155 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
             const bool have = row < rows;                     // this row exists
             const bool active = quarter * 32 < rows;          // some row of the warp does
             const int token = have ? (walk.tile * kTtRows + row) / p.G : -1;
-            const int hq = have ? walk.h * p.G + walk.tile * kTtRows + row - token * p.G : 0;
             // ---- the query rows: rotated, scaled by a power of two each (largest value 2^7 .. 2^8), fp16, pairs (0,4) (1,5)/16 (2,6)
-            // (3,7)/16 of every eight dimensions -- the order of the codes in a word of the cache.  Eight lanes make a row; sixteen
-            // rows of the quarter at a time meet in shared memory and go to the lanes that own them, half of the columns per warp
+            // (3,7)/16 of every eight dimensions -- the order of the codes in a word of the cache.  Eight lanes make a row; the rows
+            // of the quarter, sixteen per warp, meet in shared memory and go to the lanes that own them, half of the columns per warp
             float factor = 0.0f;
             if (active) {
-                uint8_t* here = stage + quarter * 16 * 256;
+                uint8_t* here = stage + quarter * 8192;
                 const int l = lane & 7, sub = lane >> 3;
+                uint4 in[2];                                  // the next four rows are on their way while these are rotated
+                auto fetch = [&](int pass) {
+                    in[0] = in[1] = make_uint4(0u, 0u, 0u, 0u);
+                    const int at = quarter * 32 + 16 * turn + 4 * pass + sub;
+                    if (pass < 4 && at < rows) {
+                        const int rho = walk.tile * kTtRows + at, t = rho / p.G;
+                        const uint4* src = reinterpret_cast<const uint4*>(
+                            static_cast<const uint16_t*>(p.q) + static_cast<size_t>((static_cast<long long>(begin) + t) * p.q_stride) + (walk.h * p.G + rho - t * p.G) * kKvD + 16 * l);
+                        in[0] = src[0], in[1] = src[1];
+                    }
+                };
+                fetch(0);
+#pragma unroll 1
+                for (int pass = 0; pass < 4; ++pass) {
+                    const int row32 = 16 * turn + 4 * pass + sub;
+                    float v[16];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t w[4] = {in[c].x, in[c].y, in[c].z, in[c].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[8 * c + 2 * e] = __uint_as_float(w[e] << 16), v[8 * c + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+                    }
+                    fetch(pass + 1);
+                    kv_rotate16(v, l, p.q_had, p.q_inv_sqrt);
+                    float top = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(v[e]));
+#pragma unroll
+                    for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    const int field = max(16, min(254, static_cast<int>(__float_as_uint(top) >> 23)));
+                    const float up = __uint_as_float(static_cast<uint32_t>(min(254, 261 - field)) << 23);
+                    if (l == 0) marks[quarter * 32 + row32].x = __uint_as_float(static_cast<uint32_t>(max(1, field - 7)) << 23) * 0x1p24f * p.scale_log2;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t x[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float f = (e & 1) ? 0.0625f * up : up;
+                            const __half2 hh = __floats2half2_rn(v[8 * c + e] * f, v[8 * c + e + 4] * f);
+                            x[e] = *reinterpret_cast<const uint32_t*>(&hh);
+                        }
+                        *reinterpret_cast<uint4*>(here + row32 * 256 + (((2 * l + c) ^ (row32 & 15)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+                    }
+                }
+                meet();
+                factor = marks[row].x;
                 uint32_t w[32];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) w[i] = 0u;
-#pragma unroll 1
-                for (int round = 0; round < 2; ++round) {
-#pragma unroll 1
-                    for (int pass = 0; pass < 2; ++pass) {
-                        const int row16 = 8 * half + 4 * pass + sub, at = quarter * 32 + 16 * round + row16;
-                        float v[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) v[e] = 0.0f;
-                        if (at < rows) {
-                            const int rho = walk.tile * kTtRows + at, t = rho / p.G;
-                            kv_load16<true>(p.q, static_cast<size_t>((static_cast<long long>(begin) + t) * p.q_stride) + (walk.h * p.G + rho - t * p.G) * kKvD + 16 * l, v);
-                        }
-                        kv_rotate16(v, l, p.q_had, p.q_inv_sqrt);
-                        float top = 0.0f;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(v[e]));
-#pragma unroll
-                        for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                        const int field = max(16, min(254, static_cast<int>(__float_as_uint(top) >> 23)));
-                        const float up = __uint_as_float(static_cast<uint32_t>(min(254, 261 - field)) << 23);
-                        if (l == 0) tops[(4 * round + quarter) * 32 + row16] = __uint_as_float(static_cast<uint32_t>(max(1, field - 7)) << 23) * 0x1p24f * p.scale_log2;
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            uint32_t x[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float f = (e & 1) ? 0.0625f * up : up;
-                                const __half2 hh = __floats2half2_rn(v[8 * c + e] * f, v[8 * c + e + 4] * f);
-                                x[e] = *reinterpret_cast<const uint32_t*>(&hh);
-                            }
-                            *reinterpret_cast<uint4*>(here + row16 * 256 + (((2 * l + c) ^ row16) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
-                        }
-                    }
-                    meet();
-                    if ((lane >> 4) == round) {
-                        factor = tops[(4 * round + quarter) * 32 + (lane & 15)];
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            const uint4 x = *reinterpret_cast<const uint4*>(here + (lane & 15) * 256 + (((8 * half + c) ^ (lane & 15)) << 4));
-                            w[4 * c] = x.x, w[4 * c + 1] = x.y, w[4 * c + 2] = x.z, w[4 * c + 3] = x.w;
-                        }
-                    }
-                    meet();
+                for (int c = 0; c < 8; ++c) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(here + lane * 256 + (((8 * turn + c) ^ (lane & 15)) << 4));
+                    w[4 * c] = x.x, w[4 * c + 1] = x.y, w[4 * c + 2] = x.z, w[4 * c + 3] = x.w;
                 }
-                tc_st32(lanes + kTtQ + 32 * half, w);
+                meet();
+                tc_st32(lanes + kTtQ + 32 * turn, w);
                 tc_wait_st();
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full);
 
-            float m = -INFINITY;
-            uint64_t l2 = 0;                                  // two sums of weights
+            float m = -INFINITY;                              // reference point and exponent field of the value scales, as of an item
             int vexp = kTreeVexp;
-            for (int unit = walk.b0; unit < walk.b1; ++unit, ++n) {
-                const bool fresh = unit == walk.b0;           // O holds nothing of this tile yet
-                if (ok) ok = mbar_wait_near(&s_full[n & 1], (n >> 1) & 1, kTreeSite + 1) && mbar_wait_near(&scale_full[n & 3], (n >> 2) & 1, kTreeSite + 2);
+            float l_m = -INFINITY;                            // those that this warp's sum of weights goes by
+            int l_vexp = kTreeVexp;
+            uint64_t l2 = 0;                                  // two sums of weights
+            const uint32_t n0 = n;
+            n += walk.b1 - walk.b0;
+            for (uint32_t i = n0 + ((n0 ^ turn) & 1); i < n; i += 2) {
+                const int unit = walk.b0 + static_cast<int>(i - n0);
+                const uint32_t buf = i % kTtDepth, s_at = lanes + kTtS + buf * kTtUnit;
+                if (ok) ok = mbar_wait_near(&s_full[buf], (i / kTtDepth) & 1, kTreeSite + 1) &&
+                             mbar_wait_near(&scale_full[i % (2 * kTtDepth)], (i / (2 * kTtDepth)) & 1, kTreeSite + 2);
                 tc_fence_after();
-                bool o_waited = n == 0;                       // O of the item before is done, and its P has been read
-                auto wait_o = [&]() {
-                    if (!o_waited && ok) ok = mbar_wait_near(o_done, (n - 1) & 1, kTreeSite + 3);
-                    o_waited = true;
-                    tc_fence_after();
-                };
                 if (active) {
-                    const uint32_t sl = smem_u32(scales + (n & 3) * kTtScaleBytes);
-                    const uint4 vtops = lds128(sl + 2 * kTtUnit * 4), info = lds128(sl + 2 * kTtUnit * 4 + 16);
-                    const uint32_t vt = max(max(vtops.x, vtops.y), max(vtops.z, vtops.w));
-                    const bool plain = (unit + 1) * kTtUnit <= min(q.first, q.len) && (info.x & info.y & info.z & info.w);
-                    auto weigh = [&](auto plain_tag) {        // 64 tokens: scores -> weights
+                    const uint32_t sl = smem_u32(scales + (i % (2 * kTtDepth)) * kTtScaleBytes);
+                    const uint4 info = lds128(sl + 2 * kTtUnit * 4);   // largest value scale of the two blocks, whether they are there
+                    const int vtop = static_cast<int>(max(info.x, info.y) >> 23);
+                    const bool plain = (unit + 1) * kTtUnit <= min(q.first, q.len) && (info.z & info.w);
+                    auto weigh = [&](auto plain_tag) {        // scores -> weights
                         constexpr bool kPlain = decltype(plain_tag)::value;
-                        uint32_t x[2][32];                    // scores, then weights, of tokens 32 i + 0 .. 31
-                        tc_ld32(lanes + kTtS + (n & 1) * 128 + 64 * half, x[0]);
-                        tc_ld32(lanes + kTtS + (n & 1) * 128 + 64 * half + 32, x[1]);
+                        uint32_t x[2][32], seen[2];           // of tokens 32 b + 0 .. 31
+                        tc_ld32(s_at, x[0]);
+                        tc_ld32(s_at + 32, x[1]);
+                        if (!kPlain) {
+                            seen[0] = have && info.z ? tree_seen(p, begin + token, token, 2 * unit, q.first, q.len) : 0u;
+                            seen[1] = have && info.w ? tree_seen(p, begin + token, token, 2 * unit + 1, q.first, q.len) : 0u;
+                        }
                         tc_wait_ld();
-                        tc_fence_before();
+                        // ---- the largest score
+                        float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) {
+                                const uint4 k4 = lds128(sl + 128 * b + 16 * c);
+                                mul2(x[b][4 * c], x[b][4 * c + 1], k4.x, k4.y), mul2(x[b][4 * c + 2], x[b][4 * c + 3], k4.z, k4.w);
+                            }
+                            if (!kPlain) {
+#pragma unroll
+                                for (int c = 0; c < 32; ++c)
+                                    if (!(seen[b] >> c & 1)) x[b][c] = 0xff800000u;   // -inf
+                            }
+#pragma unroll
+                            for (int c = 0; c < 32; c += 2)
+                                best[(c >> 1) & 3] = fmaxf(best[(c >> 1) & 3], fmaxf(__uint_as_float(x[b][c]), __uint_as_float(x[b][c + 1])));
+                        }
+                        const float top = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])) * factor;
+                        // ---- the row's reference point: the one of the item before, raised if need be
+                        float m_old = -INFINITY;
+                        int vexp_old = kTreeVexp;
+                        if (i != n0) {
+                            if (ok) ok = mbar_wait_near(&mark_full[((i - 1) & 1) * 4 + quarter], ((i - 1) >> 1) & 1, kTreeSite + 12);
+                            const float2 told = marks[((i - 1) & 1) * 128 + row];
+                            m_old = told.x, vexp_old = __float_as_int(told.y);
+                        }
+                        m = top > m_old + kTreeSlack ? ceilf(top) : m_old;   // whole binary orders
+                        vexp = max(vexp_old, vtop);
+                        marks[(i & 1) * 128 + row] = make_float2(m, __int_as_float(vexp));
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&s_free[n & 1]);   // S may be written again
-                        uint32_t seen[2];
-                        if (!kPlain) {
-                            const uint32_t i0 = half ? info.z : info.x, i1 = half ? info.w : info.y;
-                            seen[0] = have && i0 ? tree_seen(p, begin + token, token, 4 * unit + 2 * half, q.first, q.len) : 0u;
-                            seen[1] = have && i1 ? tree_seen(p, begin + token, token, 4 * unit + 2 * half + 1, q.first, q.len) : 0u;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const uint4 k4 = lds128(sl + 256 * half + 16 * i);
-                            uint32_t* y = &x[i >> 3][4 * (i & 7)];
-                            mul2(y[0], y[1], k4.x, k4.y), mul2(y[2], y[3], k4.z, k4.w);
-                        }
-                        if (!kPlain) {
-#pragma unroll
-                            for (int i = 0; i < 64; ++i)
-                                if (!(seen[i >> 5] >> (i & 31) & 1)) x[i >> 5][i & 31] = 0xff800000u;   // -inf
-                        }
-                        float best[4];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) best[c] = __uint_as_float(x[0][c]);
-#pragma unroll
-                        for (int i = 4; i < 64; i += 2)
-                            best[(i >> 1) & 3] = fmaxf(best[(i >> 1) & 3], fmaxf(__uint_as_float(x[i >> 5][i & 31]), __uint_as_float(x[i >> 5][(i & 31) + 1])));
-                        float top = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])) * factor;
-                        // the row's reference point, the same in both warps
-                        float* told = tops + (n & 1) * 256;
-                        told[warp * 32 + lane] = top;
-                        meet();
-                        top = fmaxf(top, told[(warp ^ 4) * 32 + lane]);
-                        const bool vgrew = static_cast<int>(vt >> 23) > vexp;   // the same for all rows
-                        if (vgrew || __any_sync(0xffffffffu, top > m + kTreeSlack)) {
-                            const float to = top > m + kTreeSlack ? ceilf(top) : m;
-                            float corr = to > m ? ex2(m - to) : 1.0f;
-                            m = to;
-                            if (vgrew) {
-                                const int v = static_cast<int>(vt >> 23);
-                                corr *= __uint_as_float(static_cast<uint32_t>(max(1, 127 + vexp - v)) << 23);
-                                vexp = v;
-                            }
-                            l2 = both(0.0f) | __float_as_uint(sum2(l2) * corr);
-                            if (!fresh) {
-                                wait_o();
+                        if (lane == 0) mbar_arrive(&mark_full[(i & 1) * 4 + quarter]);
+                        if (i != n0 && __any_sync(0xffffffffu, m != m_old || vexp != vexp_old)) {
+                            // O of the item before times what the references differ by, row by row
+                            const float corr = (m != m_old ? ex2(m_old - m) : 1.0f) * __uint_as_float(static_cast<uint32_t>(max(1, 127 + vexp_old - vexp)) << 23);
+                            if (ok) ok = mbar_wait_near(&o_done[(i - 1) % kTtDepth], ((i - 1) / kTtDepth) & 1, kTreeSite + 3);
+                            tc_fence_after();
 #pragma unroll 1
-                                for (int c = 0; c < 4; ++c) {   // O times corr, row by row; half of the columns per warp
-                                    uint32_t x[16];
-                                    tc_ld16(lanes + kTtO + 64 * half + 16 * c, x);
-                                    tc_wait_ld();
+                            for (int c = 0; c < 8; ++c) {
+                                uint32_t y[16];
+                                tc_ld16(lanes + kTtO + 16 * c, y);
+                                tc_wait_ld();
 #pragma unroll
-                                    for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * corr);
-                                    tc_st16(lanes + kTtO + 64 * half + 16 * c, x);
-                                }
-                                tc_wait_st();
+                                for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * corr);
+                                tc_st16(lanes + kTtO + 16 * c, y);
                             }
+                            tc_wait_st();
                         }
+                        if (__any_sync(0xffffffffu, m != l_m || vexp != l_vexp)) {
+                            const float corr = l_m > -INFINITY ? ex2(l_m - m) * __uint_as_float(static_cast<uint32_t>(max(1, 127 + l_vexp - vexp)) << 23) : 0.0f;
+                            l2 = __float_as_uint(sum2(l2) * corr);
+                            l_m = m, l_vexp = vexp;
+                        }
+                        // ---- weights
                         const uint64_t f2 = both(factor);
                         const uint64_t r2 = both(static_cast<float>(134 - vexp) - m);   // weights and their sum carry 2^8 / 2^(vexp - 126)
                         uint64_t l3 = 0;
@@ -327,11 +329,11 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                         for (int b = 0; b < 2; ++b) {
                             uint32_t out[16];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const uint4 v4 = lds128(sl + kTtUnit * 4 + 256 * half + 128 * b + 16 * i);
+                            for (int c = 0; c < 8; ++c) {
+                                const uint4 v4 = lds128(sl + kTtUnit * 4 + 128 * b + 16 * c);
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
-                                    const int j = 2 * i + e;   // tokens 2 j, 2 j + 1 of the 32
+                                    const int j = 2 * c + e;   // tokens 2 j, 2 j + 1 of the 32
                                     uint32_t &y0 = x[b][2 * j], &y1 = x[b][2 * j + 1];
                                     fma2(y0, y1, f2, r2);
                                     y0 = __float_as_uint(ex2(__uint_as_float(y0))), y1 = __float_as_uint(ex2(__uint_as_float(y1)));
@@ -350,67 +352,73 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                                     out[(j & 3) * 4 + (j >> 2)] = *reinterpret_cast<const uint32_t*>(&hw);
                                 }
                             }
-                            if (b == 0) wait_o();
-                            tc_st16(lanes + kTtP + 32 * half + 16 * b, out);
+                            // the weights take the place of scores that have been read
+                            tc_st16(s_at + 16 * b, out);
                         }
                         add2(l2, static_cast<uint32_t>(l3), static_cast<uint32_t>(l3 >> 32));
                         tc_wait_st();
                     };
                     if (plain) weigh(std::true_type{});
                     else weigh(std::false_type{});
-                } else {
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&s_free[n & 1]);
-                    wait_o();
+                } else if (lane == 0) {
+                    mbar_arrive(&mark_full[(i & 1) * 4 + quarter]);   // keeps the barrier in step with the items
                 }
                 tc_fence_before();
                 ok = __all_sync(0xffffffffu, ok);
-                if (lane == 0) mbar_arrive(p_full);
+                if (lane == 0) mbar_arrive(&p_full[buf]);
             }
             // ---- the tile, or this run's piece of it: half of the columns per warp
-            if (ok) ok = mbar_wait_near(o_done, (n - 1) & 1, kTreeSite + 3);
+            if (ok) ok = mbar_wait_near(&o_done[(n - 1) % kTtDepth], ((n - 1) / kTtDepth) & 1, kTreeSite + 3);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
             if (active) {
                 const bool whole = walk.whole();
+                // the last item's reference point, and this warp's sum brought to it
+                if (ok) ok = mbar_wait_near(&mark_full[((n - 1) & 1) * 4 + quarter], ((n - 1) >> 1) & 1, kTreeSite + 12);
+                const float2 told = marks[((n - 1) & 1) * 128 + row];
+                m = told.x, vexp = __float_as_int(told.y);
                 const float c1 = __uint_as_float(static_cast<uint32_t>(vexp) << 23);
-                float l = (sum2(l2) * 0x1p-7f) * c1;
-                float* told = tops + (n & 1) * 256;
-                told[warp * 32 + lane] = l;
+                float l = l_m > -INFINITY ? sum2(l2) * ex2(l_m - m) * __uint_as_float(static_cast<uint32_t>(max(1, 127 + l_vexp - vexp)) << 23) : 0.0f;
+                l = (l * 0x1p-7f) * c1;
+                meet();              // the reference points have been read by both
+                marks[turn * 128 + row].x = l;
                 meet();
-                l += told[(warp ^ 4) * 32 + lane];
+                l += marks[(turn ^ 1) * 128 + row].x;
                 const float inv = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
-                float* piece = p.partial + (static_cast<size_t>(2 * blockIdx.x + (walk.u == walk.u0 ? 0 : 1)) * kTtRows + row) * kTreeRow;
-                const size_t out_at = (static_cast<size_t>(begin + token) * p.Hq + hq) * kKvD;
+                float* piece = p.partial + (static_cast<size_t>(2 * blockIdx.x + (walk.u == walk.u0 ? 0 : 1)) * kTtRows + quarter * 32) * kTreeRow;
+                float4* own = reinterpret_cast<float4*>(stage + quarter * 8192 + turn * 4096);   // the quarter's own, as for the query
 #pragma unroll 1
-                for (int part = 2 * half; part < 2 * half + 2; ++part) {
+                for (int part = 2 * turn; part < 2 * turn + 2; ++part) {
                     uint32_t a[32];
-                    float y[32];
                     tc_ld32(lanes + kTtO + 32 * part, a);
                     tc_wait_ld();
+                    // column 32 w + 8 j + g is dimension 32 w + 4 g + j; odd ones carry 16.  32 rows of 32 dimensions go through shared
+                    // memory, so that eight lanes write 128 bytes of a row together
+                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)   // column 32 w + 8 j + g is dimension 32 w + 4 g + j; odd ones carry 16
-                        y[4 * (i & 7) + (i >> 3)] = (__uint_as_float(a[i]) * (((i >> 3) & 1) ? 0x1p13f : 0x1p17f)) * c1 * inv;
-                    if (!ok || !have) continue;
-                    if (whole) {
-                        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + out_at + 32 * part);
+                    for (int g = 0; g < 8; ++g) {
+                        float y[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t bits[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const __nv_bfloat162 t = __floats2bfloat162_rn(y[8 * i + 2 * e], y[8 * i + 2 * e + 1]);
-                                bits[e] = *reinterpret_cast<const uint32_t*>(&t);
-                            }
-                            dst[i] = make_uint4(bits[0], bits[1], bits[2], bits[3]);
+                        for (int j = 0; j < 4; ++j) y[j] = (__uint_as_float(a[8 * j + g]) * ((j & 1) ? 0x1p13f : 0x1p17f)) * c1 * inv;
+                        own[lane * 8 + (g ^ (lane & 7))] = make_float4(y[0], y[1], y[2], y[3]);
+                    }
+                    __syncwarp();
+#pragma unroll 1
+                    for (int i = 0; i < 8; ++i) {
+                        const int r32 = 4 * i + (lane >> 3), c = lane & 7, at = quarter * 32 + r32;
+                        const float4 y = own[r32 * 8 + (c ^ (r32 & 7))];
+                        if (!ok || at >= rows) continue;
+                        if (whole) {
+                            const int rho = walk.tile * kTtRows + at, t = rho / p.G;
+                            const __nv_bfloat162 u0 = __floats2bfloat162_rn(y.x, y.y), u1 = __floats2bfloat162_rn(y.z, y.w);
+                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + (static_cast<size_t>(begin + t) * p.Hq + walk.h * p.G + rho - t * p.G) * kKvD + 32 * part + 4 * c) =
+                                make_uint2(*reinterpret_cast<const uint32_t*>(&u0), *reinterpret_cast<const uint32_t*>(&u1));
+                        } else {
+                            *reinterpret_cast<float4*>(piece + r32 * kTreeRow + 32 * part + 4 * c) = y;
                         }
-                    } else {
-                        float4* dst = reinterpret_cast<float4*>(piece + 32 * part);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) dst[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
                     }
                 }
-                if (ok && have && half == 0 && !whole) *reinterpret_cast<float2*>(piece + kKvD) = make_float2(m, l);
+                if (ok && have && turn == 0 && !whole) *reinterpret_cast<float2*>(piece + lane * kTreeRow + kKvD) = make_float2(m, l);
                 meet();              // the sums have been read before the next tile's factors come
             }
             tc_fence_before();       // O has been read: the next tile's products may write
@@ -418,80 +426,54 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
         }
         if (tid == 0) p.desc[blockIdx.x] = ok ? mine : make_int4(0, 0, 0, 0);
     } else if (warp < 8 + kTtConvert) {
-        // ------------------------------------------------------------------ conversion: every seventh block
-        const int k = warp - 8;
+        // ------------------------------------------------------------------ conversion: every fifth task
         const int cq = lane >> 3, g = lane & 7;
-        const int page_blocks = p.pages.page_tokens / kPgTokens;
-        uint8_t* my_raw = raw + k * kTtRing * kPgBlock;
-        TtItems ahead, now;
-        now.start(p);
-        ahead = now;
-        uint32_t want = k, block = k;                         // numbers of the next block to ask for and to convert
-        uint32_t there = 0;                                   // which ring slots got one
-        int slot_in = 0, slot = 0, page = -1;
-        auto look_up = [&]() {                                // the page of block `want`: used when it is asked for, later
-            ahead.to(p, want >> 2);
-            page = -1;
-            if (!ahead.valid) return;
-            const int b = 4 * ahead.unit + (want & 3);
-            if (b * kPgTokens < ahead.w.q.len) page = p.pages.table[static_cast<size_t>(ahead.w.r) * p.pages.max_pages + b / page_blocks];
-        };
-        auto ask = [&]() {
-            const int b = 4 * ahead.unit + (want & 3);
-            const bool have = ahead.valid && static_cast<unsigned>(page) < static_cast<unsigned>(p.pages.num_pages);
-            there = have ? there | (1u << slot_in) : there & ~(1u << slot_in);
-            if (have && lane == 0) {
-                uint64_t* bar = &raw_full[k * kTtRing + slot_in];
-                mbar_expect_tx(bar, kPgBlock);
-                bulk_g2s(my_raw + slot_in * kPgBlock, p.pages.pool + ((static_cast<size_t>(page) * p.pages.H + ahead.w.h) * page_blocks + b % page_blocks) * kPgBlock,
-                         kPgBlock, bar);
+        const uint32_t piece = static_cast<uint32_t>(cq * 8 + (g ^ (2 * cq))) * 16;
+        const uint32_t raw_at = smem_u32(raw), k_at = smem_u32(k_tiles) + (cq >> 1) * 8192 + g * 128, v_at = smem_u32(v_tiles) + g * 128;
+        TreeWalk<kTtRows, kTtUnit> walk;
+        walk.start(p, blockIdx.x, gridDim.x);
+        const uint32_t items = static_cast<uint32_t>(walk.u1 - walk.u0);   // (an item's number fits: 2^32 of them take days)
+        // pairs of tasks: keys of items 0 .. 2, then values of item i and keys of item i + 3 in turn
+        for (uint32_t task = warp - 8; task < 2 * (2 * items + kTtTiles - 1); task += kTtConvert) {
+            const uint32_t pair = task >> 1, blk = task & 1;
+            const bool values = pair >= kTtTiles && !((pair - kTtTiles) & 1);
+            const uint32_t item = pair < kTtTiles ? pair : values ? (pair - kTtTiles) >> 1 : ((pair - kTtTiles) >> 1) + kTtTiles;
+            if (item >= items) continue;
+            const uint32_t buf = item % kTtTiles;
+            const uint32_t block = 2 * item + blk, slot = block % kTtRing;
+            const uint8_t* src = raw + slot * kPgBlock;
+            const uint32_t base = raw_at + slot * kPgBlock + piece;
+            if (!mbar_wait_near(&raw_full[slot], (block / kTtRing) & 1, kTreeSite + 4)) break;
+            // The item that had the tile before is done with it.  Tasks are waited for out of step -- this warp may come here while the
+            // products of earlier items are under way -- and a parity cannot tell a phase from the second next: with two barriers
+            // per tile, the phase before is the one of item - 9, over when this warp's last task began
+            if (item >= kTtTiles) {
+                const uint32_t before = item - kTtTiles;
+                uint64_t* bar = (values ? v_free : k_free) + before % (2 * kTtTiles);
+                if (!mbar_wait_near(bar, before / (2 * kTtTiles) & 1, kTreeSite + 5)) break;
             }
-            slot_in ^= 1, want += kTtConvert;
-            look_up();
-        };
-        static_assert(kTtRing == 2, "slots alternate");
-        look_up();
-        ask(), ask();
-        uint32_t phases = 0;
-        bool ok = true;
-        for (now.to(p, block >> 2); now.valid; block += kTtConvert, now.to(p, block >> 2), slot ^= 1) {
-            const int buf = now.n & 1, blk = block & 3;
-            const uint32_t use = now.n >> 1;                  // how often this pair of tiles has been used before
-            const bool have = there >> slot & 1;
-            const uint8_t* src = my_raw + slot * kPgBlock;
-            const uint32_t base = smem_u32(src);
-            if (have) {
-                if (!mbar_wait_near(&raw_full[k * kTtRing + slot], phases >> slot & 1, kTreeSite + 4)) {
-                    ok = false;
-                    break;
-                }
-                phases ^= 1u << slot;
-                there &= ~(1u << slot);
-            }
-            if (use > 0 && !mbar_wait_near(&k_free[buf], (use - 1) & 1, kTreeSite + 5)) {
-                ok = false;
-                break;
-            }
-            // ---- keys: row = token, 16-byte chunk = eight dimensions
-            const uint32_t ktile = smem_u32(k_tiles + buf * 32768) + (cq >> 1) * 16384 + blk * 4096 + g * 128;
-            if (have) {
+            const int tokens = raw_tokens[slot];
+            const bool have = tokens > 0;
+            if (!values) {
+                // ---- row = token, 16-byte chunk = eight dimensions
+                const uint32_t ktile = k_at + buf * kTtTile + blk * 4096;
+                if (have) {
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const uint4 x4 = lds128(base + (n * 32 + cq * 8 + (g ^ (2 * cq))) * 16);
-                    const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
-                    const uint32_t z = src[kPgKz + 8 * n + g] * 0x00010001u;
-                    const uint32_t z1 = z ^ 0x80008000u, z16 = (z << 4) ^ 0x80008000u;   // minus the zero-point, and 16 times it
+                    for (int n = 0; n < 4; ++n) {
+                        const uint4 x4 = lds128(base + n * 512);
+                        const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+                        const uint32_t z = src[kPgKz + 8 * n + g] * 0x00010001u;
+                        const uint32_t z1 = z ^ 0x80008000u, z16 = (z << 4) ^ 0x80008000u;   // minus the zero-point, and 16 times it
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t y = x[i] >> 8;
-                        sts128(ktile + n * 1024 + ((((cq & 1) * 4 + i) ^ g) << 4), lessened(x[i] & 0x000f000fu, z1), lessened(x[i] & 0x00f000f0u, z16),
-                               lessened(y & 0x000f000fu, z1), lessened(y & 0x00f000f0u, z16));
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t y = x[i] >> 8;
+                            sts128(ktile + n * 1024 + ((((cq & 1) * 4 + i) ^ g) << 4), lessened(x[i] & 0x000f000fu, z1), lessened(x[i] & 0x00f000f0u, z16),
+                                   lessened(y & 0x000f000fu, z1), lessened(y & 0x00f000f0u, z16));
+                        }
                     }
                 }
-            }
-            {
-                uint8_t* sl = scales + (now.n & 3) * kTtScaleBytes;
-                const bool in = have && (4 * now.unit + blk) * kPgTokens + lane < now.w.q.len;
+                uint8_t* sl = scales + (item % (2 * kTtDepth)) * kTtScaleBytes;
+                const bool in = lane < tokens;
                 const float ksc = in ? reinterpret_cast<const float*>(src + kPgKs)[lane] : 0.0f;
                 const float vsc = in ? reinterpret_cast<const float*>(src + kPgVs)[lane] : 0.0f;
                 reinterpret_cast<float*>(sl)[32 * blk + lane] = ksc;
@@ -499,95 +481,137 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                 const uint32_t bits = __float_as_uint(vsc);
                 const uint32_t top = __reduce_max_sync(0xffffffffu, bits < 0x7f800000u ? bits : 0u);
                 uint32_t* info = reinterpret_cast<uint32_t*>(sl + 2 * kTtUnit * 4);
-                if (lane == 0) info[blk] = top, info[4 + blk] = have;
-            }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&k_full[buf]), mbar_arrive(&scale_full[now.n & 3]);
-            // ---- values: row = dimension, 16-byte chunk = eight tokens
-            if (use > 0 && !mbar_wait_near(&v_free[buf], (use - 1) & 1, kTreeSite + 6)) {
-                ok = false;
-                break;
-            }
-            const uint32_t vtile = smem_u32(v_tiles + buf * 32768) + (blk >> 1) * 16384 + g * 128 + ((((blk & 1) * 4 + cq) ^ g) << 4);
-            if (have) {
-                uint32_t z1[4], z16[4];
+                if (lane == 0) info[blk] = top, info[2 + blk] = have;
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&k_full[buf]), mbar_arrive(&scale_full[item % (2 * kTtDepth)]), mbar_arrive(&raw_free[slot]);
+            } else {
+                // ---- row = dimension, 16-byte chunk = eight tokens
+                const uint32_t vtile = v_at + buf * kTtTile + (((blk * 4 + cq) ^ g) << 4);
+                if (have) {
+                    uint32_t z1[4], z16[4];
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const uint32_t z = __byte_perm(*reinterpret_cast<const uint16_t*>(src + kPgVz + 8 * n + 2 * cq), 0u, 0x4140u);
-                    z1[n] = z ^ 0x80008000u, z16[n] = (z << 4) ^ 0x80008000u;
+                    for (int n = 0; n < 4; ++n) {
+                        const uint32_t z = __byte_perm(*reinterpret_cast<const uint16_t*>(src + kPgVz + 8 * n + 2 * cq), 0u, 0x4140u);
+                        z1[n] = z ^ 0x80008000u, z16[n] = (z << 4) ^ 0x80008000u;
+                    }
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint4 x4 = lds128(base + kPgV + w * 512);
+                        const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+                        const uint32_t y[4] = {x4.x >> 8, x4.y >> 8, x4.z >> 8, x4.w >> 8};
+                        sts128(vtile + (w * 4) * 1024, lessened(x[0] & 0x000f000fu, z1[0]), lessened(x[1] & 0x000f000fu, z1[1]),
+                               lessened(x[2] & 0x000f000fu, z1[2]), lessened(x[3] & 0x000f000fu, z1[3]));
+                        sts128(vtile + (w * 4 + 1) * 1024, lessened(x[0] & 0x00f000f0u, z16[0]), lessened(x[1] & 0x00f000f0u, z16[1]),
+                               lessened(x[2] & 0x00f000f0u, z16[2]), lessened(x[3] & 0x00f000f0u, z16[3]));
+                        sts128(vtile + (w * 4 + 2) * 1024, lessened(y[0] & 0x000f000fu, z1[0]), lessened(y[1] & 0x000f000fu, z1[1]),
+                               lessened(y[2] & 0x000f000fu, z1[2]), lessened(y[3] & 0x000f000fu, z1[3]));
+                        sts128(vtile + (w * 4 + 3) * 1024, lessened(y[0] & 0x00f000f0u, z16[0]), lessened(y[1] & 0x00f000f0u, z16[1]),
+                               lessened(y[2] & 0x00f000f0u, z16[2]), lessened(y[3] & 0x00f000f0u, z16[3]));
+                    }
+                } else {   // no such block: its weights are zero, and zero times what was left there must be zero
+#pragma unroll 1
+                    for (int w = 0; w < 16; ++w) sts128(vtile + w * 1024, 0u, 0u, 0u, 0u);
                 }
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint4 x4 = lds128(base + kPgV + (w * 32 + cq * 8 + (g ^ (2 * cq))) * 16);
-                    const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
-                    const uint32_t y[4] = {x4.x >> 8, x4.y >> 8, x4.z >> 8, x4.w >> 8};
-                    sts128(vtile + (w * 4) * 1024, lessened(x[0] & 0x000f000fu, z1[0]), lessened(x[1] & 0x000f000fu, z1[1]),
-                           lessened(x[2] & 0x000f000fu, z1[2]), lessened(x[3] & 0x000f000fu, z1[3]));
-                    sts128(vtile + (w * 4 + 1) * 1024, lessened(x[0] & 0x00f000f0u, z16[0]), lessened(x[1] & 0x00f000f0u, z16[1]),
-                           lessened(x[2] & 0x00f000f0u, z16[2]), lessened(x[3] & 0x00f000f0u, z16[3]));
-                    sts128(vtile + (w * 4 + 2) * 1024, lessened(y[0] & 0x000f000fu, z1[0]), lessened(y[1] & 0x000f000fu, z1[1]),
-                           lessened(y[2] & 0x000f000fu, z1[2]), lessened(y[3] & 0x000f000fu, z1[3]));
-                    sts128(vtile + (w * 4 + 3) * 1024, lessened(y[0] & 0x00f000f0u, z16[0]), lessened(y[1] & 0x00f000f0u, z16[1]),
-                           lessened(y[2] & 0x00f000f0u, z16[2]), lessened(y[3] & 0x00f000f0u, z16[3]));
-                }
-            } else {   // no such block: its weights are zero, and zero times what was left there must be zero
-#pragma unroll
-                for (int w = 0; w < 16; ++w) sts128(vtile + w * 1024, 0u, 0u, 0u, 0u);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[item % kTtDepth]), mbar_arrive(&raw_free[slot]);
             }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&v_full[buf]);
-            ask();
+        }
+    } else if (warp == 13) {
+        // ------------------------------------------------------------------ fetch: lane i looks up block 32 j + i
+        TtItems items;
+        items.start(p);
+        const int page_blocks = p.pages.page_tokens / kPgTokens;
+        const uint32_t blocks = 2 * static_cast<uint32_t>(items.w.u1 - items.w.u0);
+        uint32_t slot = 0, round = 0;
+        bool ok = true;
+        for (uint32_t base = 0; base < blocks && ok; base += 32) {
+            const uint8_t* src = nullptr;
+            int tokens = 0;
+            items.to(p, (base + lane) >> 1);
+            if (items.valid) {
+                const int b = 2 * items.unit + (lane & 1);
+                tokens = items.w.q.len - b * kPgTokens;
+                if (tokens > 0) {
+                    const int at = b / page_blocks;
+                    const int page = p.pages.table[static_cast<size_t>(items.w.r) * p.pages.max_pages + at];
+                    if (static_cast<unsigned>(page) < static_cast<unsigned>(p.pages.num_pages))
+                        src = p.pages.pool + ((static_cast<size_t>(page) * p.pages.H + items.w.h) * page_blocks + (b - at * page_blocks)) * kPgBlock;
+                }
+            }
+            for (uint32_t i = 0; i < 32 && base + i < blocks; ++i) {
+                if (round > 0) ok = __all_sync(0xffffffffu, mbar_wait_near(&raw_free[slot], (round - 1) & 1, kTreeSite + 8));
+                if (!ok) break;
+                if (lane == static_cast<int>(i)) {
+                    raw_tokens[slot] = src ? tokens : 0;
+                    if (src) {
+                        mbar_expect_tx(&raw_full[slot], kPgBlock);
+                        bulk_g2s(raw + slot * kPgBlock, src, kPgBlock, &raw_full[slot]);
+                    } else {
+                        mbar_arrive(&raw_full[slot]);
+                    }
+                }
+                __syncwarp();
+                if (++slot == kTtRing) slot = 0, ++round;
+            }
         }
         if (!ok)   // copies in flight end (or are given up) before the shared memory does
-            for (int s = 0; s < kTtRing; ++s)
-                if (there >> s & 1) mbar_wait(&raw_full[k * kTtRing + s], phases >> s & 1, kTreeSite + 4);
-    } else {
-        // ------------------------------------------------------------------ products
+            for (uint32_t i = 0; i < kTtRing; ++i)
+                if (i < slot || round > 0) mbar_wait(&raw_full[i], (i < slot ? round : round - 1) & 1, kTreeSite + 4, 1000000ull);
+    } else if (warp == 14) {
+        // ------------------------------------------------------------------ O
+        // the whole warp follows the loop, so that descriptors stay in uniform registers; one elected lane issues
         TreeWalk<kTtRows, kTtUnit> walk;
         walk.start(p, blockIdx.x, gridDim.x);
-        if (lane == 0) {
-            const uint64_t kdesc = make_kmajor_sw128_desc(smem_u32(k_tiles)), vdesc = make_kmajor_sw128_desc(smem_u32(v_tiles));
-            uint32_t n = 0, tiles = 0;
-            bool ok = true;
-            auto scores = [&](uint32_t i) {                   // S of item i
-                const uint32_t buf = i & 1, use = i >> 1;
-                if (!mbar_wait_near(&k_full[buf], use & 1, kTreeSite + 7)) return false;
-                if (use > 0 && !mbar_wait_near(&s_free[buf], (use - 1) & 1, kTreeSite + 8)) return false;
+        const uint64_t vdesc = make_kmajor_sw128_desc(smem_u32(v_tiles));
+        uint32_t n = 0;
+        bool ok = true;
+        for (; ok && walk.tile_here(p); walk.next()) {
+            const uint32_t n0 = n;
+            for (const uint32_t end = n + (walk.b1 - walk.b0); n < end; ++n) {
+                const uint32_t buf = n % kTtDepth, tile = n % kTtTiles;
+                ok = __all_sync(0xffffffffu, mbar_wait_near(&p_full[buf], (n / kTtDepth) & 1, kTreeSite + 11));
+                if (!ok) break;
                 tc_fence_after();
+                const uint32_t a = tmem + kTtS + buf * kTtUnit, more = n != n0;
+                const uint64_t b = vdesc + tile * (kTtTile >> 4);
+                if (elect_one()) {
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    tc_mma_f16_ts(tmem + kTtS + buf * 128, tmem + kTtQ + 8 * ks, kdesc + buf * (32768 >> 4) + (ks >> 2) * (16384 >> 4) + 2 * (ks & 3), IDESC, ks != 0);
-                tc_commit(&k_free[buf]);
-                tc_commit(&s_full[buf]);
-                return true;
-            };
-            for (; ok && walk.tile_here(p); walk.next(), ++tiles) {
-                if (!mbar_wait_near(q_full, tiles & 1, kTreeSite + 9)) break;
-                tc_fence_after();
-                if (!scores(n)) break;
-                for (int unit = walk.b0; unit < walk.b1; ++unit, ++n) {
-                    const uint32_t buf = n & 1, use = n >> 1;
-                    if (unit + 1 < walk.b1 && !scores(n + 1)) {
-                        ok = false;
-                        break;
-                    }
-                    if (!mbar_wait_near(p_full, n & 1, kTreeSite + 10) || !mbar_wait_near(&v_full[buf], use & 1, kTreeSite + 11)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)
-                        tc_mma_f16_ts(tmem + kTtO, tmem + kTtP + 8 * ks, vdesc + buf * (32768 >> 4) + (ks >> 2) * (16384 >> 4) + 2 * (ks & 3), IDESC,
-                                      (unit != walk.b0 || ks != 0) ? 1u : 0u);
-                    tc_commit(&v_free[buf]);
-                    tc_commit(o_done);
+                    for (int ks = 0; ks < 4; ++ks) tc_mma_f16_ts(tmem + kTtO, a + 8 * ks, b + 2 * ks, O_IDESC, ks != 0 ? 1u : more);
+                    tc_commit(&v_free[n % (2 * kTtTiles)]);
+                    tc_commit(&o_done[buf]);
                 }
+                __syncwarp();
             }
         }
-        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ S
+        TreeWalk<kTtRows, kTtUnit> walk;
+        walk.start(p, blockIdx.x, gridDim.x);
+        const uint64_t kdesc = make_kmajor_sw128_desc(smem_u32(k_tiles));
+        uint32_t n = 0, tiles = 0;
+        bool ok = true;
+        for (; ok && walk.tile_here(p); walk.next(), ++tiles) {
+            ok = __all_sync(0xffffffffu, mbar_wait_near(q_full, tiles & 1, kTreeSite + 9));
+            for (const uint32_t end = n + (walk.b1 - walk.b0); n < end && ok; ++n) {
+                const uint32_t buf = n % kTtDepth, use = n / kTtDepth, tile = n % kTtTiles;
+                // the place is free when the weights of item n - 4 have been used
+                ok = mbar_wait_near(&k_full[tile], (n / kTtTiles) & 1, kTreeSite + 7) && (use == 0 || mbar_wait_near(&o_done[buf], (use - 1) & 1, kTreeSite + 10));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t d = tmem + kTtS + buf * kTtUnit;
+                const uint64_t b = kdesc + tile * (kTtTile >> 4);
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) tc_mma_f16_ts(d, tmem + kTtQ + 8 * ks, b + (ks >> 2) * (8192 >> 4) + 2 * (ks & 3), S_IDESC, ks != 0);
+                    tc_commit(&k_free[n % (2 * kTtTiles)]);
+                    tc_commit(&s_full[buf]);
+                }
+                __syncwarp();
+            }
+        }
     }
     tc_fence_before();
     __syncthreads();

@@ -1731,7 +1731,7 @@ int run_move(Kernel f32, Kernel bf16, int x_dtype, const KvMoveParams& p, cudaSt
 // of kv4_tree_tc.cuh (bf16 calls).
 inline int tree_rows(int total, int R, int G, bool bf16) {
     const long long mean = (static_cast<long long>(total) * G + R - 1) / R;
-    return mean <= 8 || !bf16 ? 8 : mean <= 16 ? 16 : kTtRows;
+    return mean <= 8 || !bf16 ? 8 : mean <= 40 ? 16 : kTtRows;
 }
 // runs that the items are dealt to: warps of the one kernel, CTAs of the other
 inline int tree_runs(int rows) { return sm_count() * (rows == 8 ? TreeShape<true, 8>::kWarps : rows == 16 ? TreeShape<true, 16>::kWarps : 1); }

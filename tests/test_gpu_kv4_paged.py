@@ -465,3 +465,17 @@ def test_run_twice_is_the_same():
         a = qift.qift_kv4_paged_attention(q, b.pages, b.rs, b.f, q_had_block=128)
         for _ in range(3):
             assert torch.equal(a, qift.qift_kv4_paged_attention(q, b.pages, b.rs, b.f, q_had_block=128))
+
+
+def test_many_replays_of_wide_trees_stay_in_step():
+    """Wide trees over contexts of many blocks, many times in a row: every pass gives the same bits and no wait runs out."""
+    b = filled(370, [64, 64, 40, 7], [5000, 1300, 64, 9000], 4, 64)
+    q = values(371, (b.total, 16, D), "bf16")[0]
+    want = qift.qift_kv4_paged_attention(q, b.pages, b.rs, b.f, q_had_block=128)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        gots = [qift.qift_kv4_paged_attention(q, b.pages, b.rs, b.f, q_had_block=128) for _ in range(8)]
+    for _ in range(25):
+        g.replay()
+        assert all(torch.equal(want, got) for got in gots)
+    ok()

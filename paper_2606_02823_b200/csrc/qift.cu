@@ -1759,6 +1759,42 @@ int run_tree(KvTreeParams p, void* workspace, cudaStream_t st) {
     if (rc != QIFT_OK) return rc;
     return cuda_status(launch_pdl(kv4_tree_join_kernel<BF16, ROWS>, dim3(runs, ROWS / 8), dim3(32 * kTreeJoinWarps), 0, st, p));
 }
+// Adapters.  Slices of K: enough for two CTAs per SM, of 512 k at least (every slice is read again by the second kernel).
+inline int lora_splits(long long items, int K) {
+    long long s = (2ll * sm_count() + items - 1) / items;
+    if (s > (K + 511) / 512) s = (K + 511) / 512;
+    return s > 16 ? 16 : s < 1 ? 1 : static_cast<int>(s);
+}
+template <bool BF16, bool WIDE, int RS>
+int run_lora(LoraParams p, cudaStream_t st) {
+    // a request of n > 0 rows is ceil(n / rows) items
+    const long long rows = WIDE ? 16 * kLoraWarps : 16, most = (static_cast<long long>(p.M) + (rows - 1) * p.R) / rows;
+    const long long items = most < p.M ? most : p.M;
+    const int splits = lora_splits(items, p.K);
+    p.k_slice = ((p.K + splits - 1) / splits + 63) & ~63;
+    p.splits = (p.K + p.k_slice - 1) / p.k_slice;
+    // columns of a CTA: about four CTAs per SM in all
+    long long slices = (4ll * sm_count() + items - 1) / items;
+    const int most_slices = (p.N + 255) / 256;
+    if (slices > most_slices) slices = most_slices;
+    p.n_slice = static_cast<int>(((p.N + slices - 1) / slices + 255) / 256) * 256;
+    const dim3 down(static_cast<unsigned>(items), p.splits), up(static_cast<unsigned>(items), (p.N + p.n_slice - 1) / p.n_slice);
+    cudaError_t e;
+    if constexpr (WIDE) {
+        e = allow_smem(lora_down_wide_kernel<BF16, RS>, LoraDownWide<BF16, RS>::kSmem);
+        if (e == cudaSuccess) e = allow_smem(lora_up_wide_kernel<BF16, RS>, LoraUpWide<BF16, RS>::kSmem);
+        if (e == cudaSuccess) e = launch_pdl(lora_down_wide_kernel<BF16, RS>, down, dim3(kLoraThreads), LoraDownWide<BF16, RS>::kSmem, st, p);
+        if (e == cudaSuccess) e = launch_pdl(lora_up_wide_kernel<BF16, RS>, up, dim3(kLoraThreads), LoraUpWide<BF16, RS>::kSmem, st, p);
+    } else {
+        e = launch_pdl(lora_down_kernel<BF16, RS>, down, dim3(kLoraThreads), 0, st, p);
+        if (e == cudaSuccess) e = launch_pdl(lora_up_kernel<BF16, RS>, up, dim3(kLoraThreads), 0, st, p);
+    }
+    return cuda_status(e);
+}
+template <bool BF16, bool WIDE>
+int run_lora_rank(const LoraParams& p, cudaStream_t st) {
+    return p.rank <= 16 ? run_lora<BF16, WIDE, 1>(p, st) : p.rank <= 64 ? run_lora<BF16, WIDE, 4>(p, st) : run_lora<BF16, WIDE, 8>(p, st);
+}
 }  // namespace
 
 extern "C" {
@@ -1853,7 +1889,8 @@ int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int
 
 size_t qift_lora_workspace_bytes(int M, int rank, int K) {
     if (M <= 0 || rank <= 0 || K <= 0) return 0;
-    return (static_cast<size_t>(M) * rank * sizeof(float) + 15) & ~static_cast<size_t>(15);
+    const int splits = lora_splits((M + 16 * kLoraWarps - 1) / (16 * kLoraWarps), K);   // no call has fewer items than this
+    return (static_cast<size_t>(splits) * M * rank * sizeof(float) + 15) & ~static_cast<size_t>(15);
 }
 
 int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16_t* B, const float* scaling, int adapters, int rank,
@@ -1871,10 +1908,9 @@ int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16
     p.x = X, p.A = A, p.B = B, p.scaling = scaling, p.row_start = row_start, p.adapter = adapter, p.y = y, p.out = out;
     p.t = static_cast<float*>(workspace), p.M = M, p.N = N, p.K = K, p.rank = rank, p.adapters = adapters, p.R = R;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool b = x_dtype == QIFT_BF16;
-    const int rc = cuda_status(launch_pdl(b ? lora_down_kernel<true> : lora_down_kernel<false>, dim3(M), dim3(256), 0, st, p));
-    if (rc != QIFT_OK) return rc;
-    return cuda_status(launch_pdl(b ? lora_up_kernel<true> : lora_up_kernel<false>, dim3(M), dim3(256), 0, st, p));
+    const bool wide = static_cast<long long>(M) > 32ll * R;
+    return x_dtype == QIFT_BF16 ? (wide ? run_lora_rank<true, true>(p, st) : run_lora_rank<true, false>(p, st))
+                                : (wide ? run_lora_rank<false, true>(p, st) : run_lora_rank<false, false>(p, st));
 }
 
 }  // extern "C"

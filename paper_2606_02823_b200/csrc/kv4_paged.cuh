@@ -92,34 +92,73 @@ __device__ __forceinline__ int kv_find_request(int item, int R, int& inner, Item
     return found[0];
 }
 
+// Two fp32 operations in one instruction, each rounded on its own: a pair of values in a 64-bit register.
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x), "f"(y));
+    return p;
+}
+__device__ __forceinline__ void pair_to(uint64_t p, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p)); }
+__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+
 // In-place butterfly over the 128 values of a vector in eight lanes (value index 16 * l + e), strides below had_block; natural
-// order, the same operands as everywhere else in this library.  had_block may differ between the groups of a warp.
+// order, the same operands as everywhere else in this library.  had_block may differ between the groups of a warp.  A difference is
+// taken as -1 * b + a in one rounding.
 __device__ __forceinline__ void kv_rotate16(float (&v)[16], int l, int had_block, float inv_sqrt_b) {
     if (!__any_sync(0xffffffffu, had_block > 1)) return;
+    if (1 < had_block) {
 #pragma unroll
-    for (int h = 1; h < 16; h <<= 1) {
-        if (h < had_block) {
+        for (int e = 0; e < 16; e += 2) {
+            const float a = v[e], b = v[e + 1];
+            v[e] = __fadd_rn(a, b), v[e + 1] = __fsub_rn(a, b);
+        }
+    }
+    uint64_t p[8];
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
+    for (int e = 0; e < 8; ++e) p[e] = pair_of(v[2 * e], v[2 * e + 1]);
+    const uint64_t minus = pair_of(-1.0f, -1.0f);
+#pragma unroll
+    for (int h = 1; h < 8; h <<= 1) {
+        if (2 * h < had_block) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
                 if (!(e & h)) {
-                    const float a = v[e], b = v[e + h];
-                    v[e] = __fadd_rn(a, b), v[e + h] = __fsub_rn(a, b);
+                    const uint64_t a = p[e], b = p[e + h];
+                    p[e] = pair_add(a, b), p[e + h] = pair_fma(b, minus, a);
                 }
         }
     }
 #pragma unroll
     for (int h = 16; h < kKvD; h <<= 1) {
         const float sign = (l & (h >> 4)) ? -1.0f : 1.0f;   // upper element: other - v, lower: other + v, one rounding
+        const uint64_t signs = pair_of(sign, sign);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float other = __shfl_xor_sync(0xffffffffu, v[e], h >> 4);
-            if (h < had_block) v[e] = __fmaf_rn(sign, v[e], other);
+        for (int e = 0; e < 8; ++e) {
+            const uint64_t other = __shfl_xor_sync(0xffffffffu, static_cast<unsigned long long>(p[e]), h >> 4);
+            if (h < had_block) p[e] = pair_fma(signs, p[e], other);
         }
     }
     if (had_block > 1) {
+        const uint64_t inv = pair_of(inv_sqrt_b, inv_sqrt_b);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = __fmul_rn(v[e], inv_sqrt_b);
+        for (int e = 0; e < 8; ++e) p[e] = pair_mul(p[e], inv);
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pair_to(p[e], v[2 * e], v[2 * e + 1]);
 }
 
 // Sixteen values per lane of an eight-lane group -> sixteen 4-bit codes (value e at bits 4e), scale and zero-point; the fp32 steps
@@ -148,13 +187,16 @@ __device__ __forceinline__ uint2 kv_quantize16(const float (&v)[16], float clip,
     const int bias = zi - 0x4b400000;
     uint32_t w[2] = {0u, 0u};
     bool near = false;
+    const uint64_t inv2 = pair_of(inv, inv), round2 = pair_of(kRound, kRound), back2 = pair_of(-kRound, -kRound), minus = pair_of(-1.0f, -1.0f);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const float y = __fmul_rn(v[e], inv);
-        const float t = __fadd_rn(y, kRound);
-        near |= !(fabsf(__fsub_rn(y, __fsub_rn(t, kRound))) <= 0.5f - 0x1p-16f);
-        const int c = max(0, min(15, __float_as_int(t) + bias));
-        w[e >> 3] |= static_cast<uint32_t>(c) << (4 * (e & 7));
+    for (int e = 0; e < 16; e += 2) {
+        const uint64_t y = pair_mul(pair_of(v[e], v[e + 1]), inv2), t = pair_add(y, round2);
+        float t0, t1, d0, d1;
+        pair_to(t, t0, t1);
+        pair_to(pair_fma(pair_add(t, back2), minus, y), d0, d1);   // what the rounding took
+        near |= !(fabsf(d0) <= 0.5f - 0x1p-16f) || !(fabsf(d1) <= 0.5f - 0x1p-16f);
+        w[e >> 3] |= static_cast<uint32_t>(max(0, min(15, __float_as_int(t0) + bias))) << (4 * (e & 7));
+        w[e >> 3] |= static_cast<uint32_t>(max(0, min(15, __float_as_int(t1) + bias))) << (4 * (e & 7) + 4);
     }
     if (near) {
         w[0] = w[1] = 0u;
@@ -178,28 +220,32 @@ __device__ __forceinline__ int kv_value_offset(int token, int l, int u) {
     return kPgV + ((w * 4 + cq) * 8 + (g ^ (2 * cq))) * 16 + n * 4 + (token & 1) * 2;
 }
 
+// Sixteen values of a lane as they stand in memory, and in fp32.
 template <bool BF16>
-__device__ __forceinline__ void kv_load16(const void* X, size_t offset, float (&v)[16]) {
-    if constexpr (BF16) {
-        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(X) + offset);
+struct Kv16 {
+    uint4 raw[BF16 ? 2 : 4];
+    __device__ __forceinline__ void load(const void* X, size_t offset) {
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(X) + offset * (BF16 ? 2 : 4));
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint4 q = p[i];
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        for (int i = 0; i < (BF16 ? 2 : 4); ++i) raw[i] = p[i];
+    }
+    __device__ __forceinline__ void get(float (&v)[16]) const {
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 2 : 4); ++i) {
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                v[8 * i + 2 * k] = __uint_as_float(w[k] << 16);
-                v[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+                if constexpr (BF16) v[8 * i + 2 * k] = __uint_as_float(w[k] << 16), v[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+                else v[4 * i + k] = __uint_as_float(w[k]);
             }
         }
-    } else {
-        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(X) + offset);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 f = p[i];
-            v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
-        }
     }
+};
+template <bool BF16>
+__device__ __forceinline__ void kv_load16(const void* X, size_t offset, float (&v)[16]) {
+    Kv16<BF16> x;
+    x.load(X, offset);
+    x.get(v);
 }
 template <bool BF16>
 __device__ __forceinline__ void kv_store16(void* X, size_t offset, const float (&v)[16]) {
@@ -250,8 +296,9 @@ __device__ __forceinline__ int kv_find_block(const KvMoveParams& p, int& lo, int
     return r;
 }
 
-// Rows -> codes.  Groups of eight lanes take vectors (head, token; all keys, then all values).  A whole block is put together in
-// shared memory and leaves in 16-byte stores; the tokens of a part of a block go straight to their places.
+// Rows -> codes.  Groups of eight lanes take vectors (head, token; all keys, then all values).  Blocks are put together in shared
+// memory: a whole one leaves in 16-byte stores, of a part the keys leave in 16 bytes, the values in pairs of tokens (4 bytes) or
+// alone (2).  One or two tokens go straight to their places.
 template <bool BF16>
 __global__ void __launch_bounds__(kPgThreads)
 kv4_paged_write_kernel(const KvMoveParams p) {
@@ -266,22 +313,38 @@ kv4_paged_write_kernel(const KvMoveParams p) {
     if (!block0) return;
     const size_t head_step = static_cast<size_t>(p.pages.page_tokens / kPgTokens) * kPgBlock;
     const int n = hi - lo, vectors = n * heads;
-    const bool whole = n == kPgTokens;
+    const bool whole = n == kPgTokens, direct = n < 3;
     const int l = threadIdx.x & 7, group = threadIdx.x >> 3;
     const long long row0 = p.rows.begin(r) + (static_cast<long long>(lo) - p.rows.first[r]);
+    // vector i: the first half are keys, the second values; within, token by token of head by head
+    auto where = [&](int i, bool& is_v, int& h, int& t) {
+        is_v = i >= vectors;
+        const int j = i < 2 * vectors ? (is_v ? i - vectors : i) : 0;
+        h = j / n, t = j - h * n;
+    };
+    Kv16<BF16> ahead;                    // the next vector's values are on their way while one is quantized
+    auto fetch = [&](int i) {
+        bool is_v;
+        int h, t;
+        where(i, is_v, h, t);
+        ahead.load(is_v ? p.V : p.K, static_cast<size_t>((row0 + t) * (is_v ? p.v_stride : p.k_stride)) + (h0 + h) * kKvD + 16 * l);
+    };
     // the trip count is the same for the four groups of a warp: shuffles are executed by all lanes
+    if ((group & ~3) < 2 * vectors) fetch(group);
     for (int base = group & ~3; base < 2 * vectors; base += kPgGroups) {
         const int i = base + (group & 3);
-        const bool on = i < 2 * vectors, is_v = i >= vectors;
-        const int j = on ? (is_v ? i - vectors : i) : 0;
-        const int h = j / n, t = j - h * n;
+        const bool on = i < 2 * vectors;
+        bool is_v;
+        int h, t;
+        where(i, is_v, h, t);
         float v[16];
-        kv_load16<BF16>(is_v ? p.V : p.K, static_cast<size_t>((row0 + t) * (is_v ? p.v_stride : p.k_stride)) + (h0 + h) * kKvD + 16 * l, v);
+        ahead.get(v);
+        if (base + kPgGroups < 2 * vectors) fetch(i + kPgGroups);
         kv_rotate16(v, l, is_v ? p.v_had : p.k_had, is_v ? p.v_inv_sqrt : p.k_inv_sqrt);
         float s, z;
         const uint2 c = kv_quantize16(v, p.clip, s, z);
         if (!on) continue;
-        uint8_t* dst = whole ? image[h] : block0 + h * head_step;
+        uint8_t* dst = direct ? block0 + h * head_step : image[h];
         const int token = (lo + t) % kPgTokens;
         if (is_v) {
 #pragma unroll
@@ -295,11 +358,36 @@ kv4_paged_write_kernel(const KvMoveParams p) {
             dst[(is_v ? kPgVz : kPgKz) + token] = static_cast<uint8_t>(static_cast<int>(z));
         }
     }
-    if (!whole) return;
+    if (direct) return;
     __syncthreads();
-    for (int i = threadIdx.x; i < heads * (kPgBlock / 16); i += kPgThreads) {
-        const int h = i / (kPgBlock / 16), k = i - h * (kPgBlock / 16);
-        reinterpret_cast<uint4*>(block0 + h * head_step)[k] = reinterpret_cast<const uint4*>(image[h])[k];
+    if (whole) {
+        for (int i = threadIdx.x; i < heads * (kPgBlock / 16); i += kPgThreads) {
+            const int h = i / (kPgBlock / 16), k = i - h * (kPgBlock / 16);
+            reinterpret_cast<uint4*>(block0 + h * head_step)[k] = reinterpret_cast<const uint4*>(image[h])[k];
+        }
+        return;
+    }
+    const int first = lo % kPgTokens;
+    auto in = [&](int token) { return static_cast<unsigned>(token - first) < static_cast<unsigned>(n); };
+    for (int h = 0; h < heads; ++h) {
+        uint8_t* to = block0 + h * head_step;
+        for (int i = threadIdx.x; i < 128 + 512 + 4 * kPgTokens; i += kPgThreads) {
+            if (i < 128) {                       // a piece of keys: one token
+                const int cq = (i >> 3) & 3, token = 8 * (i >> 5) + ((i & 7) ^ (2 * cq));
+                if (in(token)) reinterpret_cast<uint4*>(to)[i] = reinterpret_cast<const uint4*>(image[h])[i];
+            } else if (i < 128 + 512) {          // a word of values: two tokens
+                const int k = i - 128, cq = (k >> 5) & 3, token = 8 * (k & 3) + 2 * cq;
+                const uint32_t word = reinterpret_cast<const uint32_t*>(image[h] + kPgV)[k];
+                if (in(token) && in(token + 1)) reinterpret_cast<uint32_t*>(to + kPgV)[k] = word;
+                else if (in(token)) reinterpret_cast<uint16_t*>(to + kPgV)[2 * k] = static_cast<uint16_t>(word);
+                else if (in(token + 1)) reinterpret_cast<uint16_t*>(to + kPgV)[2 * k + 1] = static_cast<uint16_t>(word >> 16);
+            } else {
+                const int k = (i - 128 - 512) / kPgTokens, token = i % kPgTokens;
+                if (!in(token)) continue;
+                if (k < 2) reinterpret_cast<uint32_t*>(to + (k ? kPgVs : kPgKs))[token] = reinterpret_cast<const uint32_t*>(image[h] + (k ? kPgVs : kPgKs))[token];
+                else to[(k == 3 ? kPgVz : kPgKz) + token] = image[h][(k == 3 ? kPgVz : kPgKz) + token];
+            }
+        }
     }
 }
 
@@ -347,10 +435,15 @@ kv4_paged_read_kernel(const KvMoveParams p) {
             w[0] = c.x, w[1] = c.y;
         }
         const float s = reinterpret_cast<const float*>(src + (is_v ? kPgVs : kPgKs))[token];
-        const int z = src[(is_v ? kPgVz : kPgKz) + token];
+        // a code under the exponent of 2^23 is 2^23 + code: less 2^23 + zero it is code - zero, exactly
+        const float z = -(8388608.0f + static_cast<float>(src[(is_v ? kPgVz : kPgKz) + token]));
+        const uint64_t z2 = pair_of(z, z), s2 = pair_of(s, s);
         float v[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = __fmul_rn(s, static_cast<float>(static_cast<int>((w[e >> 3] >> (4 * (e & 7))) & 15u) - z));
+        for (int e = 0; e < 16; e += 2) {
+            const uint32_t c0 = ((w[e >> 3] >> (4 * (e & 7))) & 15u) | 0x4b000000u, c1 = ((w[e >> 3] >> (4 * (e & 7) + 4)) & 15u) | 0x4b000000u;
+            pair_to(pair_mul(pair_add(pair_of(__uint_as_float(c0), __uint_as_float(c1)), z2), s2), v[e], v[e + 1]);
+        }
         kv_rotate16(v, l, is_v ? p.v_had : p.k_had, is_v ? p.v_inv_sqrt : p.k_inv_sqrt);
         if (on) kv_store16<BF16>(X, static_cast<size_t>((row0 + t) * (is_v ? p.v_stride : p.k_stride)) + (h0 + h) * kKvD + 16 * l, v);
     }
@@ -380,9 +473,15 @@ kv4_paged_keep_kernel(const KvPages pages, const KvRows rows, const int32_t* __r
         uint16_t kc[kPgKeepAhead], vc[kPgKeepAhead];
         uint32_t extra[kPgKeepAhead];
         bool have[kPgKeepAhead];
+        uint8_t* to[kPgKeepAhead];   // (looked up while the indices are on their way)
+        int from_of[kPgKeepAhead];
+#pragma unroll
+        for (int i = 0; i < kPgKeepAhead; ++i) from_of[i] = i0 + i < kept ? keep[begin + i0 + i] : -1;
+#pragma unroll
+        for (int i = 0; i < kPgKeepAhead; ++i) to[i] = i0 + i < kept ? place(i0 + i) : nullptr;
 #pragma unroll
         for (int i = 0; i < kPgKeepAhead; ++i) {
-            const int from = i0 + i < kept ? keep[begin + i0 + i] : -1;
+            const int from = from_of[i];
             const uint8_t* b = place(from);
             have[i] = b != nullptr;
             kc[i] = vc[i] = 0, extra[i] = 0;
@@ -397,8 +496,8 @@ kv4_paged_keep_kernel(const KvPages pages, const KvRows rows, const int32_t* __r
         }
 #pragma unroll
         for (int i = 0; i < kPgKeepAhead; ++i) {
-            uint8_t* b = have[i] ? place(i0 + i) : nullptr;
-            if (!b) continue;
+            uint8_t* b = to[i];
+            if (!b || !have[i]) continue;
             const int token = (first + i0 + i) % kPgTokens;
             *reinterpret_cast<uint16_t*>(b + kv_key_offset(token, l) + 2 * u) = kc[i];
             *reinterpret_cast<uint16_t*>(b + kv_value_offset(token, l, u)) = vc[i];

@@ -1715,12 +1715,15 @@ inline long long most_blocks(int total, int R) {
     const long long b = (static_cast<long long>(total) + 62ll * R) / kPgTokens;
     return b < total ? b : total;
 }
-// KV heads of a CTA of the write and the read: one for prompts (a block is work enough for its 32 groups); for rows that come by
-// the few, as many as give the groups a vector each.
+// KV heads of a CTA of the write and the read: as many as leave four CTAs for an SM -- a CTA first has to find its block, which takes
+// as long as a head's work (9873 tokens x 8 heads written and read back: one head 54 us, four MEASURED_US) -- and for rows that come
+// by the few, as many as give the groups a vector each.
 inline int move_heads(int total, int R, int H) {
     const long long rows = (total + R - 1) / R;
-    const int h = rows >= 16 ? 1 : rows >= 4 ? 4 : kPgMaxHeads;
-    return h < H ? h : H;
+    long long h = most_blocks(total, R) * H / (4ll * sm_count());
+    if (rows < 4) h = kPgMaxHeads;
+    if (h > kPgMaxHeads) h = kPgMaxHeads;
+    return h < 1 ? 1 : h < H ? static_cast<int>(h) : H;
 }
 template <typename Kernel>
 int run_move(Kernel f32, Kernel bf16, int x_dtype, const KvMoveParams& p, cudaStream_t st) {

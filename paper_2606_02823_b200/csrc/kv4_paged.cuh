@@ -118,8 +118,9 @@ __device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c)
 // In-place butterfly over the 128 values of a vector in eight lanes (value index 16 * l + e), strides below had_block; natural
 // order, the same operands as everywhere else in this library.  had_block may differ between the groups of a warp.  A difference is
 // taken as -1 * b + a in one rounding.
-__device__ __forceinline__ void kv_rotate16(float (&v)[16], int l, int had_block, float inv_sqrt_b) {
-    if (!__any_sync(0xffffffffu, had_block > 1)) return;
+template <bool FULL>   // had_block is 128 in every lane
+__device__ __forceinline__ void kv_rotate16_as(float (&v)[16], int l, int had, float inv_sqrt_b) {
+    const int had_block = FULL ? kKvD : had;
     if (1 < had_block) {
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
@@ -159,6 +160,10 @@ __device__ __forceinline__ void kv_rotate16(float (&v)[16], int l, int had_block
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) pair_to(p[e], v[2 * e], v[2 * e + 1]);
+}
+__device__ __forceinline__ void kv_rotate16(float (&v)[16], int l, int had_block, float inv_sqrt_b) {
+    if (__all_sync(0xffffffffu, had_block == kKvD)) kv_rotate16_as<true>(v, l, had_block, inv_sqrt_b);
+    else if (__any_sync(0xffffffffu, had_block > 1)) kv_rotate16_as<false>(v, l, had_block, inv_sqrt_b);
 }
 
 // Sixteen values per lane of an eight-lane group -> sixteen 4-bit codes (value e at bits 4e), scale and zero-point; the fp32 steps

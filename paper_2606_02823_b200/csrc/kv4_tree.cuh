@@ -44,7 +44,7 @@ struct KvTreeParams {
 };
 
 constexpr int kTreeRow = 132;        // floats of a row's piece: numerator, reference point, sum, two unused
-constexpr int kTreeMinRun = 2;       // items of a warp's run at least
+constexpr int kTreeMinRun = 1;       // items of a run at least (mma.sync, one token over 1023 cached ones: 1: 13.4 us, 2: 15.7, 4: 21.0)
 constexpr float kTreeSlack = 6.0f;   // binary orders that a weight may exceed its reference by: w * 2^8 stays below 2^14
 constexpr int kTreeVexp = 40;           // exponent field of the smallest power of two that value scales are measured against
 constexpr int kTreeSite = 48;        // site of an expired wait
@@ -185,18 +185,18 @@ __device__ __forceinline__ void tree_load_query(const KvTreeParams& p, int begin
     using S = TreeShape<BF16, ROWS>;
     const int lane = threadIdx.x & 31, l = lane & 7, sub = lane >> 3;
     const int valid = min(ROWS, n * p.G - tile * ROWS);
-    for (int base = 0; base < ROWS; base += 4) {
+    // rows that do not exist keep what an earlier tile left, or the zeros of the start: they are columns of their own
+#pragma unroll 1
+    for (int base = 0; base < valid; base += 4) {
         const int row = base + sub, rho = tile * ROWS + row;
         float v[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] = 0.0f;
-        if (base < valid) {                      // the same for the whole warp
-            if (row < valid) {
-                const int i = rho / p.G, g = rho - i * p.G;
-                kv_load16<BF16>(p.q, static_cast<size_t>((static_cast<long long>(begin) + i) * p.q_stride) + (h * p.G + g) * kKvD + 16 * l, v);
-            }
-            kv_rotate16(v, l, p.q_had, p.q_inv_sqrt);
+        if (row < valid) {
+            const int i = rho / p.G, g = rho - i * p.G;
+            kv_load16<BF16>(p.q, static_cast<size_t>((static_cast<long long>(begin) + i) * p.q_stride) + (h * p.G + g) * kKvD + 16 * l, v);
         }
+        kv_rotate16(v, l, p.q_had, p.q_inv_sqrt);
         float top = 0.0f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(v[e]));
@@ -289,6 +289,7 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
     uint64_t* bars = reinterpret_cast<uint64_t*>(fact + ROWS * S::kParts);
     if (lane < ST) mbar_init(&bars[lane], 1);
     mbar_fence_init();
+    for (int i = lane; i < (S::kQuery + ROWS * S::kParts * 16) / 16; i += 32) reinterpret_cast<uint4*>(operands)[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncwarp();
     pdl_wait();
 
@@ -468,14 +469,16 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
                 const int to = max(vexp, static_cast<int>(__reduce_max_sync(0xffffffffu, top) >> 23));
                 const float corr = __uint_as_float(static_cast<uint32_t>(max(1, 127 + vexp - to)) << 23);   // what is 2^126 smaller is gone
                 vexp = to;
+                if (b != b0) {            // (nothing to scale before the first block)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
+                    for (int t = 0; t < NT; ++t) {
 #pragma unroll
-                    for (int x = 0; x < 8; ++x)
+                        for (int x = 0; x < 8; ++x)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[t][x][i] *= corr;
-                    z[t][0] *= corr, z[t][1] *= corr;
-                    l_run[t][0] *= corr, l_run[t][1] *= corr;
+                            for (int i = 0; i < 4; ++i) o[t][x][i] *= corr;
+                        z[t][0] *= corr, z[t][1] *= corr;
+                        l_run[t][0] *= corr, l_run[t][1] *= corr;
+                    }
                 }
             }
             const float vshift = static_cast<float>(134 - vexp);   // weights and their sum carry 2^8 / 2^(vexp - 126)
@@ -498,9 +501,12 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
                         for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
                         const float to = fmaxf(top, m_run[t][e]);
                         const float corr = to > m_run[t][e] ? ex2(m_run[t][e] - to) : 1.0f;   // from -inf: 0
-                        m_run[t][e] = to, l_run[t][e] *= corr, z[t][e] *= corr;
+                        m_run[t][e] = to;
+                        if (b != b0) {
+                            l_run[t][e] *= corr, z[t][e] *= corr;
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) o[t][x][e] *= corr, o[t][x][2 + e] *= corr;
+                            for (int x = 0; x < 8; ++x) o[t][x][e] *= corr, o[t][x][2 + e] *= corr;
+                        }
                     }
                     const float ref = vshift - m_run[t][e];
 #pragma unroll

@@ -1716,7 +1716,7 @@ inline long long most_blocks(int total, int R) {
     return b < total ? b : total;
 }
 // KV heads of a CTA of the write and the read: as many as leave four CTAs for an SM -- a CTA first has to find its block, which takes
-// as long as a head's work (9873 tokens x 8 heads written and read back: one head 54 us, four MEASURED_US) -- and for rows that come
+// as long as a head's work (9873 tokens x 8 heads written and read back: one head 53 us, four 50) -- and for rows that come
 // by the few, as many as give the groups a vector each.
 inline int move_heads(int total, int R, int H) {
     const long long rows = (total + R - 1) / R;

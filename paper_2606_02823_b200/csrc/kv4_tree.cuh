@@ -530,15 +530,22 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
                 }
             }
             // ---- O += codes . w: row tile 2w + j of dimensions 32w + 4g + {j, j + 2}
+            // The matrix instruction cuts its sums off instead of rounding them, always towards zero, which a long run of blocks
+            // would add up (fp32, 3087 tokens a tile: 2.7e-6 of the output's norm): there each block's sum starts from zero and
+            // joins the others by an fp32 addition.  To bf16's 2^-9 it is nothing.
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < NT; ++t) {
+                float sum[4] = {};
 #pragma unroll
-                for (int part = 0; part < S::kParts; ++part)
+                for (int part = S::kParts - 1; part >= 0; --part)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) mma_f16(z[t], vz[2 * k], 0u, vz[2 * k + 1], 0u, wb[t][part][2 * k], wb[t][part][2 * k + 1]);
+                    for (int k = 0; k < 2; ++k) mma_f16(S::kSplit ? sum : z[t], vz[2 * k], 0u, vz[2 * k + 1], 0u, wb[t][part][2 * k], wb[t][part][2 * k + 1]);
+                if (S::kSplit) z[t][0] += sum[0], z[t][1] += sum[1];
+            }
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 const uint32_t x[4] = {vw[w].x, vw[w].y, vw[w].z, vw[w].w};
+                float sum[2][4] = {};
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -552,9 +559,14 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
 #pragma unroll
                         for (int t = 0; t < NT; ++t)
 #pragma unroll
-                            for (int part = 0; part < S::kParts; ++part)
-                                mma_f16(o[t][2 * w + j], v[0], v[1], v[2], v[3], wb[t][part][2 * k], wb[t][part][2 * k + 1]);
+                            for (int part = S::kParts - 1; part >= 0; --part)
+                                mma_f16(S::kSplit ? sum[j] : o[t][2 * w + j], v[0], v[1], v[2], v[3], wb[t][part][2 * k], wb[t][part][2 * k + 1]);
                     }
+                if (S::kSplit)            // one column tile
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[0][2 * w + j][i] += sum[j][i];
             }
         };
         for (int b = b0; b < b1; ++b, stage = stage + 1 == ST ? 0 : stage + 1) {

@@ -410,8 +410,7 @@ int qift_kv4_attention_decode(const float* q, const uint8_t* k_codes, const floa
  *                        dimensions 32w + 4g .. + 3, ascending                        (w, cq, n 0..3, g 0..7, h 0..1)
  *   4096 / 4224  fp32 scales of the keys / values by token     4352 / 4384  their zero-points, one byte by token
  * value = scale * (code - zero), quantized exactly as qift_kv4_quantize does it (a range so small that its scale would round to 0
- * counts as empty).  D must be 128; page_tokens is a multiple of
- * 32, 32 .. 1024.  Every byte belongs to one token.
+ * counts as empty).  D must be 128; page_tokens is a multiple of 32, 32 .. 1024.  Every byte belongs to one token.
  *
  * A call takes `total` rows that R requests share:
  *   row_start   [R + 1] int32, ascending: request r has rows row_start[r] .. row_start[r + 1] - 1 (possibly none); rows from
@@ -433,14 +432,14 @@ int qift_kv4_attention_decode(const float* q, const uint8_t* k_codes, const floa
  *
  * qift_kv4_paged_keep: after the check of a drafted tree that was written at positions first ..: position first + i takes the
  * token at first + keep[row_start[r] + i], i = 0 .. kept_start[r + 1] - kept_start[r] - 1 (at most the request's rows).
- *   keep        [total] int32, ascending within a request (the accepted path); indices outside its rows move nothing
+ *   keep        [total] int32, ascending within a request, none twice (the accepted path); indices outside its rows move nothing
  *   kept_start  [R + 1] int32: the row_start of a batch of the kept tokens alone
  *
  * qift_kv4_paged_attention: out[row][h] = sum_t softmax_t(scale * q[row][h] . K[t]) V[t] for KV head h / (Hq / H), over the
  * positions that the row sees: all before `first`, and of the drafted ones first + j (written before the call) those whose
  * bit j & 31 of mask[row][j / 32] is set -- its ancestors and itself, for a tree.  A row that sees nothing gets zeros.
  *   q           in  [total][Hq][D] fp32 or bf16, rows q_stride elements apart (>= Hq * D, whole 16-byte units);
- *               out has its type, [total][Hq][D] contiguous
+ *               out has its type, [total][Hq][D] contiguous, and shares no memory with q
  *   q_had_block the rotation of the keys, applied to the query in the call;  scale > 0, or 0 for 1 / sqrt(D)
  *   mask        [total][mask_words] int32, mask_words 1 .. 32 (drafted tokens beyond its bits are not seen), or NULL: a row sees
  *               the drafted tokens up to itself
@@ -470,15 +469,16 @@ int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int
 /* Low-rank adapters of many requests beside a shared projection (whose product is any of the linear calls above):
  *     out[m] = y[m] + scaling[a] * B[a] (A[a] x[m]),   a = adapter[r] of the request r that row m belongs to
  *   X           in  [M][K] fp32 or bf16, the projection's input before its rotation; K % 8 == 0
- *   A, B        in  bf16 [adapters][rank][K] and [adapters][N][rank]; rank a multiple of 8, 8 .. 128 (pad with zeros); N % 8 == 0
+ *   A, B        in  bf16 [adapters][rank][K] and [adapters][N][rank]; rank a multiple of 8, 8 .. 128 (pad with zeros); N % 8 == 0;
+ *               M up to 2^31 - 256
  *   scaling     in  fp32 [adapters]
  *   row_start   [R + 1] int32, ascending; rows before row_start[0] and from row_start[R] on belong to nobody and keep their `out`
  *   adapter     [R] int32; values that are not 0 .. adapters - 1: no adapter, out = y
  *   y           in  [M][N], or NULL for zeros;  out [M][N], may be y itself; both of X's type
  *   workspace   >= qift_lora_workspace_bytes(M, rank, K) bytes, as for the attention
- * Sums in fp32; the small product A x is kept in fp32; fp32 inputs are multiplied at (at least) 16-bit precision in two exact
- * parts.
- * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (K, N, rank), ALIGNMENT, WORKSPACE, CUDA. */
+ * Sums in fp32.  fp32 rows are multiplied in three bf16 parts (2^-25 of a value is lost); the small product A x is kept in fp32 and
+ * multiplied in three such parts for fp32 results, in two (2^-17) for bf16 ones.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (M, K, N, rank), ALIGNMENT, WORKSPACE, CUDA. */
 size_t qift_lora_workspace_bytes(int M, int rank, int K);
 int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16_t* B, const float* scaling, int adapters, int rank,
                      int M, int N, int K, const int32_t* row_start, const int32_t* adapter, int R, const void* y, void* out,

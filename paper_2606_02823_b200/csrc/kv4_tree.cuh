@@ -442,6 +442,8 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 ks[n] = *reinterpret_cast<const float*>(blk + kPgKs + (8 * n + g) * 4);
+                // an infinite scale stands for a vector that is no number; the codes' product, 0, is exact without the 8 only
+                if (S::kSplit) ks[n] = fmaf(ks[n], 0.0f, ks[n]);
                 vs[n] = *reinterpret_cast<const float*>(blk + kPgVs + (8 * n + g) * 4);
                 vz[n] = __byte_perm(*reinterpret_cast<const uint16_t*>(blk + kPgVz + 8 * n + 2 * cq), 0u, 0x4140u);
                 if (S::kSplit) vz[n] = lessened(vz[n] | 0x64006400u, 0xe408e408u);   // - 1032
@@ -602,7 +604,7 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
                 if (token_of[t][e] < 0) continue;
                 const int row = 8 * t + 2 * cq + e, hq = h * p.G + tile * ROWS + row - token_of[t][e] * p.G;
                 const size_t out_at = (static_cast<size_t>(begin + token_of[t][e]) * p.Hq + hq) * kKvD;
-                const float inv = whole ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
+                const float inv = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;   // 0: nothing was seen
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     float y[4];
@@ -673,7 +675,7 @@ kv4_tree_join_kernel(const KvTreeParams p) {
                 }
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
-                    if (!(t[i].x > -INFINITY)) continue;
+                    if (t[i].y == 0.0f) continue;   // saw nothing; scores that are no numbers leave a sum that is none, which stays
                     const float to = fmaxf(m, t[i].x), a = ex2(m - to), c = ex2(t[i].x - to);
                     acc.x = fmaf(acc.x, a, x[i].x * c), acc.y = fmaf(acc.y, a, x[i].y * c);
                     acc.z = fmaf(acc.z, a, x[i].z * c), acc.w = fmaf(acc.w, a, x[i].w * c);
@@ -689,7 +691,7 @@ kv4_tree_join_kernel(const KvTreeParams p) {
             if (sub == 0) {
                 for (int s = 1; s < share; ++s) {
                     const float2 t = ml[warp + s];
-                    if (!(t.x > -INFINITY)) continue;
+                    if (t.y == 0.0f) continue;
                     const float4 x = num[warp + s][lane];
                     const float to = fmaxf(m, t.x), a = ex2(m - to), c = ex2(t.x - to);
                     acc.x = fmaf(acc.x, a, x.x * c), acc.y = fmaf(acc.y, a, x.y * c);
@@ -700,7 +702,7 @@ kv4_tree_join_kernel(const KvTreeParams p) {
         }
         if (local < valid && sub == 0) {
             const int rho = tile * ROWS + row, i = rho / p.G, hq = h * p.G + rho - i * p.G;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
             const size_t at = (static_cast<size_t>(begin + i) * p.Hq + hq) * kKvD + 4 * lane;
             if constexpr (BF16) {
                 const __nv_bfloat162 a = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), c = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);

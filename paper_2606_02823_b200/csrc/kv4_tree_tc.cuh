@@ -380,7 +380,8 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                 const float2 told = marks[((n - 1) & 1) * 128 + row];
                 m = told.x, vexp = __float_as_int(told.y);
                 const float c1 = __uint_as_float(static_cast<uint32_t>(vexp) << 23);
-                float l = l_m > -INFINITY ? sum2(l2) * ex2(l_m - m) * __uint_as_float(static_cast<uint32_t>(max(1, 127 + l_vexp - vexp)) << 23) : 0.0f;
+                float l = sum2(l2);  // without a reference point: 0, or no number when no score was one
+                if (l_m > -INFINITY) l *= ex2(l_m - m) * __uint_as_float(static_cast<uint32_t>(max(1, 127 + l_vexp - vexp)) << 23);
                 l = (l * 0x1p-7f) * c1;
                 meet();              // the reference points have been read by both
                 marks[turn * 128 + row].x = l;

@@ -17,9 +17,10 @@
 //   q is scaled by a power of two per row (largest value 2^7 .. 2^8) and held in fp16: exact for bf16 queries that are not
 //   rotated, else off by 2^-12.  fp32 calls hold q and w in two fp16 parts each (residual 2^-22), multiplied one after the other
 //   into the same sums, and all codes lessened by 8 (1024 + c - 1032 in fp16, exact): the sums of an average over many tokens
-//   would otherwise be far larger than the result and lose what the zero-points take away.  w is normalised by the largest value
-//   scale seen so far (a power of two, one for the warp) and by the row's reference point, which moves only when a score exceeds
-//   it by more than kTreeSlack.
+//   would otherwise be far larger than the result and lose what the zero-points take away.
+//   w = 2^(score - R) vs, and the sum of 2^(score - R) beside it, go by one reference point R for each row: a bound of score + log2(vs)
+//   over the tokens that the row has seen, so a large value scale counts with its weight, and for the rows that see it alone.  R
+//   moves (by whole binary orders, so nothing is rounded) only when a token exceeds it by more than kTreeSlack.
 // Bound by instruction issue and the latency that 16 (12) warps an SM leave: about 515 warp instructions a block with eight rows, 530
 // with sixteen.  32 query and 8 KV heads: 64 single tokens over 8000 cached ones each (286 MB) 64 us = 4.5 TB/s; 16 trees of up to 13
 // tokens over 6000 (67 MB, read again by every tile) 68 us.
@@ -49,7 +50,7 @@ struct KvTreeParams {
 constexpr int kTreeRow = 132;        // floats of a row's piece: numerator, reference point, sum, two unused
 constexpr int kTreeMinRun = 1;       // items of a run at least (mma.sync, one token over 1023 cached ones: 1: 13.4 us, 2: 15.7, 4: 21.0)
 constexpr float kTreeSlack = 6.0f;   // binary orders that a weight may exceed its reference by: w * 2^8 stays below 2^14
-constexpr int kTreeVexp = 40;           // exponent field of the smallest power of two that value scales are measured against
+constexpr int kTreeVexp = 40;        // exponent field that smaller value scales count with: sums of 2^(score - R) stay below 2^100 a token
 constexpr int kTreeSite = 48;        // site of an expired wait
 
 // As mbar_wait, for waits that are short and mostly over when they begin: a loop of four instructions, bounded by its trips (a trip
@@ -81,6 +82,11 @@ __device__ __forceinline__ uint32_t lessened(uint32_t x, uint32_t by) {   // fp1
     uint32_t y;
     asm("add.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(by));
     return y;
+}
+
+// The power of two above a value scale, as its exponent.
+__device__ __forceinline__ float tree_order(float vs) {
+    return static_cast<float>(max(kTreeVexp, static_cast<int>(__float_as_uint(vs) >> 23 & 0xffu)) - 126);
 }
 
 // What a call makes of a request, in row tiles of ROWS and units of UNIT tokens.
@@ -378,8 +384,6 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) m_run[t][e] = -INFINITY, l_run[t][e] = 0.0f;
         }
-        // value scales are measured against 2^(vexp - 126), the first power of two above them: weights carry 2^8 over it
-        int vexp = kTreeVexp;
         const int plain_blocks = min(q.first, q.len) / kPgTokens;   // blocks that are context altogether
 
         int stage = 0;
@@ -465,59 +469,75 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
                 for (int n = 0; n < 4; ++n)
                     if (8 * n + g >= left) vs[n] = 0.0f;
             }
-            // ---- the power of two of the value scales
-            const float vtop = fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3]));
-            if (__any_sync(0xffffffffu, vtop >= __uint_as_float(static_cast<uint32_t>(vexp + 1) << 23))) {
-                uint32_t top = 0;         // the largest finite one
+            // ---- vectors of zeros: scale 1, whatever the others' are, and codes and zero-point 0 (in lane cq of token 8n + 2cq + h).  They
+            // add nothing, so a scale of 0 does as well, which neither moves R nor leaves a rounding error of the codes less 8
+            auto drop_zero_vectors = [&]() {
+                if (!__any_sync(0xffffffffu, vs[0] == 1.0f || vs[1] == 1.0f || vs[2] == 1.0f || vs[3] == 1.0f)) return;
 #pragma unroll
-                for (int n = 0; n < 4; ++n) top = max(top, __float_as_uint(vs[n]) < 0x7f800000u ? __float_as_uint(vs[n]) : 0u);
-                const int to = max(vexp, static_cast<int>(__reduce_max_sync(0xffffffffu, top) >> 23));
-                const float corr = __uint_as_float(static_cast<uint32_t>(max(1, 127 + vexp - to)) << 23);   // what is 2^126 smaller is gone
-                vexp = to;
-                if (b != b0) {            // (nothing to scale before the first block)
+                for (int n = 0; n < 4; ++n) {
+                    uint32_t x = vz[n] ^ (S::kSplit ? 0xc800c800u : 0u);   // - 8
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
+                    for (int w = 0; w < 4; ++w) x |= n == 0 ? vw[w].x : n == 1 ? vw[w].y : n == 2 ? vw[w].z : vw[w].w;
 #pragma unroll
-                        for (int x = 0; x < 8; ++x)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[t][x][i] *= corr;
-                        z[t][0] *= corr, z[t][1] *= corr;
-                        l_run[t][0] *= corr, l_run[t][1] *= corr;
-                    }
+                    for (int i = 4; i < 32; i <<= 1) x |= __shfl_xor_sync(0xffffffffu, x, i);
+                    x = __shfl_sync(0xffffffffu, x, g >> 1);
+                    if (vs[n] == 1.0f && ((g & 1) ? x >> 16 : x & 0xffffu) == 0u) vs[n] = 0.0f;
                 }
+            };
+            if (S::kSplit) drop_zero_vectors();
+            // ---- scores, and whether one may exceed its row's reference point: by the lane's largest score and value scale, of whatever
+            // tokens they are
+            const float order = tree_order(fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])));
+            bool raise = false;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        float& x = sc[t][n >> 1][2 * (n & 1) + e];
+                        x *= ks[n];
+                        if (!kPlain && !(seen[t][e] >> (8 * n) & 1)) x = -INFINITY;
+                        top = fmaxf(top, x);
+                    }
+                    raise |= fmaf(top, factor[t][e], order) > m_run[t][e] + kTreeSlack;
+                }
+            if (__any_sync(0xffffffffu, raise)) {   // token by token
+                if (!S::kSplit) drop_zero_vectors();
+                float of[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) of[n] = tree_order(vs[n]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) top = fmaxf(top, fmaf(sc[t][n >> 1][2 * (n & 1) + e], factor[t][e], of[n]));
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                        const float to = fmaxf(ceilf(top), m_run[t][e]);
+                        const float corr = to > m_run[t][e] ? ex2(m_run[t][e] - to) : 1.0f;   // from -inf: 0
+                        m_run[t][e] = to;
+                        if (b != b0) {    // (nothing to scale before the first block)
+                            l_run[t][e] *= corr, z[t][e] *= corr;
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) o[t][x][e] *= corr, o[t][x][2 + e] *= corr;
+                        }
+                    }
             }
-            const float vshift = static_cast<float>(134 - vexp);   // weights and their sum carry 2^8 / 2^(vexp - 126)
             uint32_t wb[NT][S::kParts][4];   // weights as B operands: tokens of group n, columns = rows
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 float w[2][4];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float s[4], top = -INFINITY;
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        s[n] = sc[t][n >> 1][2 * (n & 1) + e] * ks[n];
-                        if (!kPlain && !(seen[t][e] >> (8 * n) & 1)) s[n] = -INFINITY;
-                        top = fmaxf(top, s[n]);
-                    }
-                    top *= factor[t][e];
-                    if (__any_sync(0xffffffffu, top > m_run[t][e] + kTreeSlack)) {
-#pragma unroll
-                        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-                        const float to = fmaxf(top, m_run[t][e]);
-                        const float corr = to > m_run[t][e] ? ex2(m_run[t][e] - to) : 1.0f;   // from -inf: 0
-                        m_run[t][e] = to;
-                        if (b != b0) {
-                            l_run[t][e] *= corr, z[t][e] *= corr;
-#pragma unroll
-                            for (int x = 0; x < 8; ++x) o[t][x][e] *= corr, o[t][x][2 + e] *= corr;
-                        }
-                    }
-                    const float ref = vshift - m_run[t][e];
+                    const float at = 8.0f - m_run[t][e];   // weights and their sum carry 2^8
 #pragma unroll
                     for (int n = 0; n < 4; ++n) {
                         const bool on = kPlain || (seen[t][e] >> (8 * n) & 1);
-                        const float pr = on ? ex2(fmaf(s[n], factor[t][e], ref)) : 0.0f;
+                        const float pr = on ? ex2(fmaf(sc[t][n >> 1][2 * (n & 1) + e], factor[t][e], at)) : 0.0f;
                         l_run[t][e] += pr;
                         w[e][n] = on ? pr * vs[n] : 0.0f;
                     }
@@ -591,7 +611,6 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
 
         // ---- the tile, or this warp's piece of it
         const bool whole = walk.whole();
-        const float c1 = __uint_as_float(static_cast<uint32_t>(vexp) << 23);   // 2^(vexp - 127), times 2 / 2^8 and the codes' 2^24 below
         float* piece_at = p.partial + static_cast<size_t>(2 * me + (walk.u == walk.u0 ? 0 : 1)) * ROWS * kTreeRow;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -600,7 +619,6 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
                 float l = l_run[t][e];
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-                l = (l * 0x1p-7f) * c1;      // the weights' own power of two
                 if (token_of[t][e] < 0) continue;
                 const int row = 8 * t + 2 * cq + e, hq = h * p.G + tile * ROWS + row - token_of[t][e] * p.G;
                 const size_t out_at = (static_cast<size_t>(begin + token_of[t][e]) * p.Hq + hq) * kKvD;
@@ -610,7 +628,7 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
                     float y[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        y[j] = (fmaf(o[t][2 * w + (j & 1)][(j & 2) + e], (j & 1) ? 0.0625f : 1.0f, -z[t][e]) * (S::kSplit ? 0x1p-7f : 0x1p17f)) * c1 * inv;
+                        y[j] = fmaf(o[t][2 * w + (j & 1)][(j & 2) + e], (j & 1) ? 0.0625f : 1.0f, -z[t][e]) * (S::kSplit ? 1.0f : 0x1p24f) * inv;
                     const int d = 32 * w + 4 * g;
                     if (!whole) {
                         *reinterpret_cast<float4*>(piece_at + row * kTreeRow + d) = make_float4(y[0], y[1], y[2], y[3]);

@@ -36,9 +36,9 @@ constexpr int kTtTile = 16384;               // bytes of a tile
 constexpr int kTtConvert = 5;                // conversion warps
 constexpr int kTtThreads = 32 * (8 + kTtConvert + 3);
 constexpr int kTtRing = 20;                  // blocks on their way to the conversion; three items of them wait for their values to be due
-constexpr int kTtScaleBytes = 2 * kTtUnit * 4 + 16;   // scales of keys and values; per block: largest value scale, whether it is there
+constexpr int kTtScaleBytes = 2 * kTtUnit * 4 + 16;   // scales of keys and values; largest and smallest value scale of both blocks (0: no such block)
 constexpr int kTtStage = 8 * 4096;           // 4 KB of a softmax warp: query operands on their way in, results on their way out
-constexpr int kTtSmem = 1024 + 2 * kTtTiles * kTtTile + kTtRing * kPgBlock + 2 * kTtDepth * kTtScaleBytes + kTtStage + 2 * 128 * 8 + 768;
+constexpr int kTtSmem = 1024 + 2 * kTtTiles * kTtTile + kTtRing * kPgBlock + 2 * kTtDepth * kTtScaleBytes + kTtStage + 2 * 128 * 4 + 768;
 constexpr uint32_t kTtS = 0, kTtO = 256, kTtQ = 384;   // tensor-memory columns: four S (the weights take the place of the first half), O, Q
 
 // D[tmem] (+)= A[tmem] * B[smem descriptor], fp16 operands, fp32 sums
@@ -58,6 +58,11 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint32_t tc_ld1(uint32_t taddr) {
+    uint32_t x;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(x) : "r"(taddr) : "memory");
+    return x;
 }
 __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&v)[16]) {
     asm volatile(
@@ -113,7 +118,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
     uint8_t* raw = smem + 2 * kTtTiles * kTtTile;  // ring of blocks
     uint8_t* scales = raw + kTtRing * kPgBlock;    // [2 * kTtDepth] items
     uint8_t* stage = scales + 2 * kTtDepth * kTtScaleBytes;
-    float2* marks = reinterpret_cast<float2*>(stage + kTtStage);   // [item parity][row] reference points
+    float* marks = reinterpret_cast<float*>(stage + kTtStage);     // [item parity][row] reference points
     uint64_t* bars = reinterpret_cast<uint64_t*>(marks + 2 * 128);
     uint64_t* raw_full = bars;                     // [kTtRing] fetch -> conversion
     uint64_t* raw_free = raw_full + kTtRing;       // [kTtRing] conversion -> fetch
@@ -213,7 +218,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                     for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                     const int field = max(16, min(254, static_cast<int>(__float_as_uint(top) >> 23)));
                     const float up = __uint_as_float(static_cast<uint32_t>(min(254, 261 - field)) << 23);
-                    if (l == 0) marks[quarter * 32 + row32].x = __uint_as_float(static_cast<uint32_t>(max(1, field - 7)) << 23) * 0x1p24f * p.scale_log2;
+                    if (l == 0) marks[quarter * 32 + row32] = __uint_as_float(static_cast<uint32_t>(max(1, field - 7)) << 23) * 0x1p24f * p.scale_log2;
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         uint32_t x[4];
@@ -227,7 +232,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                     }
                 }
                 meet();
-                factor = marks[row].x;
+                factor = marks[row];
                 uint32_t w[32];
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
@@ -242,10 +247,8 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full);
 
-            float m = -INFINITY;                              // reference point and exponent field of the value scales, as of an item
-            int vexp = kTreeVexp;
-            float l_m = -INFINITY;                            // those that this warp's sum of weights goes by
-            int l_vexp = kTreeVexp;
+            float m = -INFINITY;                              // reference point as of an item
+            float l_m = -INFINITY;                            // the one that this warp's sum of weights goes by
             uint64_t l2 = 0;                                  // two sums of weights
             const uint32_t n0 = n;
             n += walk.b1 - walk.b0;
@@ -256,10 +259,12 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                              mbar_wait_near(&scale_full[i % (2 * kTtDepth)], (i / (2 * kTtDepth)) & 1, kTreeSite + 2);
                 tc_fence_after();
                 if (active) {
-                    const uint32_t sl = smem_u32(scales + (i % (2 * kTtDepth)) * kTtScaleBytes);
-                    const uint4 info = lds128(sl + 2 * kTtUnit * 4);   // largest value scale of the two blocks, whether they are there
-                    const int vtop = static_cast<int>(max(info.x, info.y) >> 23);
-                    const bool plain = (unit + 1) * kTtUnit <= min(q.first, q.len) && (info.z & info.w);
+                    const float* item_scales = reinterpret_cast<const float*>(scales + (i % (2 * kTtDepth)) * kTtScaleBytes);
+                    const uint32_t sl = smem_u32(item_scales);
+                    const uint4 info = lds128(sl + 2 * kTtUnit * 4);   // largest and smallest value scale of the two blocks (0: not there)
+                    const float order = tree_order(__uint_as_float(max(info.x, info.y)));
+                    const bool alike = order - tree_order(__uint_as_float(min(info.z - 1, info.w - 1))) <= 4.0f;   // (a block that is not there: 0 - 1)
+                    const bool plain = (unit + 1) * kTtUnit <= min(q.first, q.len) && info.z && info.w && alike;
                     auto weigh = [&](auto plain_tag) {        // scores -> weights
                         constexpr bool kPlain = decltype(plain_tag)::value;
                         uint32_t x[2][32], seen[2];           // of tokens 32 b + 0 .. 31
@@ -288,23 +293,33 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                             for (int c = 0; c < 32; c += 2)
                                 best[(c >> 1) & 3] = fmaxf(best[(c >> 1) & 3], fmaxf(__uint_as_float(x[b][c]), __uint_as_float(x[b][c + 1])));
                         }
-                        const float top = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])) * factor;
+                        const float top = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
                         // ---- the row's reference point: the one of the item before, raised if need be
                         float m_old = -INFINITY;
-                        int vexp_old = kTreeVexp;
                         if (i != n0) {
                             if (ok) ok = mbar_wait_near(&mark_full[((i - 1) & 1) * 4 + quarter], ((i - 1) >> 1) & 1, kTreeSite + 12);
-                            const float2 told = marks[((i - 1) & 1) * 128 + row];
-                            m_old = told.x, vexp_old = __float_as_int(told.y);
+                            m_old = marks[((i - 1) & 1) * 128 + row];
                         }
-                        m = top > m_old + kTreeSlack ? ceilf(top) : m_old;   // whole binary orders
-                        vexp = max(vexp_old, vtop);
-                        marks[(i & 1) * 128 + row] = make_float2(m, __int_as_float(vexp));
+                        m = m_old;
+                        const float bound = fmaf(top, factor, order);   // by the largest value scale of any token
+                        if (__any_sync(0xffffffffu, bound > m_old + kTreeSlack)) {
+                            float highest = bound;
+                            if (!kPlain && !alike) {          // token by token, of those that are seen
+                                highest = -INFINITY;
+#pragma unroll 1
+                                for (int c = 0; c < kTtUnit; ++c) {   // (a short loop: as long code it slows the whole kernel, 258 -> 280 us)
+                                    const float score = __uint_as_float(tc_ld1(s_at + c)) * item_scales[c] * factor;
+                                    if ((c < 32 ? seen[0] : seen[1]) >> (c & 31) & 1) highest = fmaxf(highest, score + tree_order(item_scales[kTtUnit + c]));
+                                }
+                            }
+                            if (highest > m_old + kTreeSlack) m = ceilf(highest);   // whole binary orders
+                        }
+                        marks[(i & 1) * 128 + row] = m;
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&mark_full[(i & 1) * 4 + quarter]);
-                        if (i != n0 && __any_sync(0xffffffffu, m != m_old || vexp != vexp_old)) {
+                        if (i != n0 && __any_sync(0xffffffffu, m != m_old)) {
                             // O of the item before times what the references differ by, row by row
-                            const float corr = (m != m_old ? ex2(m_old - m) : 1.0f) * __uint_as_float(static_cast<uint32_t>(max(1, 127 + vexp_old - vexp)) << 23);
+                            const float corr = m != m_old ? ex2(m_old - m) : 1.0f;
                             if (ok) ok = mbar_wait_near(&o_done[(i - 1) % kTtDepth], ((i - 1) / kTtDepth) & 1, kTreeSite + 3);
                             tc_fence_after();
 #pragma unroll 1
@@ -318,14 +333,14 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                             }
                             tc_wait_st();
                         }
-                        if (__any_sync(0xffffffffu, m != l_m || vexp != l_vexp)) {
-                            const float corr = l_m > -INFINITY ? ex2(l_m - m) * __uint_as_float(static_cast<uint32_t>(max(1, 127 + l_vexp - vexp)) << 23) : 0.0f;
+                        if (__any_sync(0xffffffffu, m != l_m)) {
+                            const float corr = l_m > -INFINITY ? ex2(l_m - m) : 0.0f;
                             l2 = __float_as_uint(sum2(l2) * corr);
-                            l_m = m, l_vexp = vexp;
+                            l_m = m;
                         }
                         // ---- weights
                         const uint64_t f2 = both(factor);
-                        const uint64_t r2 = both(static_cast<float>(134 - vexp) - m);   // weights and their sum carry 2^8 / 2^(vexp - 126)
+                        const uint64_t r2 = both(8.0f - m);   // weights and their sum carry 2^8
                         uint64_t l3 = 0;
 #pragma unroll
                         for (int b = 0; b < 2; ++b) {
@@ -377,16 +392,13 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                 const bool whole = walk.whole();
                 // the last item's reference point, and this warp's sum brought to it
                 if (ok) ok = mbar_wait_near(&mark_full[((n - 1) & 1) * 4 + quarter], ((n - 1) >> 1) & 1, kTreeSite + 12);
-                const float2 told = marks[((n - 1) & 1) * 128 + row];
-                m = told.x, vexp = __float_as_int(told.y);
-                const float c1 = __uint_as_float(static_cast<uint32_t>(vexp) << 23);
+                m = marks[((n - 1) & 1) * 128 + row];
                 float l = sum2(l2);  // without a reference point: 0, or no number when no score was one
-                if (l_m > -INFINITY) l *= ex2(l_m - m) * __uint_as_float(static_cast<uint32_t>(max(1, 127 + l_vexp - vexp)) << 23);
-                l = (l * 0x1p-7f) * c1;
+                if (l_m > -INFINITY) l *= ex2(l_m - m);
                 meet();              // the reference points have been read by both
-                marks[turn * 128 + row].x = l;
+                marks[turn * 128 + row] = l;
                 meet();
-                l += marks[(turn ^ 1) * 128 + row].x;
+                l += marks[(turn ^ 1) * 128 + row];
                 const float inv = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
                 float* piece = p.partial + (static_cast<size_t>(2 * blockIdx.x + (walk.u == walk.u0 ? 0 : 1)) * kTtRows + quarter * 32) * kTreeRow;
                 float4* own = reinterpret_cast<float4*>(stage + quarter * 8192 + turn * 4096);   // the quarter's own, as for the query
@@ -402,7 +414,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                     for (int g = 0; g < 8; ++g) {
                         float y[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) y[j] = (__uint_as_float(a[8 * j + g]) * ((j & 1) ? 0x1p13f : 0x1p17f)) * c1 * inv;
+                        for (int j = 0; j < 4; ++j) y[j] = __uint_as_float(a[8 * j + g]) * ((j & 1) ? 0x1p20f : 0x1p24f) * inv;
                         own[lane * 8 + (g ^ (lane & 7))] = make_float4(y[0], y[1], y[2], y[3]);
                     }
                     __syncwarp();
@@ -478,13 +490,21 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                 uint8_t* sl = scales + (item % (2 * kTtDepth)) * kTtScaleBytes;
                 const bool in = lane < tokens;
                 const float ksc = in ? reinterpret_cast<const float*>(src + kPgKs)[lane] : 0.0f;
-                const float vsc = in ? reinterpret_cast<const float*>(src + kPgVs)[lane] : 0.0f;
+                float vsc = in ? reinterpret_cast<const float*>(src + kPgVs)[lane] : 0.0f;
+                if (vsc == 1.0f && src[kPgVz + lane] == 0) {   // a vector of zeros?  It adds nothing, and its scale says nothing
+                    uint32_t codes = 0;
+#pragma unroll 1
+                    for (int i = 0; i < 32; ++i) codes |= *reinterpret_cast<const uint16_t*>(src + kv_value_offset(lane, i >> 2, i & 3));
+                    if (codes == 0) vsc = 0.0f;
+                }
+                __syncwarp();
                 reinterpret_cast<float*>(sl)[32 * blk + lane] = ksc;
                 reinterpret_cast<float*>(sl + kTtUnit * 4)[32 * blk + lane] = vsc;
                 const uint32_t bits = __float_as_uint(vsc);
-                const uint32_t top = __reduce_max_sync(0xffffffffu, bits < 0x7f800000u ? bits : 0u);
+                const bool counts = bits - 1u < 0x7f7fffffu;   // finite, not 0
+                const uint32_t top = __reduce_max_sync(0xffffffffu, counts ? bits : 0u), least = __reduce_min_sync(0xffffffffu, counts ? bits : 0x7f7fffffu);
                 uint32_t* info = reinterpret_cast<uint32_t*>(sl + 2 * kTtUnit * 4);
-                if (lane == 0) info[blk] = top, info[2 + blk] = have;
+                if (lane == 0) info[blk] = top, info[2 + blk] = have ? least : 0u;
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&k_full[buf]), mbar_arrive(&scale_full[item % (2 * kTtDepth)]), mbar_arrive(&raw_free[slot]);

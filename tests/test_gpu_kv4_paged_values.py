@@ -69,3 +69,72 @@ def test_a_cached_token_that_is_no_number_reaches_the_rows_that_see_it(where, n,
     isnan = torch.isnan(got).cpu().numpy()
     assert isnan[bad].all() and not isnan[~bad].any()
     ok()
+
+
+# -------------------------------------------------------------------------------------- scales that differ by many orders
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [4, 12, 60])
+@pytest.mark.parametrize("factor", [1e6, 1e10, 1e20, 1e30])
+def test_large_values_leave_the_rows_that_do_not_see_them(factor, n, dtype):
+    rows, first = [n, n], [75, 300]
+    b = filled(540, rows, first, 2, 32)
+    mask = trees(9, rows, 2)
+    K, V = qift.qift_kv4_paged_read(b.pages, b.rs, b.f, 2 * n)
+    V[1] *= factor                                                                    # drafted token 1 of request 0, 2 of request 1
+    V[n + 2] *= -factor
+    qift.qift_kv4_paged_write(K, V, b.pages, b.rs, b.f)
+    q, qn = values(550, (2 * n, 8, D), dtype)
+    sees = np.array([(mask[i, 0] >> (1 if i < n else 2)) & 1 for i in range(2 * n)], bool)
+    assert sees.any() and not sees.all()
+    check(b, q, qn, dtype, mask)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", WIDTHS)
+@pytest.mark.parametrize("strength,factor", [(2.0, 1e6), (4.0, 1e10), (16.0, 1e30)])
+def test_large_values_of_tokens_that_hardly_count(strength, factor, n, dtype):
+    """Tokens that every row sees, with values so large and weights so small that their product is nothing, or of the others' size."""
+    rows, first = [n, n], [400, 1000]
+    b = filled(560, rows, first, 2, 32, had=0)
+    w = torch.ones(D, device="cuda")
+    w[::2] = -1.0
+    at = [[33, 200], [0, 999]]
+    for r, where in enumerate(at):
+        for pos in where:                                                             # one token of request r
+            K = (-strength * w).expand(1, 2, D).contiguous()
+            V = values(570 + pos, (1, 2, D), "f32", scale=factor)[0]
+            qift.qift_kv4_paged_write(K, V, b.pages, ints([0, 1, 1] if r == 0 else [0, 0, 1]), ints([pos, pos]))
+    q, _ = values(580, (2 * n, 8, D), "f32", scale=0.5)
+    q = (q + strength * w / 2).to(DTYPES[dtype])
+    check(b, q, q.float().cpu().numpy(), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", WIDTHS)
+@pytest.mark.parametrize("size", [1e-6, 1e-9, 1e-20])
+def test_zero_vectors_among_small_values(size, n, dtype):
+    """A vector of zeros is held with scale 1, whatever the others' scales are."""
+    rows, first = [n, n], [200, 130]
+    b = Batch(590, rows, first, 2, 64)
+    cut = np.concatenate([[0], np.cumsum([f + n for f in first])])
+    k = values(591, (int(cut[-1]), 2, D), "f32", 0.1)[0]
+    v = values(592, (int(cut[-1]), 2, D), "f32", -0.1)[0] * size
+    v[3::7] = 0.0
+    v[int(cut[1]) - 1, 1] = 0.0
+    qift.qift_kv4_paged_write(k, v, b.pages, ints(cut), ints([0, 0]))
+    q, qn = values(593, (2 * n, 8, D), dtype)
+    check(b, q, qn, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", WIDTHS)
+@pytest.mark.parametrize("size", [1e24, 1e-24])
+def test_values_of_any_size(size, n, dtype):
+    rows, first = [n, n], [200, 1300]
+    b = Batch(600, rows, first, 2, 64)
+    cut = np.concatenate([[0], np.cumsum([f + n for f in first])])
+    k = values(601, (int(cut[-1]), 2, D), "f32", 0.1)[0]
+    v = values(602, (int(cut[-1]), 2, D), "f32", -0.1)[0] * size
+    qift.qift_kv4_paged_write(k, v, b.pages, ints(cut), ints([0, 0]))
+    q, qn = values(603, (2 * n, 8, D), dtype)
+    check(b, q, qn, dtype)

@@ -53,6 +53,20 @@ __device__ __forceinline__ uint32_t take_bf16(float& x, float& y) {
     return bits;
 }
 
+// acc += 32 k of fp32 rows in three parts.  The matrix instruction cuts its sums off instead of rounding them, always towards zero: one
+// accumulator through all of K = 11008 ended up to 5e-5 short.  So 32 k are summed from zero, the small parts first, and join by a rounded
+// addition.  (bf16 rows, two instructions per 32 k, lose 2e-5 at that length beside the 2^-9 of their result.)
+__device__ __forceinline__ void lora_add_parts(float (&acc)[4], const uint32_t (&a)[3][2][4], const uint4& b) {
+    float sum[4] = {};
+#pragma unroll
+    for (int part = 2; part >= 0; --part) {
+        mma_bf16(sum, a[part][0], b.x, b.y);
+        mma_bf16(sum, a[part][1], b.z, b.w);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += sum[i];
+}
+
 // The CTA's item: rows [m0, m1) of a request and its adapter (-1: none); false when there is no such item.
 template <int WM>
 __device__ __forceinline__ bool lora_item(const LoraParams& p, int& m0, int& m1, int& adapter) {
@@ -144,20 +158,17 @@ lora_down_kernel(const LoraParams p) {
                     v[h][4 * i] = __uint_as_float(mine[h][i].x), v[h][4 * i + 1] = __uint_as_float(mine[h][i].y);
                     v[h][4 * i + 2] = __uint_as_float(mine[h][i].z), v[h][4 * i + 3] = __uint_as_float(mine[h][i].w);
                 }
+            uint32_t a[kParts][2][4];                       // part, k-step
 #pragma unroll
-            for (int part = 0; part < kParts; ++part) {
-                uint32_t w[2][4];
+            for (int part = 0; part < kParts; ++part)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[h][e] = take_bf16(v[h][2 * e], v[h][2 * e + 1]);
-                const uint32_t a0[4] = {w[0][0], w[1][0], w[0][1], w[1][1]}, a1[4] = {w[0][2], w[1][2], w[0][3], w[1][3]};
+                    for (int e = 0; e < 4; ++e) a[part][e >> 1][2 * (e & 1) + h] = take_bf16(v[h][2 * e], v[h][2 * e + 1]);
 #pragma unroll
-                for (int j = 0; j < 2 * RS; ++j) {
-                    if (8 * j >= p.rank) break;
-                    mma_bf16(acc[j], a0, b[j].x, b[j].y);
-                    mma_bf16(acc[j], a1, b[j].z, b[j].w);
-                }
+            for (int j = 0; j < 2 * RS; ++j) {
+                if (8 * j >= p.rank) break;
+                lora_add_parts(acc[j], a, b[j]);
             }
         }
     };
@@ -438,10 +449,11 @@ lora_down_wide_kernel(const LoraParams p) {
             for (int j = 0; j < 2 * RS; ++j) {
                 if (8 * j >= p.rank) break;
                 const uint4 b = lds128(from + 8 * j * S::kPitch + 64 * half);
-#pragma unroll
-                for (int part = 0; part < kParts; ++part) {
-                    mma_bf16(acc[j], a[part][0], b.x, b.y);
-                    mma_bf16(acc[j], a[part][1], b.z, b.w);
+                if constexpr (BF16) {
+                    mma_bf16(acc[j], a[0][0], b.x, b.y);
+                    mma_bf16(acc[j], a[0][1], b.z, b.w);
+                } else {
+                    lora_add_parts(acc[j], a, b);
                 }
             }
         }

@@ -191,7 +191,8 @@ __device__ __forceinline__ uint2 kv_quantize16(const float (&v)[16], float clip,
     const float inv = __fdiv_rn(1.0f, s);
     const int bias = zi - 0x4b400000;
     uint32_t w[2] = {0u, 0u};
-    bool near = false;
+    // beyond 2^21 (tiny clipping ratios, values that are no numbers) the sum's bits are not the integer's
+    bool near = !(fmaxf(-mn, mx) * inv <= 0x1p21f);
     const uint64_t inv2 = pair_of(inv, inv), round2 = pair_of(kRound, kRound), back2 = pair_of(-kRound, -kRound), minus = pair_of(-1.0f, -1.0f);
 #pragma unroll
     for (int e = 0; e < 16; e += 2) {

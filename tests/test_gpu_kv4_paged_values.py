@@ -138,3 +138,33 @@ def test_values_of_any_size(size, n, dtype):
     qift.qift_kv4_paged_write(k, v, b.pages, ints(cut), ints([0, 0]))
     q, qn = values(603, (2 * n, 8, D), dtype)
     check(b, q, qn, dtype)
+
+
+# ------------------------------------------------------------------------------------------------- clipping ratios
+def quantized(x, clip):
+    """The definition, each step rounded to fp32 once; codes are clamped, however large the quotient."""
+    f = np.float32
+    lo, hi = (np.minimum(x.min(-1), f(0)) * f(clip)).astype(f), (np.maximum(x.max(-1), f(0)) * f(clip)).astype(f)
+    s = ((hi - lo).astype(f) / f(15)).astype(f)
+    z = np.rint((-lo / s).astype(f))
+    return np.clip(np.rint((x / s[..., None]).astype(f)).astype(np.float64) + z[..., None], 0, 15).astype(np.uint8), s, z
+
+
+def clip_rows():
+    x = values(660, (64, 1, D), "f32")[1].copy()
+    x[:8] = np.abs(x[:8])                                                             # one-sided ranges
+    x[8:16] = -np.abs(x[8:16])
+    x[16, 0, :2], x[17, 0, :2] = (-1.0, -0.9), (1.0, 0.9)
+    return x
+
+
+@pytest.mark.parametrize("clip", [1e-3, 1e-5, 3e-6, 1.2e-6, 1e-6, 8e-7, 6e-7, 5e-7, 3e-7, 1e-7])
+def test_write_with_small_clipping_ratios(clip):
+    x = clip_rows()
+    b = Batch(670, [64], [0], 1, 64)
+    qift.qift_kv4_paged_write(torch.from_numpy(x).cuda(), torch.from_numpy(x).cuda(), b.pages, b.rs, b.f, clip_ratio=clip)
+    held = limits.ref.cached(b.pool(), b.table, 64, 0, 64)
+    code, s, z = quantized(x, clip)
+    for got in (held[:3], held[3:]):
+        assert np.array_equal(got[1], s) and np.array_equal(got[2], z.astype(np.uint8)) and np.array_equal(got[0], code)
+    ok()

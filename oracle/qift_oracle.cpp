@@ -495,7 +495,8 @@ void orc_kv4_quantize(const float* X, long long rows, int D, int B, float clip, 
         }
         for (int d = 0; d < D; ++d) {
             const float t = scratch[d] / s;
-            const int c = (int)std::rint(t) + (int)z;
+            const float u = (float)std::rint(t);   // clamped before it becomes an int: a tiny clipping ratio makes it any size
+            const int c = (u > 15.0f ? 15 : u < -15.0f ? -15 : (int)u) + (int)z;
             codes[(size_t)r * D + d] = (uint8_t)clampi(c, 0, 15);
         }
         scale[r] = s;

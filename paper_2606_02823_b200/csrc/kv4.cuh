@@ -70,7 +70,7 @@ __device__ __forceinline__ uint32_t kv4_quantize_vector(float (&v)[4], int lane,
     uint32_t packed = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const int c = max(0, min(15, __float2int_rn(__fdiv_rn(v[e], s)) + zi));
+        const int c = max(0, min(15, min(__float2int_rn(__fdiv_rn(v[e], s)), 15) + zi));   // 2^31 - 1, of any larger quotient, plus zi would wrap
         packed |= static_cast<uint32_t>(c) << (4 * e);
     }
     return packed;

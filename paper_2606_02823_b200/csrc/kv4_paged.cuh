@@ -208,7 +208,7 @@ __device__ __forceinline__ uint2 kv_quantize16(const float (&v)[16], float clip,
         w[0] = w[1] = 0u;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const int c = max(0, min(15, __float2int_rn(__fdiv_rn(v[e], s)) + zi));
+            const int c = max(0, min(15, min(__float2int_rn(__fdiv_rn(v[e], s)), 15) + zi));   // 2^31 - 1, of any larger quotient, plus zi would wrap
             w[e >> 3] |= static_cast<uint32_t>(c) << (4 * (e & 7));
         }
     }

@@ -168,3 +168,24 @@ def test_write_with_small_clipping_ratios(clip):
     for got in (held[:3], held[3:]):
         assert np.array_equal(got[1], s) and np.array_equal(got[2], z.astype(np.uint8)) and np.array_equal(got[0], code)
     ok()
+
+
+# --------------------------------------------------------------------------------- quotients beyond 32-bit integers
+@pytest.mark.parametrize("clip", [1e-9, 2e-10, 1e-12, 1e-20])
+def test_quotients_beyond_32_bit_integers(clip):
+    """All of a vector but its zeros is far outside the range: end codes, in the paged cache and in the contiguous one."""
+    x = clip_rows()
+    x[20:30, 0, ::3] = 0.0
+    X = torch.from_numpy(x).cuda()
+    code, s, z = quantized(x, clip)
+    assert set(np.unique(code)) > {0, 15}
+    b = Batch(680, [64], [0], 1, 64)
+    qift.qift_kv4_paged_write(X, X, b.pages, b.rs, b.f, clip_ratio=clip)
+    held = limits.ref.cached(b.pool(), b.table, 64, 0, 64)
+    for got in (held[:3], held[3:]):
+        assert np.array_equal(got[1], s) and np.array_equal(got[2], z.astype(np.uint8)) and np.array_equal(got[0], code)
+    one = qift.Kv4Cache(1, 64)
+    qift.qift_kv4_quantize(X, one, clip_ratio=clip)
+    packed = code[:, 0, 0::2] | code[:, 0, 1::2] << 4
+    assert np.array_equal(one.codes.cpu().numpy()[0], packed) and np.array_equal(one.scale.cpu().numpy()[0], s[:, 0])
+    ok()

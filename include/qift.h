@@ -470,7 +470,7 @@ int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int
  *     out[m] = y[m] + scaling[a] * B[a] (A[a] x[m]),   a = adapter[r] of the request r that row m belongs to
  *   X           in  [M][K] fp32 or bf16, the projection's input before its rotation; K % 8 == 0
  *   A, B        in  bf16 [adapters][rank][K] and [adapters][N][rank]; rank a multiple of 8, 8 .. 128 (pad with zeros); N % 8 == 0;
- *               M up to 2^31 - 256
+ *               M up to 2^31 - 256, N and K up to 2^31 - 2^20
  *   scaling     in  fp32 [adapters]
  *   row_start   [R + 1] int32, ascending; rows before row_start[0] and from row_start[R] on belong to nobody and keep their `out`
  *   adapter     [R] int32; values that are not 0 .. adapters - 1: no adapter, out = y

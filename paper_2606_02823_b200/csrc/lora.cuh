@@ -38,6 +38,7 @@ constexpr int kLoraThreads = 256;
 constexpr int kLoraWarps = kLoraThreads / 32;
 constexpr int kLoraMaxRank = 128;
 constexpr int kLoraMaxRows = 0x7fffff00;   // a row index and a tile more fit 32 bits
+constexpr int kLoraMaxSize = 0x7ff00000;   // N, K: an index and all slices' roundings (592 x 256, 16 x 64) and steps more fit 32 bits
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile(

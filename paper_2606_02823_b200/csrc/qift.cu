@@ -1777,13 +1777,13 @@ int run_lora(LoraParams p, cudaStream_t st) {
     const long long items = most < p.M ? most : p.M;
     const int splits = lora_splits(items, p.K);
     p.k_slice = ((p.K + splits - 1) / splits + 63) & ~63;
-    p.splits = (p.K + p.k_slice - 1) / p.k_slice;
+    p.splits = (p.K - 1) / p.k_slice + 1;
     // columns of a CTA: about four CTAs per SM in all
     long long slices = (4ll * sm_count() + items - 1) / items;
     const int most_slices = (p.N + 255) / 256;
     if (slices > most_slices) slices = most_slices;
     p.n_slice = static_cast<int>(((p.N + slices - 1) / slices + 255) / 256) * 256;
-    const dim3 down(static_cast<unsigned>(items), p.splits), up(static_cast<unsigned>(items), (p.N + p.n_slice - 1) / p.n_slice);
+    const dim3 down(static_cast<unsigned>(items), p.splits), up(static_cast<unsigned>(items), (p.N - 1) / p.n_slice + 1);
     cudaError_t e;
     if constexpr (WIDE) {
         e = allow_smem(lora_down_wide_kernel<BF16, RS>, LoraDownWide<BF16, RS>::kSmem);
@@ -1893,7 +1893,7 @@ int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int
 }
 
 size_t qift_lora_workspace_bytes(int M, int rank, int K) {
-    if (M <= 0 || rank <= 0 || K <= 0) return 0;
+    if (M <= 0 || rank <= 0 || K <= 0 || rank > kLoraMaxRank || M > kLoraMaxRows || K > kLoraMaxSize) return 0;
     const int splits = lora_splits((M + 16ll * kLoraWarps - 1) / (16 * kLoraWarps), K);   // no call has fewer items than this
     return (static_cast<size_t>(splits) * M * rank * sizeof(float) + 15) & ~static_cast<size_t>(15);
 }
@@ -1904,7 +1904,8 @@ int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16
     if (!X || !A || !B || !scaling || !row_start || !adapter || !out) return QIFT_ERR_INVALID_ARG;
     if (adapters <= 0 || rank <= 0 || M <= 0 || N <= 0 || K <= 0 || R <= 0) return QIFT_ERR_INVALID_ARG;
     if (x_dtype != QIFT_F32 && x_dtype != QIFT_BF16) return QIFT_ERR_INVALID_ARG;
-    if (K % 8 != 0 || N % 8 != 0 || rank % 8 != 0 || rank > kLoraMaxRank || M > kLoraMaxRows) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (K % 8 != 0 || N % 8 != 0 || N > kLoraMaxSize || K > kLoraMaxSize || rank % 8 != 0 || rank > kLoraMaxRank || M > kLoraMaxRows)
+        return QIFT_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(X) || !aligned16(A) || !aligned16(B) || !aligned16(y) || !aligned16(out) || !aligned16(workspace) ||
         !aligned4(scaling) || !aligned4(row_start) || !aligned4(adapter))
         return QIFT_ERR_ALIGNMENT;

@@ -417,8 +417,8 @@ int qift_kv4_attention_decode(const float* q, const uint8_t* k_codes, const floa
  *               row_start[R] on belong to nobody: nothing of them is read or written
  *   first       [R] int32: the cache position of the request's first row (= its cached tokens before this call)
  *   page_table  [R][max_pages] int32: the page that holds positions i * page_tokens .. of a request.  Entries that are not
- *               0 .. num_pages - 1 are no pages, and positions before 0 or from max_pages * page_tokens on have none: such
- *               tokens are not written, not moved, seen by nobody, and their rows of a read are left as they were.
+ *               0 .. num_pages - 1 are no pages, and positions before 0 or from max_pages * page_tokens (at most 2^31 - 32) on
+ *               have none: such tokens are not written, not moved, seen by nobody, and their rows of a read are left as they were.
  * Requests may share pages that are read; a position that two requests write in one call, or that one call writes twice, ends up
  * with the bytes of either.  All four calls read these arrays on the device, in stream order: they can be captured into a graph
  * and replayed with other contents (the same total, R and max_pages).

@@ -99,7 +99,7 @@ __device__ __forceinline__ TreeRequest tree_request(const KvTreeParams& p, int r
     q.n = p.rows.count(r), q.first = p.rows.first[r];
     const long long end = static_cast<long long>(q.first) + q.n;
     q.len = static_cast<int>(max(0ll, min(end, static_cast<long long>(capacity))));
-    q.units = q.n > 0 ? max(1, (q.len + UNIT - 1) / UNIT) : 0;   // rows over nothing still get their zeros
+    q.units = q.n > 0 ? (q.len - 1) / UNIT + 1 : 0;   // rows over nothing (-1 / UNIT is 0) still get their zeros; len + UNIT may not fit
     q.tiles = (q.n * p.G + ROWS - 1) / ROWS;
     return q;
 }

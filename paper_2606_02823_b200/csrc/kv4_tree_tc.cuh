@@ -264,7 +264,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                     const uint4 info = lds128(sl + 2 * kTtUnit * 4);   // largest and smallest value scale of the two blocks (0: not there)
                     const float order = tree_order(__uint_as_float(max(info.x, info.y)));
                     const bool alike = order - tree_order(__uint_as_float(min(info.z - 1, info.w - 1))) <= 4.0f;   // (a block that is not there: 0 - 1)
-                    const bool plain = (unit + 1) * kTtUnit <= min(q.first, q.len) && info.z && info.w && alike;
+                    const bool plain = unit < min(q.first, q.len) / kTtUnit && info.z && info.w && alike;
                     auto weigh = [&](auto plain_tag) {        // scores -> weights
                         constexpr bool kPlain = decltype(plain_tag)::value;
                         uint32_t x[2][32], seen[2];           // of tokens 32 b + 0 .. 31

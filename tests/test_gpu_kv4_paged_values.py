@@ -140,6 +140,48 @@ def test_values_of_any_size(size, n, dtype):
     check(b, q, qn, dtype)
 
 
+# ------------------------------------------------------------------------------------------------- every block counts
+@pytest.mark.parametrize("rows,first", [([1], [1000]), ([64, 20], [700, 31]), ([1], [40000]), ([64, 40, 7], [5000, 64, 9000]), ([13, 0, 4, 7], [95, 20, 0, 257]),
+                                        ([1] * 20 + [64], list(range(900, 920)) + [2000])])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_error_of_each_row(rows, first, dtype):
+    """The last batch holds a wide tree beside single tokens."""
+    b = filled(610, rows, first, 2, 64)
+    q, qn = values(620, (b.total, 8, D), dtype, scale=1.2)
+    check(b, q, qn, dtype, trees(11, rows, 2), q_had_block=128)
+
+
+@pytest.mark.parametrize("rows,first", [([700], [0]), ([300, 1, 1, 90], [0, 500, 31, 1000])])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_causal_runs(rows, first, dtype):
+    """Prompts over the paged cache, alone and beside single tokens."""
+    b = filled(630, rows, first, 2, 64)
+    q, qn = values(640, (b.total, 8, D), dtype, scale=1.2)
+    check(b, q, qn, dtype, q_had_block=128)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", WIDTHS)
+@pytest.mark.parametrize("tokens", [2048, 2100])
+def test_rows_that_look_at_one_token_find_it(tokens, n, dtype):
+    """Each row's query points at one token, block after block: whatever run, stage or piece a block falls into, it is there."""
+    blocks = -(-tokens // 32)
+    R = -(-blocks // n)
+    b = filled(650, [n], [tokens], 2, 64, had=0)
+    b.table = np.repeat(b.table, R, 0)                                                # the same pages for every request
+    pages = qift.Kv4Pages(b.pages.pool, ints(b.table), 64)
+    K, V = qift.qift_kv4_paged_read(b.pages, ints([0, tokens]), ints([0]), tokens)
+    at = np.array([min(tokens - 1, 32 * (i % blocks) + 7 * i % 32) for i in range(R * n)])
+    q = (K[torch.from_numpy(at).cuda()].repeat_interleave(4, 1) * 3.0).to(DTYPES[dtype])
+    row_start, first = np.arange(R + 1) * n, [tokens] * R
+    got = qift.qift_kv4_paged_attention(q, pages, ints(row_start), ints(first))
+    want, limit = limits.attention(q.float().cpu().numpy(), b.pool(), b.table, 64, row_start, first, None, 0, None, dtype == "f32")
+    within(got, want, limit)
+    token = V[torch.from_numpy(at).cuda()].repeat_interleave(4, 1).cpu().numpy()
+    assert (np.linalg.norm(want - token, axis=-1) < 0.1 * np.linalg.norm(token, axis=-1)).mean() > 0.9       # the reference's own rows
+    ok()
+
+
 # ------------------------------------------------------------------------------------------------- clipping ratios
 def quantized(x, clip):
     """The definition, each step rounded to fp32 once; codes are clamped, however large the quotient."""

@@ -534,7 +534,8 @@ int qift_device_status(void* stream, uint32_t* detail);
  * status word and lets the kernel end normally; a product call whose kernel gave up has still returned
  * QIFT_OK (everything is asynchronous) and leaves Y unwritten -- qift_device_status is how a caller learns
  * of it.  This entry makes such a wait run out on purpose, with a short bound and without any fault:
- *   which = 0   one CTA waits for an mbarrier phase that nobody completes; site byte 0x7e
+ *   which = 0   one CTA waits for an mbarrier phase that nobody completes, twice (bounded by wall time, and by trips as
+ *               the tree attention's waits are); site byte 0x7e
  *   which = 1   the CTA-pair prefill GEMM on one 256 x 256 x 128 tile whose producers issue no loads (the
  *               operands are the library's built-in scratch and are never read): the wait for operands
  *               (site 32) and the waits for the accumulator (site 33) run out, all roles leave, tensor

@@ -1537,7 +1537,7 @@ int qift_device_status(void* stream, uint32_t* detail) {
 
 namespace qift {
 constexpr unsigned int kSiteProbe = 0x7e;
-// One thread waits, with the given bound, for a phase of an mbarrier that nobody completes.
+// One thread waits, with the given bound, for a phase of an mbarrier that nobody completes: in either form of a bounded wait.
 __global__ void wait_probe_kernel(uint64_t limit_ns) {
     __shared__ uint64_t bar;
     if (threadIdx.x == 0) {
@@ -1545,7 +1545,9 @@ __global__ void wait_probe_kernel(uint64_t limit_ns) {
         mbar_fence_init();
     }
     __syncthreads();
-    if (threadIdx.x == 0) mbar_wait(&bar, 0, kSiteProbe, limit_ns);
+    if (threadIdx.x != 0) return;
+    mbar_wait(&bar, 0, kSiteProbe, limit_ns);
+    mbar_wait_near(&bar, 0, kSiteProbe, static_cast<uint32_t>(limit_ns / kNearTripNs) + 1);
 }
 }  // namespace qift
 

@@ -604,6 +604,12 @@ def _on(t, dtype, *shape):
     return t.data_ptr()
 
 
+def _space(t):
+    """The address and size of a workspace: bytes that are all there (an expanded or strided tensor has fewer than it counts)."""
+    assert t.is_cuda and t.is_contiguous(), "expected a contiguous CUDA workspace"
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _same_device(t, *others):
     device = t.get_device()
     for o in others:
@@ -705,7 +711,7 @@ def qift_kv4_paged_attention(q, pages: Kv4Pages, row_start, first, mask=None, q_
     words = 0 if mask is None else mask.shape[1]
     _call(q, L.qift_kv4_paged_attention, q.data_ptr(), _float_type(q), qs, total, Hq, pages.H, D, q_had_block, scale,
           None if mask is None else _on(mask, torch.int32, total, words), words, *pages._batch(row_start, first),
-          _on(out, q.dtype, total, Hq, D), workspace.data_ptr(), workspace.numel() * workspace.element_size())
+          _on(out, q.dtype, total, Hq, D), *_space(workspace))
     return out
 
 
@@ -729,8 +735,7 @@ def qift_lora_linear(x, A, B, scaling, row_start, adapter, y=None, out=None, wor
     _same_device(x, A, B, scaling, row_start, adapter, y, out, workspace)
     _call(x, L.qift_lora_linear, _on(x, x.dtype), _float_type(x), _on(A, torch.bfloat16, n, rank, K), _on(B, torch.bfloat16, n, N, rank),
           _on(scaling, torch.float32, n), n, rank, M, N, K, _on(row_start, torch.int32, R + 1), _on(adapter, torch.int32, R), R,
-          None if y is None else _on(y, x.dtype, M, N), _on(out, x.dtype, M, N), workspace.data_ptr(),
-          workspace.numel() * workspace.element_size())
+          None if y is None else _on(y, x.dtype, M, N), _on(out, x.dtype, M, N), *_space(workspace))
     return out
 
 

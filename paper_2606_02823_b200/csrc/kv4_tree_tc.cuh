@@ -39,6 +39,9 @@ constexpr int kTtRing = 20;                  // blocks on their way to the conve
 constexpr int kTtScaleBytes = 2 * kTtUnit * 4 + 16;   // scales of keys and values; largest and smallest value scale of both blocks (0: no such block)
 constexpr int kTtStage = 8 * 4096;           // 4 KB of a softmax warp: query operands on their way in, results on their way out
 constexpr int kTtSmem = 1024 + 2 * kTtTiles * kTtTile + kTtRing * kPgBlock + 2 * kTtDepth * kTtScaleBytes + kTtStage + 2 * 128 * 4 + 768;
+// Binary orders between the value scales of an item up to which the largest stands for all in the bound on a row's weights.  The
+// largest weight is then 2^(6 - 12) at least, and fp16's smallest step, 2^-24, is still 2^-18 of it.
+constexpr float kTtAlike = 12.0f;
 constexpr uint32_t kTtS = 0, kTtO = 256, kTtQ = 384;   // tensor-memory columns: four S (the weights take the place of the first half), O, Q
 
 // D[tmem] (+)= A[tmem] * B[smem descriptor], fp16 operands, fp32 sums
@@ -59,10 +62,9 @@ __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.a
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ uint32_t tc_ld1(uint32_t taddr) {
-    uint32_t x;
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(x) : "r"(taddr) : "memory");
-    return x;
+__device__ __forceinline__ void tc_ld4(uint32_t taddr, uint32_t (&v)[4]) {   // and waits for it
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&v)[16]) {
     asm volatile(
@@ -263,7 +265,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                     const uint32_t sl = smem_u32(item_scales);
                     const uint4 info = lds128(sl + 2 * kTtUnit * 4);   // largest and smallest value scale of the two blocks (0: not there)
                     const float order = tree_order(__uint_as_float(max(info.x, info.y)));
-                    const bool alike = order - tree_order(__uint_as_float(min(info.z - 1, info.w - 1))) <= 4.0f;   // (a block that is not there: 0 - 1)
+                    const bool alike = order - tree_order(__uint_as_float(min(info.z - 1, info.w - 1))) <= kTtAlike;   // (a block that is not there: 0 - 1)
                     const bool plain = unit < min(q.first, q.len) / kTtUnit && info.z && info.w && alike;
                     auto weigh = [&](auto plain_tag) {        // scores -> weights
                         constexpr bool kPlain = decltype(plain_tag)::value;
@@ -307,9 +309,15 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                             if (!kPlain && !alike) {          // token by token, of those that are seen
                                 highest = -INFINITY;
 #pragma unroll 1
-                                for (int c = 0; c < kTtUnit; ++c) {   // (a short loop: as long code it slows the whole kernel, 258 -> 280 us)
-                                    const float score = __uint_as_float(tc_ld1(s_at + c)) * item_scales[c] * factor;
-                                    if ((c < 32 ? seen[0] : seen[1]) >> (c & 31) & 1) highest = fmaxf(highest, score + tree_order(item_scales[kTtUnit + c]));
+                                for (int c = 0; c < kTtUnit; c += 4) {   // (short code: 64 tokens at once slow the whole kernel, 258 -> 280 us)
+                                    uint32_t y[4];
+                                    tc_ld4(s_at + c, y);
+                                    const uint32_t on = (c < 32 ? seen[0] : seen[1]) >> (c & 31);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        const float score = __uint_as_float(y[e]) * item_scales[c + e] * factor;
+                                        if (on >> e & 1) highest = fmaxf(highest, score + tree_order(item_scales[kTtUnit + c + e]));
+                                    }
                                 }
                             }
                             if (highest > m_old + kTreeSlack) m = ceilf(highest);   // whole binary orders
@@ -491,13 +499,21 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                 const bool in = lane < tokens;
                 const float ksc = in ? reinterpret_cast<const float*>(src + kPgKs)[lane] : 0.0f;
                 float vsc = in ? reinterpret_cast<const float*>(src + kPgVs)[lane] : 0.0f;
-                if (vsc == 1.0f && src[kPgVz + lane] == 0) {   // a vector of zeros?  It adds nothing, and its scale says nothing
-                    uint32_t codes = 0;
+                const bool suspect = vsc == 1.0f && src[kPgVz + lane] == 0;   // a vector of zeros?  It adds nothing, and its scale says nothing
+                if (__any_sync(0xffffffffu, suspect)) {
+                    uint32_t codes = 0;      // of this lane's token: 16 bits (lane & 1) of word lane / 8 of all pieces with cq = lane / 2 % 4
 #pragma unroll 1
-                    for (int i = 0; i < 32; ++i) codes |= *reinterpret_cast<const uint16_t*>(src + kv_value_offset(lane, i >> 2, i & 3));
-                    if (codes == 0) vsc = 0.0f;
+                    for (int n = 0; n < 4; ++n) {
+                        uint32_t x = 0;
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) x |= *reinterpret_cast<const uint32_t*>(src + kPgV + w * 512 + piece + 4 * n);
+#pragma unroll
+                        for (int o = 1; o < 8; o <<= 1) x |= __shfl_xor_sync(0xffffffffu, x, o);
+                        x = __shfl_sync(0xffffffffu, x, (lane >> 1 & 3) * 8);
+                        if (lane >> 3 == n) codes = x >> (16 * (lane & 1)) & 0xffffu;
+                    }
+                    if (suspect && codes == 0) vsc = 0.0f;
                 }
-                __syncwarp();
                 reinterpret_cast<float*>(sl)[32 * blk + lane] = ksc;
                 reinterpret_cast<float*>(sl + kTtUnit * 4)[32 * blk + lane] = vsc;
                 const uint32_t bits = __float_as_uint(vsc);

@@ -79,6 +79,13 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// x * 2^d for whole d <= 0, in two steps: sums of weights go by reference points up to 212 binary orders apart (tokens whose values are
+// next to nothing beside the largest), and a factor below 2^-126 would be 0.  (Numerators of that size do vanish beside the others.)
+__device__ __forceinline__ float times_ex2(float x, float d) {
+    const float most = fmaxf(d, -100.0f);
+    return x * ex2(most) * ex2(d - most);
+}
+
 __device__ __forceinline__ uint32_t lessened(uint32_t x, uint32_t by) {   // fp16 pairs, x + by
     uint32_t y;
     asm("add.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(by));
@@ -519,10 +526,11 @@ kv4_tree_mma_kernel(const KvTreeParams p) {
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
                         const float to = fmaxf(ceilf(top), m_run[t][e]);
-                        const float corr = to > m_run[t][e] ? ex2(m_run[t][e] - to) : 1.0f;   // from -inf: 0
+                        const float d = to > m_run[t][e] ? m_run[t][e] - to : 0.0f, corr = ex2(d);   // from -inf: 0
                         m_run[t][e] = to;
                         if (b != b0) {    // (nothing to scale before the first block)
-                            l_run[t][e] *= corr, z[t][e] *= corr;
+                            l_run[t][e] = times_ex2(l_run[t][e], d);
+                            z[t][e] *= corr;
 #pragma unroll
                             for (int x = 0; x < 8; ++x) o[t][x][e] *= corr, o[t][x][2 + e] *= corr;
                         }
@@ -698,7 +706,7 @@ kv4_tree_join_kernel(const KvTreeParams p) {
                     const float to = fmaxf(m, t[i].x), a = ex2(m - to), c = ex2(t[i].x - to);
                     acc.x = fmaf(acc.x, a, x[i].x * c), acc.y = fmaf(acc.y, a, x[i].y * c);
                     acc.z = fmaf(acc.z, a, x[i].z * c), acc.w = fmaf(acc.w, a, x[i].w * c);
-                    l = fmaf(l, a, t[i].y * c), m = to;
+                    l = times_ex2(l, m - to) + times_ex2(t[i].y, t[i].x - to), m = to;
                 }
             }
         }
@@ -715,7 +723,7 @@ kv4_tree_join_kernel(const KvTreeParams p) {
                     const float to = fmaxf(m, t.x), a = ex2(m - to), c = ex2(t.x - to);
                     acc.x = fmaf(acc.x, a, x.x * c), acc.y = fmaf(acc.y, a, x.y * c);
                     acc.z = fmaf(acc.z, a, x.z * c), acc.w = fmaf(acc.w, a, x.w * c);
-                    l = fmaf(l, a, t.y * c), m = to;
+                    l = times_ex2(l, m - to) + times_ex2(t.y, t.x - to), m = to;
                 }
             }
         }

@@ -342,8 +342,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                             tc_wait_st();
                         }
                         if (__any_sync(0xffffffffu, m != l_m)) {
-                            const float corr = l_m > -INFINITY ? ex2(l_m - m) : 0.0f;
-                            l2 = __float_as_uint(sum2(l2) * corr);
+                            l2 = __float_as_uint(times_ex2(sum2(l2), m != l_m ? l_m - m : 0.0f));
                             l_m = m;
                         }
                         // ---- weights
@@ -402,7 +401,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                 if (ok) ok = mbar_wait_near(&mark_full[((n - 1) & 1) * 4 + quarter], ((n - 1) >> 1) & 1, kTreeSite + 12);
                 m = marks[((n - 1) & 1) * 128 + row];
                 float l = sum2(l2);  // without a reference point: 0, or no number when no score was one
-                if (l_m > -INFINITY) l *= ex2(l_m - m);
+                if (l_m > -INFINITY) l = times_ex2(l, l_m - m);
                 meet();              // the reference points have been read by both
                 marks[turn * 128 + row] = l;
                 meet();

@@ -231,3 +231,21 @@ def test_quotients_beyond_32_bit_integers(clip):
     packed = code[:, 0, 0::2] | code[:, 0, 1::2] << 4
     assert np.array_equal(one.codes.cpu().numpy()[0], packed) and np.array_equal(one.scale.cpu().numpy()[0], s[:, 0])
     ok()
+
+
+# ------------------------------------------------------------------------------------------------- scales all over
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", WIDTHS)
+@pytest.mark.parametrize("orders", [3, 6, 12, 40])
+def test_scales_that_differ_from_token_to_token(orders, n, dtype):
+    """Values of 2^-orders to 2^orders side by side, vectors of zeros among them."""
+    rows, first = [n, n], [700, 1300]
+    b = Batch(720, rows, first, 2, 64)
+    cut = np.concatenate([[0], np.cumsum([f + n for f in first])])
+    k = values(721, (int(cut[-1]), 2, D), "f32", 0.1)[0]
+    v = values(722, (int(cut[-1]), 2, D), "f32")[0]
+    u = torch.from_numpy(np.random.default_rng(5).random((int(cut[-1]), 2, 1)).astype(np.float32)).cuda()
+    v *= torch.exp2((2 * u - 1) * orders) * (u > 0.1)
+    qift.qift_kv4_paged_write(k, v, b.pages, ints(cut), ints([0, 0]))
+    q, qn = values(723, (2 * n, 8, D), dtype)
+    check(b, q, qn, dtype, trees(13, rows, 2))

@@ -261,8 +261,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                              mbar_wait_near(&scale_full[i % (2 * kTtDepth)], (i / (2 * kTtDepth)) & 1, kTreeSite + 2);
                 tc_fence_after();
                 if (active) {
-                    const float* item_scales = reinterpret_cast<const float*>(scales + (i % (2 * kTtDepth)) * kTtScaleBytes);
-                    const uint32_t sl = smem_u32(item_scales);
+                    const uint32_t sl = smem_u32(scales + (i % (2 * kTtDepth)) * kTtScaleBytes);
                     const uint4 info = lds128(sl + 2 * kTtUnit * 4);   // largest and smallest value scale of the two blocks (0: not there)
                     const float order = tree_order(__uint_as_float(max(info.x, info.y)));
                     const bool alike = order - tree_order(__uint_as_float(min(info.z - 1, info.w - 1))) <= kTtAlike;   // (a block that is not there: 0 - 1)
@@ -273,8 +272,9 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                         tc_ld32(s_at, x[0]);
                         tc_ld32(s_at + 32, x[1]);
                         if (!kPlain) {
-                            seen[0] = have && info.z ? tree_seen(p, begin + token, token, 2 * unit, q.first, q.len) : 0u;
-                            seen[1] = have && info.w ? tree_seen(p, begin + token, token, 2 * unit + 1, q.first, q.len) : 0u;
+                            const bool context = unit < min(q.first, q.len) / kTtUnit;
+                            seen[0] = !have || !info.z ? 0u : context ? 0xffffffffu : tree_seen(p, begin + token, token, 2 * unit, q.first, q.len);
+                            seen[1] = !have || !info.w ? 0u : context ? 0xffffffffu : tree_seen(p, begin + token, token, 2 * unit + 1, q.first, q.len);
                         }
                         tc_wait_ld();
                         // ---- the largest score
@@ -313,11 +313,12 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                                     uint32_t y[4];
                                     tc_ld4(s_at + c, y);
                                     const uint32_t on = (c < 32 ? seen[0] : seen[1]) >> (c & 31);
+                                    const uint4 k4 = lds128(sl + 4 * c), v4 = lds128(sl + 4 * (kTtUnit + c));
+                                    const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w}, v[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        const float score = __uint_as_float(y[e]) * item_scales[c + e] * factor;
-                                        if (on >> e & 1) highest = fmaxf(highest, score + tree_order(item_scales[kTtUnit + c + e]));
-                                    }
+                                    for (int e = 0; e < 4; ++e)
+                                        if (on >> e & 1)
+                                            highest = fmaxf(highest, fmaf(__uint_as_float(y[e]) * __uint_as_float(k[e]), factor, tree_order(__uint_as_float(v[e]))));
                                 }
                             }
                             if (highest > m_old + kTreeSlack) m = ceilf(highest);   // whole binary orders
@@ -517,7 +518,7 @@ kv4_tree_tc_kernel(const KvTreeParams p) {
                 reinterpret_cast<float*>(sl + kTtUnit * 4)[32 * blk + lane] = vsc;
                 const uint32_t bits = __float_as_uint(vsc);
                 const bool counts = bits - 1u < 0x7f7fffffu;   // finite, not 0
-                const uint32_t top = __reduce_max_sync(0xffffffffu, counts ? bits : 0u), least = __reduce_min_sync(0xffffffffu, counts ? bits : 0x7f7fffffu);
+                const uint32_t top = __reduce_max_sync(0xffffffffu, counts ? bits : 0u), least = __reduce_min_sync(0xffffffffu, counts ? bits : in ? 1u : 0x7f7fffffu);   // (nothing: unlike any)
                 uint32_t* info = reinterpret_cast<uint32_t*>(sl + 2 * kTtUnit * 4);
                 if (lane == 0) info[blk] = top, info[2 + blk] = have ? least : 0u;
                 fence_async_smem();

@@ -249,3 +249,22 @@ def test_scales_that_differ_from_token_to_token(orders, n, dtype):
     qift.qift_kv4_paged_write(k, v, b.pages, ints(cut), ints([0, 0]))
     q, qn = values(723, (2 * n, 8, D), dtype)
     check(b, q, qn, dtype, trees(13, rows, 2))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", WIDTHS)
+@pytest.mark.parametrize("strength", [1.0, 2.0, 3.0])
+def test_zero_vectors_that_take_the_weight(strength, n, dtype):
+    """A row looks at tokens whose values are zeros; its result is what little the others have left (about e^-11, -23, -34 of them)."""
+    rows, first = [n, n], [200, 1300]
+    b = Batch(730, rows, first, 2, 64)
+    cut = np.concatenate([[0], np.cumsum([f + n for f in first])])
+    k = values(731, (int(cut[-1]), 2, D), "f32", scale=0.3)[0]
+    v = values(732, (int(cut[-1]), 2, D), "f32")[0]
+    w = torch.ones(D, device="cuda")
+    w[::2] = -1.0
+    for at in (0, 70, int(cut[1]), int(cut[1]) + 640, int(cut[1]) + 1299):
+        k[at], v[at] = w, 0.0
+    qift.qift_kv4_paged_write(k, v, b.pages, ints(cut), ints([0, 0]))
+    q = (values(733, (2 * n, 8, D), "f32", scale=0.3)[0] + strength * w).to(DTYPES[dtype])
+    check(b, q, q.float().cpu().numpy(), dtype)

@@ -151,6 +151,16 @@ def test_error_of_each_row(rows, first, dtype):
     check(b, q, qn, dtype, trees(11, rows, 2), q_had_block=128)
 
 
+@pytest.mark.parametrize("Hq,H", [(64, 1), (66, 2), (5, 1)])
+@pytest.mark.parametrize("rows,first", [([1], [300]), ([1, 1, 3], [0, 2000, 65])])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_query_heads_and_odd_numbers_of_them(rows, first, Hq, H, dtype):
+    """Also single tokens reach the widest tiles: 64 query heads a KV head."""
+    b = filled(625, rows, first, H, 32, pad_rows=1)
+    q, qn = values(626, (b.total, Hq, D), dtype, scale=1.2)
+    check(b, q, qn, dtype, q_had_block=128)
+
+
 @pytest.mark.parametrize("rows,first", [([700], [0]), ([300, 1, 1, 90], [0, 500, 31, 1000])])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_causal_runs(rows, first, dtype):

@@ -29,11 +29,12 @@ def compare(x, A, B, rows, limit):
     assert abs(bias) <= limit and whole <= limit, (bias, whole, limit)
 
 
-# A matrix instruction cuts up to 2^-23 off the sum that it adds to.  A step of 32 k (16 ranks) is six (three) of them on a sum of its own,
-# which then joins the others by a rounded addition; those, about K / 32 of them in a row, are off by 2^-24 / sqrt(3) each, without a common
-# direction: sqrt(K / 32 / 3) 2^-24 of the largest sum.  Rows of positive numbers have all their sums grow.
+# A matrix instruction cuts up to 2^-23 off the sum that it adds to.  A step of 32 k is six of them on a sum of its own, which then joins the
+# others by a rounded addition; those, about K / 32 of them in a row, are off by 2^-24 / sqrt(3) each, without a common direction:
+# sqrt(K / 32 / 3) 2^-24 of the largest sum.  16 ranks are three on one sum that runs through all of them: it grows evenly, to 9/16 of the
+# result on average, and half of 2^-23 of it is cut off on average.  Rows of positive numbers have all their sums grow.
 def bound(K, rank):
-    return (6 + 3) * 2.0 ** -23 + 2.0 ** -24 * (np.sqrt(K / 96) + np.sqrt(rank / 48) + 2)
+    return 6 * 2.0 ** -23 + 2.0 ** -24 * (np.sqrt(K / 96) + 2) + 3 * (rank / 16) * 2.0 ** -24 * 9 / 16
 
 
 # 16-row items with K split and unsplit, 128-row items with K split and unsplit
@@ -55,3 +56,13 @@ def test_sums_over_the_rank(rows, rank, positive):
     if positive:
         x, A, B = x.abs(), A.abs(), B.abs()
     compare(x, A, B, rows, bound(32, rank))
+
+
+@pytest.mark.parametrize("rows", [[1] * 20, [200]])
+def test_the_sum_over_ranks_alone(rows):
+    """A x is exact here (one bf16 value of x a row): two bf16 parts, the third is zero, so 16 instructions cut off the sum over 128 ranks."""
+    rank, M = 128, sum(rows)
+    x = torch.zeros((M, 16), device="cuda")
+    x[torch.arange(M), torch.arange(M) % 16] = normal(720, (M,)).bfloat16().float().abs()
+    A, B = normal(721, (rank, 16)).bfloat16().abs(), normal(722, (512, rank)).bfloat16().abs()
+    compare(x, A, B, rows, 16 * 2.0 ** -24 * 9 / 16 + 2.0 ** -24)

@@ -447,7 +447,10 @@ int qift_kv4_attention_decode(const float* q, const uint8_t* k_codes, const floa
  *   workspace   >= qift_kv4_paged_attention_workspace_bytes(total, R, Hq, H) bytes.  It may be shared by calls that follow
  *               one another in a stream, captured or not, and needs no initial contents
  *   fp32 calls keep fp32 accuracy; bf16 calls hold the rotated query and the weights in 16 bits (fp16) beside exact codes,
- *   with fp32 scores, sums and results.
+ *   with fp32 scores, sums and results.  This holds for value scales from 2^-86 to 2^108 (values of about 1e-25 to 1e33), however
+ *   they differ from token to token; smaller and larger ones lose bits.  What a row does not see has no influence on it.  A
+ *   query row with a NaN or an infinity gives NaN, and so does a row that sees a token in whose key or value an infinity was
+ *   written (a NaN is written as 0).
  * Errors: INVALID_ARG (null pointer, sizes <= 0, mask_words, scale, clip_ratio, dtype), UNSUPPORTED_SHAPE (D != 128, page_tokens,
  * had_block, Hq / H, strides), ALIGNMENT (arrays of codes and rows 16 bytes, int32 arrays 4), WORKSPACE, CUDA. */
 size_t qift_kv4_page_bytes(int page_tokens, int H, int D);
@@ -477,7 +480,8 @@ int qift_kv4_paged_attention(const void* q, int q_dtype, long long q_stride, int
  *   y           in  [M][N], or NULL for zeros;  out [M][N], may be y itself; both of X's type
  *   workspace   >= qift_lora_workspace_bytes(M, rank, K) bytes, as for the attention
  * Sums in fp32.  fp32 rows are multiplied in three bf16 parts (2^-25 of a value is lost); the small product A x is kept in fp32 and
- * multiplied in three such parts for fp32 results, in two (2^-17) for bf16 ones.
+ * multiplied in three such parts for fp32 results, in two (2^-17) for bf16 ones.  A row with an infinite x or A x (beyond bf16's range,
+ * 3.39e38), or a NaN, has results that are no numbers; the other rows are not touched by it.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (M, K, N, rank), ALIGNMENT, WORKSPACE, CUDA. */
 size_t qift_lora_workspace_bytes(int M, int rank, int K);
 int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16_t* B, const float* scaling, int adapters, int rank,

@@ -305,8 +305,8 @@ __device__ __forceinline__ int kv_find_block(const KvMoveParams& p, int& lo, int
 // Rows -> codes.  Groups of eight lanes take vectors (head, token; all keys, then all values).  Blocks are put together in shared
 // memory: a whole one leaves in 16-byte stores, of a part the keys leave in 16 bytes, the values in pairs of tokens (4 bytes) or
 // alone (2).  One or two tokens go straight to their places.
-// Bound by instruction issue (68 % of the slots; about 455 warp instructions for four vectors, most of them the rotation and the
-// quantizer): 9873 tokens x 8 heads, bf16, written and read back, 103 MB in all: 46 us.
+// Bound by instruction issue (68 % of the slots; about 459 warp instructions for four vectors, most of them the rotation and the
+// quantizer): 9873 tokens x 8 heads, bf16: 28 us, 46 with the read of them (103 MB in all).
 template <bool BF16>
 __global__ void __launch_bounds__(kPgThreads)
 kv4_paged_write_kernel(const KvMoveParams p) {
@@ -400,7 +400,8 @@ kv4_paged_write_kernel(const KvMoveParams p) {
 }
 
 // Codes -> rows: scale * (code - zero), rotated back on request.
-// 3339 tokens x 32 heads, fp32 (124 MB, most of it written): 36 us, 3.4 TB/s.
+// 3339 tokens x 32 heads, fp32 (124 MB, most of it written): 36 us, 3.5 TB/s, 64 % of the L1 and shared-memory path (the 16-bit reads of
+// value codes; warps wait for its queue more than for anything else) and 41 % of the issue slots.
 template <bool BF16>
 __global__ void __launch_bounds__(kPgThreads)
 kv4_paged_read_kernel(const KvMoveParams p) {
@@ -461,7 +462,8 @@ kv4_paged_read_kernel(const KvMoveParams p) {
 // Slot first + i <- slot first + keep[i], i = 0 .. kept - 1: one warp per request and head, eight tokens read before any of them
 // is written.  The indices ascend, so a slot is never written before the tokens that come from it are read, and a lane only ever
 // reads and writes its own share of every token.
-// Bound by its chain of dependent loads (request, indices, pages, tokens), about 2 us each when they come from memory.
+// Bound by its chain of dependent loads (request, indices, pages, tokens), once for every eight tokens: 4 requests of up to 12 drafted
+// tokens 6.1 us, 192 of up to 64 16 us.
 constexpr int kPgKeepAhead = 8;
 __global__ void __launch_bounds__(kPgThreads)
 kv4_paged_keep_kernel(const KvPages pages, const KvRows rows, const int32_t* __restrict__ keep, const int32_t* __restrict__ kept_start) {

@@ -21,9 +21,9 @@
 //   w = 2^(score - R) vs, and the sum of 2^(score - R) beside it, go by one reference point R for each row: a bound of score + log2(vs)
 //   over the tokens that the row has seen, so a large value scale counts with its weight, and for the rows that see it alone.  R
 //   moves (by whole binary orders, so nothing is rounded) only when a token exceeds it by more than kTreeSlack.
-// Bound by instruction issue and the latency that 16 (12) warps an SM leave: about 515 warp instructions a block with eight rows, 530
-// with sixteen.  32 query and 8 KV heads: 64 single tokens over 8000 cached ones each (286 MB) 64 us = 4.5 TB/s; 16 trees of up to 13
-// tokens over 6000 (67 MB, read again by every tile) 68 us.
+// Bound by latency and instruction issue: about 507 warp instructions a block with eight rows, 722 with sixteen, on 59 and 44 % of the
+// issue slots, which is what 16 and 12 warps an SM (128 and 168 registers a thread) keep busy.  32 query and 8 KV heads: 64 single tokens
+// over 8000 cached ones each (286 MB) 62.5 us = 4.6 TB/s; 16 trees of up to 13 tokens over 6000 (67 MB, read again by every tile) 67 us.
 #pragma once
 
 #include <type_traits>

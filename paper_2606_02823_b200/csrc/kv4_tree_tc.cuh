@@ -19,7 +19,8 @@
 // What bounds it, per item: the tensor cores (8 instructions of 32 cycles, 4 of 64), the exponentials (128 rows x 64 at 16 a cycle) and
 // shared memory (32 KB of tiles written, 32 KB read) each take about 512 cycles.
 // Measured it is the hand-overs between the roles: about 1700 cycles an item, and 20000 a tile for its query, its results and the refill.
-// 8 trees of 64 tokens over 32000, 32 query and 8 KV heads: 254 us (85 at the tensor cores' rate); 16-row tiles of mma.sync 611.
+// 8 trees of 64 tokens over up to 32000, 32 query and 8 KV heads: 260 us (85 at the tensor cores' rate).  Value scales more than 2^12
+// apart within 64 tokens take longer (2^-8 to 2^8 487 us), vectors of zeros too (a fifth of the tokens 359 us).
 #pragma once
 
 #include "kv4_tree.cuh"

@@ -9,8 +9,9 @@
 //   lora_down_wide_kernel, lora_up_wide_kernel   longer ones: up to 128 rows, 16 per warp; the adapter's rows, which all warps need, are
 //                                                staged in shared memory three steps deep (read by every warp through L1 instead, the
 //                                                second kernel took 147 us for 3259 rows, rank 64, N = 14336)
-// fp32 rows enter in three bf16 parts (exact to 2^-25), t in two beside bf16 results (2^-17 of t, next to a result rounded at 2^-9)
-// and in three beside fp32 ones.
+// fp32 rows enter in three bf16 parts (exact to 2^-25; an infinite value leaves NaN parts, its row no numbers), t in two beside bf16 results
+// (2^-17 of t, next to a result rounded at 2^-9) and in three beside fp32 ones.  fp32 results over K = 11008 are within 3.4e-7 of 64 bits.
+// 7 requests of up to 11 fp32 rows, rank 24, 4096 -> 1024: 9.9 us; 5 of up to 800, rank 64, 4096 -> 4096: 86 us.
 #pragma once
 
 #include "common.cuh"

@@ -1734,8 +1734,10 @@ int run_move(Kernel f32, Kernel bf16, int x_dtype, const KvMoveParams& p, cudaSt
 }
 // Attention of trees: rows of a tile, by the mean of a request's rows for one KV head.  8 and 16: kv4_tree.cuh, 128: the tcgen05 kernel
 // of kv4_tree_tc.cuh (bf16 calls), whose cost does not depend on the rows of a tile.  32 query and 8 KV heads, 16- and 128-row tiles:
-// 48 rows: 16 requests over 6000 cached tokens 83 and 86 us, 64 over 1000 118 and 145, 4 over 30000 106 and 89; 64 rows: 101 and 100,
-// 142 and 153, 127 and 90.
+// 48 rows: 16 requests over 6000 cached tokens 89 and 100 us, 64 over 1000 104 and 134, 4 over 30000 101 and 87; 64 rows: 118 and 103,
+// 134 and 129, 120 and 88.  The lengths of single requests are on the device, so a mixed batch goes by its mean, too: one of 256 rows
+// beside 64 of 4 (single tokens) over 4000: 82 us in 8-row tiles as chosen, 247 in 128-row ones; a run of 2000 tokens from nothing beside
+// them 570 in 128-row tiles as chosen, 534 in 16-row ones.
 inline int tree_rows(int total, int R, int G, bool bf16) {
     const long long mean = (static_cast<long long>(total) * G + R - 1) / R;
     return mean <= 8 || !bf16 ? 8 : mean <= 48 ? 16 : kTtRows;
@@ -1918,8 +1920,8 @@ int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     // Items of 128 rows from 32 rows a request on, of 2048 / rank where that is more: below, 16-row items are faster, above, their
     // reading of the adapter again for every 16 rows costs more (16 requests, 4096 -> 4096, bf16, 16- and 128-row items: rank 16, 64
-    // rows 13 and 15 us, 256 rows 40 and 32; rank 32, 32 rows 17 and 21, 128 rows 43 and 28; rank 64, 16 rows 18 and 23, 48 rows 33 and
-    // 26; rank 128, 32 rows 48 and 46, 64 rows 64 and 49)
+    // rows 13 and 15 us, 256 rows 40 and 32; rank 32, 32 rows 17 and 21, 128 rows 35 and 28; rank 64, 16 rows 17 and 22, 48 rows 31 and
+    // 25; rank 128, 32 rows 45 and 46, 64 rows 64 and 49).  By the mean of the requests: 500 rows beside 60 single ones, rank 16, 13 and 30
     const bool wide = M > 32ll * R && static_cast<long long>(M) * rank > 2048ll * R;
     return x_dtype == QIFT_BF16 ? (wide ? run_lora_rank<true, true>(p, st) : run_lora_rank<true, false>(p, st))
                                 : (wide ? run_lora_rank<false, true>(p, st) : run_lora_rank<false, false>(p, st));

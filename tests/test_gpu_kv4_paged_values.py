@@ -128,7 +128,7 @@ def test_zero_vectors_among_small_values(size, n, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", WIDTHS)
-@pytest.mark.parametrize("size", [1e24, 1e-24])
+@pytest.mark.parametrize("size", [1e24, 1e-24, 1e32, 3e-25])
 def test_values_of_any_size(size, n, dtype):
     rows, first = [n, n], [200, 1300]
     b = Batch(600, rows, first, 2, 64)

@@ -488,6 +488,79 @@ int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16
                      int M, int N, int K, const int32_t* row_start, const int32_t* adapter, int R, const void* y, void* out,
                      void* workspace, size_t workspace_bytes, void* stream);
 
+/* Page tables kept on the device: what a step of many requests needs before the four calls above, made from the requests' lengths
+ * in stream order, so that a captured step goes on from page to page by itself.  Free pages are a stack, free_pages [num_pages] int32 with
+ * free_count [1] int32 of them in use (counts outside 0 .. num_pages are taken as the nearest of these).
+ *
+ * qift_kv4_pages_begin: rows[r] new tokens of each request behind its first[r] cached ones.
+ *   rows        in  [R] int32 (negative: none);  first  in  [R] int32
+ *   page_table  in/out [R][max_pages]: of the entries of positions first .. first + rows - 1 those that are no page of the pool take
+ *               one from the stack, request by request and in ascending order; pages that are there stay (left of an earlier draft, or
+ *               shared).  When the stack is empty, or what it holds is no page, the entry becomes -1.  A second call with the same arguments fills
+ *               in what was missing.
+ *   row_start   out [R + 1]: the sums of rows, none beyond `total`: rows that do not fit are cut off, the last requests' first
+ *   position    out [total] int32: the position of each row for its rotation, first + i; with a mask (as for the attention: a token's
+ *               ancestors and itself) first + bits - 1, its depth in the drafted tree.  Rows of nobody, and positions before 0, -1;
+ *               beyond 2^31 - 1, that
+ *   slot        out [total] int64, or NULL: page * page_tokens + offset of the place that the row's token has in the pool, -1 without one
+ *   lost        out [1] int32: of all rows asked for, those without a place: cut off, without a page, at positions before 0 or from
+ *               max_pages * page_tokens on
+ *
+ * qift_kv4_pages_end: length[r] tokens of each request stay (0: it has ended).  The pages behind them, entries from
+ * ceil(length / page_tokens) on, go back to the stack and the entries become -1.
+ *   shared      in  [R] int32, or NULL: entries before shared[r] are not given back (a prefix that others hold, too)
+ * The first page given back, request by request in ascending order, ends on top: a begin that is taken back leaves the stack as it was.
+ * A page that two entries hold goes back twice unless `shared` says otherwise; what would not fit on the stack is dropped.
+ * Both: int32 arrays 4-byte aligned, slot 8.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_tokens, mask_words, R * max_pages >= 2^31),
+ * ALIGNMENT, CUDA. */
+int qift_kv4_pages_begin(const int32_t* rows, const int32_t* first, int R, int32_t* page_table, int max_pages, int num_pages,
+                         int page_tokens, int32_t* free_pages, int32_t* free_count, const int32_t* mask, int mask_words, int total,
+                         int32_t* row_start, int32_t* position, int64_t* slot, int32_t* lost, void* stream);
+int qift_kv4_pages_end(const int32_t* length, const int32_t* shared, int R, int32_t* page_table, int max_pages, int num_pages,
+                       int page_tokens, int32_t* free_pages, int32_t* free_count, void* stream);
+
+/* Norms of queries and keys for each head and their rotation by position, in one pass over the rows of a projection:
+ *     y = x / sqrt(mean(x^2) + eps) * weight   over the D dimensions of a head, where a weight is given
+ *     (a, b) <- (a cos t - b sin t, b cos t + a sin t),  t = position * inv_freq[i],   for the pairs of the first rot dimensions
+ *   Q, K        in  [total][Hq][D] and [total][H][D] fp32 or bf16, rows q_stride / k_stride elements apart (>= heads * D, whole 16-byte units)
+ *   q_weight, k_weight   in  [D] of the rows' type, or NULL: no norm
+ *   eps         > 0 and finite
+ *   inv_freq    in  fp32 [rot / 2];  rot a multiple of 16, 16 .. D;  D a multiple of 16, up to 512
+ *   pairs       QIFT_ROPE_HALVES: (i, i + rot / 2), QIFT_ROPE_NEIGHBOURS: (2i, 2i + 1)
+ *   position    in  [total] int32; rows with a negative one belong to nobody: nothing of them is read or written
+ *   Q_out, K_out  out, of Q's and K's shape and type, strides as above; each may be its input with the same stride, and shares no memory
+ *               with the inputs otherwise
+ * fp32 arithmetic, angles in fp64 until their whole turns are gone, one rounding to bf16.  Squares are summed in fp32: they must not
+ * overflow there (heads whose values reach 1e18 do).
+ * Errors: INVALID_ARG (null pointer, sizes <= 0, eps, pairs, dtype), UNSUPPORTED_SHAPE (D, rot, strides, Hq + H > 65535), ALIGNMENT (rows
+ * and weights 16 bytes, the others 4), CUDA. */
+enum { QIFT_ROPE_HALVES = 0, QIFT_ROPE_NEIGHBOURS = 1 };
+int qift_qk_norm_rope(const void* Q, const void* K, int x_dtype, long long q_stride, long long k_stride, int total, int Hq, int H, int D,
+                      const void* q_weight, const void* k_weight, float eps, const float* inv_freq, int rot, int pairs,
+                      const int32_t* position, void* Q_out, void* K_out, long long q_out_stride, long long k_out_stride, void* stream);
+
+/* The gated half of a feed-forward block: both products of one quantized activation, the activation function and their product,
+ *     h[m,n] = act(g[m,n]) * u[m,n],   g and u the results that qift_linear_multi would give for the two outputs in fp32
+ *   gate_up     HOST array of two outputs with the same N: packed / s_n of the gate's and of the other projection; acc_debug dev int32
+ *               [M,N] or NULL; Y is not used
+ *   activation  QIFT_ACT_SILU: g / (1 + exp(-g)); QIFT_ACT_GELU_TANH: g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2
+ *   H           out [M,N] fp32 or bf16 (rounded once)
+ *   levels_buf  dev, >= qift_levels_bytes(K, gate_up, 2), 256-byte aligned; needed from qift_gated_levels_min_rows() token rows on
+ *               when K % 16 == 0.  levels_ready, ahead: as for qift_linear_multi / qift_forward_multi, in whose chains the call can stand
+ * qift_gated_forward takes the activation itself, X [M,K], and rotates and quantizes it first (qift_quantize_act);
+ *   scratch     dev, >= qift_gated_forward_scratch_bytes(M, K), 256-byte aligned: q_a and s_a
+ * No other workspace.  The sums are exact: h follows from the accumulators in fp32, and does not depend on the route.
+ * Errors: INVALID_ARG (null pointers, different N, enums, ahead), UNSUPPORTED_SHAPE, ALIGNMENT, WORKSPACE, CUDA. */
+typedef enum { QIFT_ACT_SILU = 0, QIFT_ACT_GELU_TANH = 1 } qift_activation;
+int qift_gated_levels_min_rows(void);
+int qift_gated_linear(const int8_t* q_a, const float* s_a, int M, int K, int levels, const qift_linear_output* gate_up, int activation,
+                      void* H, int h_dtype, void* levels_buf, size_t levels_bytes, int levels_ready, const qift_decode_ahead* ahead,
+                      void* stream);
+size_t qift_gated_forward_scratch_bytes(int M, int K);
+int qift_gated_forward(const void* X, int x_dtype, int M, int K, int had_block, float clip_ratio, int levels,
+                       const qift_linear_output* gate_up, int activation, void* H, int h_dtype, void* scratch, size_t scratch_bytes,
+                       void* levels_buf, size_t levels_bytes, int levels_ready, const qift_decode_ahead* ahead, void* stream);
+
 /* Quantizer diagnostics (not on the inference path).  Sec. 3.3 (list of evaluated grids), Sec. 4.5.1
  * (bucket diagnostic), Sec. 4.5.2 (scale-invariant ratio scan).
  *

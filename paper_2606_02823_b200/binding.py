@@ -22,6 +22,8 @@ F32, BF16 = 0, 1
 ROUTE_AUTO, ROUTE_GENERIC, ROUTE_DECODE, ROUTE_PREFILL, ROUTE_PREFILL_SCRATCH, ROUTE_PREFILL_PAIR = 0, 1, 2, 3, 4, 5
 ROUTE_PREFILL_FUSED_PAIR = 6
 ROUTE_DECODE_ROWS = 7
+ROPE_HALVES, ROPE_NEIGHBOURS = 0, 1
+ACT_SILU, ACT_GELU_TANH = 0, 1
 
 EXPORTS = [
     "qift_status_string", "qift_packed_bytes", "qift_workspace_bytes", "qift_workspace_bytes_route", "qift_pack_weights",
@@ -32,6 +34,8 @@ EXPORTS = [
     "qift_kv4_quantize", "qift_kv4_attention_workspace_bytes", "qift_kv4_attention_decode",
     "qift_kv4_page_bytes", "qift_kv4_paged_write", "qift_kv4_paged_read", "qift_kv4_paged_keep",
     "qift_kv4_paged_attention_workspace_bytes", "qift_kv4_paged_attention", "qift_lora_workspace_bytes", "qift_lora_linear",
+    "qift_kv4_pages_begin", "qift_kv4_pages_end", "qift_qk_norm_rope",
+    "qift_gated_levels_min_rows", "qift_gated_linear", "qift_gated_forward_scratch_bytes", "qift_gated_forward",
     "qift_expand_weights", "qift_expanded_linear",
     "qift_diag_grid_quantize", "qift_diag_bucket_stats", "qift_diag_ratio_scan_workspace_bytes", "qift_diag_ratio_scan",
     "qift_selftest_wait_timeout", "qift_levels_bytes", "qift_forward_multi_scratch_bytes", "qift_forward_multi",
@@ -107,6 +111,16 @@ def lib() -> ctypes.CDLL:
         L.qift_lora_workspace_bytes.restype = sz
         L.qift_lora_workspace_bytes.argtypes = [ci, ci, ci]
         L.qift_lora_linear.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, ci, vp, vp, vp, sz, vp]
+        tables = [vp, ci, ci, ci, vp, vp]          # page_table, max_pages, num_pages, page_tokens, free_pages, free_count
+        L.qift_kv4_pages_begin.argtypes = [vp, vp, ci] + tables + [vp, ci, ci, vp, vp, vp, vp, vp]
+        L.qift_kv4_pages_end.argtypes = [vp, vp, ci] + tables + [vp]
+        L.qift_qk_norm_rope.argtypes = [vp, vp, ci, ll, ll, ci, ci, ci, ci, vp, vp, cf, vp, ci, ci, vp, vp, vp, ll, ll, vp]
+        L.qift_gated_levels_min_rows.argtypes = []
+        levels_args = [vp, sz, ci, vp, vp]         # levels_buf, levels_bytes, levels_ready, ahead, stream
+        L.qift_gated_linear.argtypes = [vp, vp, ci, ci, ci, vp, ci, vp, ci] + levels_args
+        L.qift_gated_forward_scratch_bytes.restype = sz
+        L.qift_gated_forward_scratch_bytes.argtypes = [ci, ci]
+        L.qift_gated_forward.argtypes = [vp, ci, ci, ci, ci, cf, ci, vp, ci, vp, ci, vp, sz] + levels_args
         L.qift_diag_grid_quantize.argtypes = [vp, ci, ci, vp, ci, vp, vp, vp]
         L.qift_diag_bucket_stats.argtypes = [vp, vp, ci, ci, vp, vp, ci, vp, vp, vp]
         L.qift_diag_ratio_scan_workspace_bytes.restype = sz
@@ -128,7 +142,7 @@ def lib() -> ctypes.CDLL:
                             "qift_forward_scratch_bytes", "qift_group_plan_bytes", "qift_static_scratch_bytes",
                             "qift_workspace_bytes_route", "qift_kv4_attention_workspace_bytes", "qift_levels_bytes",
                             "qift_kv4_page_bytes", "qift_kv4_paged_attention_workspace_bytes", "qift_lora_workspace_bytes",
-                            "qift_forward_multi_scratch_bytes", "qift_linear_multi_workspace_bytes"):
+                            "qift_forward_multi_scratch_bytes", "qift_linear_multi_workspace_bytes", "qift_gated_forward_scratch_bytes"):
                 getattr(L, name).restype = ci
         _lib = L
     return _lib
@@ -737,6 +751,132 @@ def qift_lora_linear(x, A, B, scaling, row_start, adapter, y=None, out=None, wor
           _on(scaling, torch.float32, n), n, rank, M, N, K, _on(row_start, torch.int32, R + 1), _on(adapter, torch.int32, R), R,
           None if y is None else _on(y, x.dtype, M, N), _on(out, x.dtype, M, N), *_space(workspace))
     return out
+
+
+# ---------------------------------------------------------------------------------------- page tables of many requests
+class Kv4FreePages:
+    """The stack of free pages of a pool: pages int32 [num_pages], of which the first count[0] are free."""
+
+    def __init__(self, pages, count):
+        _on(pages, torch.int32), _on(count, torch.int32, 1)
+        _same_device(pages, count)
+        self.pages, self.count = pages, count
+
+    @classmethod
+    def all_of(cls, num_pages: int, device="cuda"):
+        """Every page is free; page 0 is taken first."""
+        return cls(torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device), torch.full((1,), num_pages, dtype=torch.int32, device=device))
+
+
+class Kv4Rows:
+    """What qift_kv4_pages_begin makes of a step's rows: row_start int32 [R + 1], position int32 [total], slot int64 [total], lost int32 [1]."""
+
+    def __init__(self, row_start, position, slot, lost):
+        self.row_start, self.position, self.slot, self.lost = row_start, position, slot, lost
+
+    @classmethod
+    def empty(cls, R: int, total: int, device="cuda"):
+        new = lambda n, t: torch.empty(n, dtype=t, device=device)  # noqa: E731
+        return cls(new(R + 1, torch.int32), new(total, torch.int32), new(total, torch.int64), new(1, torch.int32))
+
+
+def _tables(pages: Kv4Pages, free: Kv4FreePages):
+    _same_device(pages.page_table, free.pages)
+    return (_on(pages.page_table, torch.int32, pages.R, pages.max_pages), pages.max_pages, pages.num_pages, pages.page_tokens,
+            _on(free.pages, torch.int32, pages.num_pages), _on(free.count, torch.int32, 1))
+
+
+def qift_kv4_pages_begin(pages: Kv4Pages, free: Kv4FreePages, rows, first, total: int, mask=None, out: Kv4Rows | None = None):
+    """rows, first int32 [R]: rows[r] new tokens behind first[r] cached ones -> pages for them (pages.page_table, free) and a Kv4Rows of
+    `total` rows; mask int32 [total, words]: drafted trees, whose tokens' positions are their depths."""
+    if out is None:
+        out = Kv4Rows.empty(pages.R, total, rows.device)
+    _same_device(pages.page_table, rows, first, mask, out.row_start, out.position, out.slot, out.lost)
+    words = 0 if mask is None else mask.shape[1]
+    _call(rows, lib().qift_kv4_pages_begin, _on(rows, torch.int32, pages.R), _on(first, torch.int32, pages.R), pages.R, *_tables(pages, free),
+          None if mask is None else _on(mask, torch.int32, total, words), words, total, _on(out.row_start, torch.int32, pages.R + 1),
+          _on(out.position, torch.int32, total), None if out.slot is None else _on(out.slot, torch.int64, total), _on(out.lost, torch.int32, 1))
+    return out
+
+
+def qift_kv4_pages_end(pages: Kv4Pages, free: Kv4FreePages, length, shared=None):
+    """length int32 [R]: the tokens of each request that stay (0: it has ended).  Pages behind them go back to `free`, but not the first
+    shared[r] of a request."""
+    _same_device(pages.page_table, length, shared)
+    _call(length, lib().qift_kv4_pages_end, _on(length, torch.int32, pages.R), None if shared is None else _on(shared, torch.int32, pages.R),
+          pages.R, *_tables(pages, free))
+
+
+# ---------------------------------------------------------------------------------------- norms and rotation of queries and keys
+def qift_qk_norm_rope(q, k, position, inv_freq, q_weight=None, k_weight=None, eps: float = 1e-6, pairs: int = ROPE_HALVES, q_out=None,
+                      k_out=None):
+    """q [total, Hq, D], k [total, H, D] fp32 or bf16 (slices of a projection's rows), position int32 [total], inv_freq fp32 [rot / 2],
+    weights [D] of the rows' type or None -> (q_out, k_out): normed and rotated.  q_out / k_out may be q / k; rows with a negative position
+    are left as they are there."""
+    total, Hq, D = q.shape
+    H = k.shape[1]
+    assert k.shape == (total, H, D) and q.dtype == k.dtype, "q and k have the same rows, head size and type"
+    if q_out is None:
+        q_out = torch.empty((total, Hq, D), dtype=q.dtype, device=q.device)
+    if k_out is None:
+        k_out = torch.empty((total, H, D), dtype=k.dtype, device=k.device)
+    assert q_out.shape == q.shape and k_out.shape == k.shape and q_out.dtype == q.dtype and k_out.dtype == q.dtype
+    _same_device(q, k, position, inv_freq, q_weight, k_weight, q_out, k_out)
+    weights = [None if w is None else _on(w, q.dtype, D) for w in (q_weight, k_weight)]
+    _call(q, lib().qift_qk_norm_rope, q.data_ptr(), k.data_ptr(), _float_type(q), _rows(q), _rows(k), total, Hq, H, D, *weights, eps,
+          _on(inv_freq, torch.float32), 2 * inv_freq.numel(), pairs, _on(position, torch.int32, total), q_out.data_ptr(), k_out.data_ptr(),
+          _rows(q_out), _rows(k_out))
+    return q_out, k_out
+
+
+# ---------------------------------------------------------------------------------------- gated feed-forward block
+def qift_gated_levels_min_rows() -> int:
+    """Token rows from which on the gated calls need a levels buffer."""
+    return int(lib().qift_gated_levels_min_rows())
+
+
+def _gated(X, M, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready):
+    """What the gated calls have in common: (result, accumulators, descriptors of the two outputs, levels buffer, its bytes)."""
+    (pg, sg), (pu, su) = gate, up
+    N = sg.shape[0]
+    _same_device(X, pg, sg, pu, su, out, levels_buf)
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype, device=X.device)
+    accs = [torch.empty((M, N), dtype=torch.int32, device=X.device) if want_acc else None for _ in range(2)]
+    arr = _outputs_array([gate, up], [out, out], accs)
+    if levels_buf is None:
+        assert not levels_ready
+        if M >= qift_gated_levels_min_rows() and K % 16 == 0:
+            levels_buf = torch.empty(int(lib().qift_levels_bytes(K, ctypes.addressof(arr), 2)), dtype=torch.uint8, device=X.device)
+    buf = (None, 0) if levels_buf is None else _space(levels_buf)
+    return out, accs, arr, levels_buf, buf
+
+
+def qift_gated_linear(q_a, s_a, gate, up, levels: int, activation: int = ACT_SILU, out_dtype=torch.float32, out=None, want_acc: bool = False,
+                      levels_buf=None, levels_ready: bool = False, ahead=None):
+    """q_a int8 [M, K], s_a fp32 [M], gate = up = (packed, s_n) -> h [M, N] = activation(gate product) * up product; with want_acc
+    (h, gate accumulators, up accumulators).  levels_buf, levels_ready, ahead: as for qift_forward_multi."""
+    M, K = q_a.shape
+    out, accs, arr, levels_buf, buf = _gated(q_a, M, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready)
+    _same_device(q_a, s_a)
+    ah, keep = _ahead_chain(ahead)
+    _call(q_a, lib().qift_gated_linear, _on(q_a, torch.int8), _on(s_a, torch.float32), M, K, levels, ctypes.addressof(arr), activation,
+          _on(out, out.dtype, M, arr[0].N), _float_type(out), *buf, 1 if levels_ready else 0, ah)
+    return (out, *accs) if want_acc else out
+
+
+def qift_gated_forward(X, had_block: int, gate, up, levels: int, clip_ratio: float = 0.9, activation: int = ACT_SILU, out_dtype=torch.float32,
+                       out=None, want_acc: bool = False, scratch=None, levels_buf=None, levels_ready: bool = False, ahead=None):
+    """The same from X fp32 or bf16 [M, K], which is rotated and quantized first."""
+    M, K = X.shape
+    out, accs, arr, levels_buf, buf = _gated(X, M, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready)
+    if scratch is None:
+        scratch = torch.empty(lib().qift_gated_forward_scratch_bytes(M, K), dtype=torch.uint8, device=X.device)
+    _same_device(X, scratch)
+    ah, keep = _ahead_chain(ahead)
+    _call(X, lib().qift_gated_forward, _on(X, X.dtype), _float_type(X), M, K, had_block, clip_ratio, levels, ctypes.addressof(arr), activation,
+          _on(out, out.dtype, M, arr[0].N), _float_type(out), *_space(scratch), *buf, 1 if levels_ready else 0, ah)
+    return (out, *accs) if want_acc else out
 
 
 # ---------------------------------------------------------------------------------------- resident decoded weights

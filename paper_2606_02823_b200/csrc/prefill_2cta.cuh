@@ -28,9 +28,15 @@
 // into the int8 levels that the NEXT product will read needs nothing this product computes.  Eight
 // extra warps per CTA therefore run a list of such decoding jobs (units of 8 channels x 128
 // packed words) beside the GEMM; they touch neither the pipeline's barriers nor its shared memory.
+//
+// GATED: the two segments are a feed-forward block's gate and its other projection.  A tile is BN / 2 channels of both: one CTA of a pair
+// loads the gate's rows, its peer the other matrix's, so that both accumulators of a channel lie in the same lane of tensor
+// memory, BN / 2 columns apart, and the epilogue writes h alone.
 #pragma once
 
 #include "common.cuh"
+#include "decode_tc.cuh"
+#include "gated.cuh"
 #include "prefill.cuh"
 
 namespace qift {
@@ -101,6 +107,8 @@ struct alignas(64) PairParams {
     int nseg, n_tiles;       // segments, channel tiles over all of them
     int njobs, units;        // side jobs, units over all of them
     int starve;              // self-test only (qift_selftest_wait_timeout): the producers issue no loads
+    void* H;                 // GATED: the output [M, N], and the activation function
+    int act;
 };
 
 // Side-job units: eight channel rows x 128 packed words, a word of each row per thread of a 128-thread group.
@@ -171,7 +179,7 @@ __device__ __forceinline__ void side_jobs(const PairParams& p, int t, int group)
     }
 }
 
-template <int BN>
+template <int BN, bool GATED = false>
 __global__ void __launch_bounds__(kPairThreads, 1)
 gemm_i8_pair_kernel(const __grid_constant__ PairParams p) {
     constexpr uint32_t A_BYTES = kGemmBM * kGemmBK, B_BYTES = (BN / 2) * kGemmBK, STAGE = A_BYTES + B_BYTES;
@@ -240,10 +248,10 @@ gemm_i8_pair_kernel(const __grid_constant__ PairParams p) {
             uint32_t it = 0;
             for (int tile = pair; tile < num_tiles && !*fail; tile += npairs) {
                 const int mt = tile % m_tiles, g = tile / m_tiles;
-                const int sg = segment_of(g);
+                const int sg = GATED ? 0 : segment_of(g);
                 const int m0 = mt * 2 * kGemmBM + static_cast<int>(rank) * kGemmBM;           // this CTA's tokens
-                const int n0 = (g - p.seg[sg].tile0) * BN + static_cast<int>(rank) * (BN / 2);  // this CTA's half of the channels
-                const CUtensorMap* mb = &p.map_b[sg];
+                const int n0 = GATED ? g * (BN / 2) : (g - p.seg[sg].tile0) * BN + static_cast<int>(rank) * (BN / 2);  // this CTA's half of the channels
+                const CUtensorMap* mb = GATED ? &p.map_b[rank] : &p.map_b[sg];
                 for (int kb = 0; kb < k_blocks; ++kb, ++it) {
                     const int s = it % kPairStages;
                     if (it >= kPairStages && !mbar_wait(&empty[s], ((it / kPairStages) - 1) & 1, 30, limit)) {
@@ -293,7 +301,7 @@ gemm_i8_pair_kernel(const __grid_constant__ PairParams p) {
         uint32_t tcount = 0;
         for (int tile = pair; tile < num_tiles; tile += npairs, ++tcount) {
             const int mt = tile % m_tiles, g = tile / m_tiles;
-            const int sg = segment_of(g);
+            const int sg = GATED ? 0 : segment_of(g);
             const PairSegment& S = p.seg[sg];
             const int N = S.N;
             const int buf = tcount & 1;
@@ -304,6 +312,50 @@ gemm_i8_pair_kernel(const __grid_constant__ PairParams p) {
             tc_fence_after();
             const int m = mt * 2 * kGemmBM + static_cast<int>(rank) * kGemmBM + quarter * 32 + lane;
             const float sa = (m < p.M) ? p.s_a[m] : 0.0f;
+            if constexpr (GATED) {
+                const PairSegment& U = p.seg[1];
+                for (int c0 = 0; c0 < BN / 2; c0 += 16) {
+                    uint32_t vg[16], vu[16];
+                    const uint32_t at = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BN + c0;
+                    tc_ld16(at, vg);
+                    tc_ld16(at + BN / 2, vu);
+                    tc_wait_ld();
+                    const int n = g * (BN / 2) + c0;
+                    if (m >= p.M || n >= N) continue;
+                    const size_t o = static_cast<size_t>(m) * N + n;
+                    const int live = min(16, N - n);
+                    if (S.acc_debug)
+                        for (int j = 0; j < live; ++j) S.acc_debug[o + j] = static_cast<int>(vg[j]);
+                    if (U.acc_debug)
+                        for (int j = 0; j < live; ++j) U.acc_debug[o + j] = static_cast<int>(vu[j]);
+                    float h[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (j < live)
+                            h[j] = gated_value(static_cast<int>(vg[j]), static_cast<int>(vu[j]), sa, __ldg(S.s_n + n + j), __ldg(U.s_n + n + j), p.act);
+                    if (live == 16 && (N & 7) == 0) {
+                        if (p.y_bf16) {
+                            uint32_t b[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                b[j] = static_cast<uint32_t>(f32_to_bf16_bits(h[2 * j])) | (static_cast<uint32_t>(f32_to_bf16_bits(h[2 * j + 1])) << 16);
+                            uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.H) + o);
+                            dst[0] = make_uint4(b[0], b[1], b[2], b[3]), dst[1] = make_uint4(b[4], b[5], b[6], b[7]);
+                        } else {
+                            float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.H) + o);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) dst[j] = make_float4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (j < live) {
+                                if (p.y_bf16) static_cast<uint16_t*>(p.H)[o + j] = f32_to_bf16_bits(h[j]);
+                                else static_cast<float*>(p.H)[o + j] = h[j];
+                            }
+                    }
+                }
+            } else
             for (int c0 = 0; c0 < BN; c0 += 32) {
                 uint32_t v[32];
                 tc_ld32(tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BN + c0, v);

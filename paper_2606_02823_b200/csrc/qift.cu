@@ -1,5 +1,6 @@
 // C-ABI entry points of the qift library: argument checks on the host, then kernel launches on the
 // caller's stream.  Single translation unit; the kernels live in the headers included below.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <cstdio>
@@ -11,6 +12,9 @@
 #include "decode.cuh"
 #include "decode_tc.cuh"
 #include "diag.cuh"
+#include "gated.cuh"
+#include "gated_stream.cuh"
+#include "gated_tc.cuh"
 #include "grouped.cuh"
 #include "kv4.cuh"
 #include "kv4_paged.cuh"
@@ -18,10 +22,12 @@
 #include "kv4_tree_tc.cuh"
 #include "lora.cuh"
 #include "pack.cuh"
+#include "page_tables.cuh"
 #include "prefill.cuh"
 #include "prefill_2cta.cuh"
 #include "prefill_fused.cuh"
 #include "prefill_fused_pair.cuh"
+#include "qk_rope.cuh"
 #include "quant_rows.cuh"
 #include "rotate_quant.cuh"
 
@@ -346,11 +352,13 @@ struct PairCall {
     } job[kPairMaxJobs];
     uint64_t wait_limit_ns;
     int starve;
+    void* H;               // the gated form: two segments, gate and the other projection, one output
+    int act;
 };
 
-template <int BN>
+template <int BN, bool GATED = false>
 int launch_gemm_pairs(const PairParams& pp, int tiles, cudaStream_t st) {
-    auto kernel = gemm_i8_pair_kernel<BN>;
+    auto kernel = gemm_i8_pair_kernel<BN, GATED>;
     const size_t smem = pair_smem_bytes<BN>();
     cudaError_t e = allow_smem(kernel, smem);
     if (e != cudaSuccess) return cuda_status(e);
@@ -363,8 +371,9 @@ int run_pair_gemm(const PairCall& c, cudaStream_t st) {
     if (c.nseg < 1 || c.nseg > kPairMaxSegments || c.njobs < 0 || c.njobs > kPairMaxJobs) return QIFT_ERR_INVALID_ARG;
     PairParams pp = {};
     int widths[kPairMaxSegments];
-    for (int i = 0; i < c.nseg; ++i) widths[i] = c.seg[i].N;
-    const int bn = pair_tile_width(c.M, widths, c.nseg);
+    // a gated tile is half as wide for each of its two matrices: the rounds are those of one matrix of all their channels
+    for (int i = 0; i < c.nseg; ++i) widths[i] = c.H ? 2 * c.seg[0].N : c.seg[i].N;
+    const int bn = pair_tile_width(c.M, widths, c.H ? 1 : c.nseg);
     if (!make_i8_map(&pp.map_a, c.q_a, c.M, c.K, kGemmBM)) return QIFT_ERR_CUDA;
     int tiles = 0;
     for (int i = 0; i < c.nseg; ++i) {
@@ -382,7 +391,16 @@ int run_pair_gemm(const PairCall& c, cudaStream_t st) {
         units += ((c.job[i].N + kSideUnitRows - 1) / kSideUnitRows) * ((words + kSideUnitWords - 1) / kSideUnitWords);
     }
     pp.njobs = c.njobs, pp.units = units;
+    pp.H = c.H, pp.act = c.act;
+    if (c.H) pp.n_tiles = tiles = (c.seg[0].N + bn / 2 - 1) / (bn / 2);
     const int all_tiles = ((c.M + 2 * kGemmBM - 1) / (2 * kGemmBM)) * tiles;
+    if (c.H) {
+        switch (bn) {
+            case 256: return launch_gemm_pairs<256, true>(pp, all_tiles, st);
+            case 224: return launch_gemm_pairs<224, true>(pp, all_tiles, st);
+            default: return launch_gemm_pairs<128, true>(pp, all_tiles, st);
+        }
+    }
     switch (bn) {
         case 256: return launch_gemm_pairs<256>(pp, all_tiles, st);
         case 224: return launch_gemm_pairs<224>(pp, all_tiles, st);
@@ -1925,6 +1943,251 @@ int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16
     const bool wide = M > 32ll * R && static_cast<long long>(M) * rank > 2048ll * R;
     return x_dtype == QIFT_BF16 ? (wide ? run_lora_rank<true, true>(p, st) : run_lora_rank<true, false>(p, st))
                                 : (wide ? run_lora_rank<false, true>(p, st) : run_lora_rank<false, false>(p, st));
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------------------------------- page tables, norms and rotation, gated block
+namespace {
+int check_tables(int R, const int32_t* page_table, int max_pages, int num_pages, int page_tokens, int32_t* free_pages, int32_t* free_count,
+                 PageTables* t) {
+    if (!page_table || !free_pages || !free_count || R <= 0 || max_pages <= 0 || num_pages <= 0) return QIFT_ERR_INVALID_ARG;
+    if (qift_kv4_page_bytes(page_tokens, 1, kKvD) == 0 || static_cast<long long>(R) * max_pages > 0x7fffffffll) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned4(page_table) || !aligned4(free_pages) || !aligned4(free_count)) return QIFT_ERR_ALIGNMENT;
+    *t = PageTables{const_cast<int32_t*>(page_table), free_pages, free_count, R, max_pages, num_pages, page_tokens};
+    return QIFT_OK;
+}
+
+template <bool BF16>
+int run_qk_rope(const RopeParams& p, int lanes, dim3 grid, cudaStream_t st) {
+    switch (lanes) {
+        case 2: return cuda_status(launch_pdl(qk_norm_rope_kernel<BF16, 2>, grid, dim3(kRopeThreads), 0, st, p));
+        case 4: return cuda_status(launch_pdl(qk_norm_rope_kernel<BF16, 4>, grid, dim3(kRopeThreads), 0, st, p));
+        case 8: return cuda_status(launch_pdl(qk_norm_rope_kernel<BF16, 8>, grid, dim3(kRopeThreads), 0, st, p));
+        case 16: return cuda_status(launch_pdl(qk_norm_rope_kernel<BF16, 16>, grid, dim3(kRopeThreads), 0, st, p));
+        default: return cuda_status(launch_pdl(qk_norm_rope_kernel<BF16, 32>, grid, dim3(kRopeThreads), 0, st, p));
+    }
+}
+
+constexpr int kGatedLevelsMinM = 513;   // token rows from which on the codes are decoded to int8 first
+
+template <int LV, int NT>
+int launch_gated_stream(const GatedParams& p, cudaStream_t st) {
+    auto kernel = gated_stream_kernel<LV, NT>;
+    int stages = gs_stages(p.M, p.K, LV);
+    const int tiles = (p.N + 15) / 16, chunks = (packed_pitch(p.K, LV) + kChunkWords - 1) / kChunkWords;
+    const int grid = std::min(tiles, sm_count());
+    stages = static_cast<int>(std::min<long long>(stages, static_cast<long long>((tiles + grid - 1) / grid) * chunks));
+    const size_t smem = gs_fixed_bytes(p.M, p.K, LV) + static_cast<size_t>(stages) * (gs_unit_bytes(LV) + 16);
+    const cudaError_t e = allow_smem(kernel, kGsSmem);
+    if (e != cudaSuccess) return cuda_status(e);
+    return cuda_status(launch_pdl(kernel, dim3(grid), dim3(kGsThreads), smem, st, p, stages));
+}
+template <int LV>
+int run_gated_stream(GatedParams p, cudaStream_t st) {
+    // rows of long activations are taken in blocks that leave three units of shared memory
+    int block = std::min(p.M, kGsMaxM);
+    while (block > 1 && gs_stages(block, p.K, LV) < 3) --block;
+    const int M = p.M, size = p.h_bf16 ? 2 : 4;
+    const GatedParams all = p;
+    for (int m0 = 0; m0 < M; m0 += block) {
+        p.M = std::min(block, M - m0), p.q_a = all.q_a + static_cast<size_t>(m0) * p.K, p.s_a = all.s_a + m0;
+        p.H = static_cast<unsigned char*>(all.H) + static_cast<size_t>(m0) * p.N * size;
+        for (int i = 0; i < 2; ++i)
+            if (p.w[i].acc_debug) p.w[i].acc_debug = all.w[i].acc_debug + static_cast<size_t>(m0) * p.N;
+        const int rc = p.M > 8 ? launch_gated_stream<LV, 2>(p, st) : launch_gated_stream<LV, 1>(p, st);
+        if (rc != QIFT_OK) return rc;
+    }
+    return QIFT_OK;
+}
+
+template <int LV>
+int run_gated_tc(const GatedParams& p, cudaStream_t st) {
+    GatedTcParams tp{};
+    tp.g = p, tp.blocks = (p.M + kGtTokens - 1) / kGtTokens;
+    tp.ntok = ((p.M + tp.blocks - 1) / tp.blocks + 15) / 16 * 16;
+    tp.blocks = (p.M + tp.ntok - 1) / tp.ntok;
+    tp.stages = gt_stages(LV, tp.ntok);
+    CUtensorMap map;
+    if (!make_i8_map(&map, p.q_a, p.M, p.K, tp.ntok)) return QIFT_ERR_CUDA;
+    auto kernel = gated_tc_kernel<LV>;
+    const cudaError_t e = allow_smem(kernel, kGtSmem);
+    if (e != cudaSuccess) return cuda_status(e);
+    const long long items = static_cast<long long>((p.N + kGtRows - 1) / kGtRows) * tp.blocks;
+    return cuda_status(launch_pdl(kernel, dim3(static_cast<unsigned>(std::min<long long>(items, sm_count()))), dim3(kGtThreads), kGtSmem, st, map, tp));
+}
+
+template <int LV>
+int run_gated_generic(const GatedParams& p, cudaStream_t st) {
+    const dim3 grid((p.N + kGenericWarps - 1) / kGenericWarps, static_cast<unsigned>(std::min((p.M + kGatedTokens - 1) / kGatedTokens, 4096)));
+    return cuda_status(launch_pdl(gated_generic_kernel<LV>, grid, dim3(kGenericWarps * 32), 0, st, p));
+}
+
+// Everything that can be wrong with a call, found before anything is launched.
+int check_gated(int M, int K, int levels, const qift_linear_output* gate_up, int activation, const void* H, int h_dtype, const void* levels_buf,
+                size_t levels_bytes, const qift_decode_ahead* ahead) {
+    if (!gate_up || !H || gate_up[0].N != gate_up[1].N) return QIFT_ERR_INVALID_ARG;
+    if (activation != QIFT_ACT_SILU && activation != QIFT_ACT_GELU_TANH) return QIFT_ERR_INVALID_ARG;
+    qift_linear_output o[2] = {gate_up[0], gate_up[1]};
+    for (auto& x : o) x.Y = const_cast<void*>(H);      // the outputs' own Y are not used
+    const int rc = check_outputs_and_ahead(M, K, levels, o, 2, h_dtype, ahead);
+    if (rc != QIFT_OK) return rc;
+    if (M >= kGatedLevelsMinM && K % 16 == 0) {
+        if (!levels_buf || levels_bytes < qift_levels_bytes(K, o, 2)) return QIFT_ERR_WORKSPACE;
+        if ((reinterpret_cast<uintptr_t>(levels_buf) & 255u) != 0) return QIFT_ERR_ALIGNMENT;
+    }
+    return QIFT_OK;
+}
+
+// The codes of later calls, each list into its own buffer; `int3` alone, or all level sets.
+int run_ahead(const qift_decode_ahead* ahead, bool int3_only, cudaStream_t st) {
+    for (const qift_decode_ahead* a = ahead; a; a = a->next) {
+        if (int3_only && a->levels != QIFT_LEVELS_INT3) continue;
+        for (int i = 0; i < a->count; ++i) {
+            const int rc = run_expand(a->outputs[i].packed, a->levels, a->outputs[i].N, a->K,
+                                      static_cast<int8_t*>(a->levels_buf) + levels_offset(a->K, a->outputs, i), st);
+            if (rc != QIFT_OK) return rc;
+        }
+    }
+    return QIFT_OK;
+}
+
+int gated_impl(const int8_t* q_a, const float* s_a, int M, int K, int levels, const qift_linear_output* gate_up, int activation, void* H,
+               int h_dtype, void* levels_buf, int levels_ready, const qift_decode_ahead* ahead, cudaStream_t st) {
+    GatedParams p{};
+    for (int i = 0; i < 2; ++i) p.w[i] = GatedMatrix{gate_up[i].packed, gate_up[i].s_n, gate_up[i].acc_debug};
+    p.q_a = q_a, p.s_a = s_a, p.H = H, p.M = M, p.N = gate_up[0].N, p.K = K, p.h_bf16 = h_dtype == QIFT_BF16, p.act = activation;
+    int rc;
+    if (M >= kGatedLevelsMinM && K % 16 == 0) {
+        PairCall c = {};
+        c.q_a = q_a, c.s_a = s_a, c.M = M, c.K = K, c.y_bf16 = p.h_bf16, c.nseg = 2, c.H = H, c.act = activation;
+        for (int i = 0; i < 2; ++i) {
+            int8_t* wexp = static_cast<int8_t*>(levels_buf) + levels_offset(K, gate_up, i);
+            if (!levels_ready && (rc = run_expand(gate_up[i].packed, levels, p.N, K, wexp, st)) != QIFT_OK) return rc;
+            c.seg[i].wexp = wexp, c.seg[i].s_n = gate_up[i].s_n, c.seg[i].acc_debug = gate_up[i].acc_debug, c.seg[i].N = p.N;
+        }
+        for (const qift_decode_ahead* a = ahead; a; a = a->next) {   // decoded by spare warps, three-bit codes by launches of their own
+            if (a->levels == QIFT_LEVELS_INT3) continue;
+            for (int i = 0; i < a->count; ++i) {
+                auto& j = c.job[c.njobs++];
+                j.packed = a->outputs[i].packed, j.N = a->outputs[i].N, j.K = a->K, j.levels = a->levels;
+                j.out = static_cast<int8_t*>(a->levels_buf) + levels_offset(a->K, a->outputs, i);
+            }
+        }
+        rc = run_pair_gemm(c, st);
+        return rc != QIFT_OK ? rc : run_ahead(ahead, true, st);
+    }
+#define QIFT_GATED(run)                                                        \
+    switch (levels) {                                                          \
+        case QIFT_LEVELS_MNZ: rc = run<QIFT_LEVELS_MNZ>(p, st); break;         \
+        case QIFT_LEVELS_POT: rc = run<QIFT_LEVELS_POT>(p, st); break;         \
+        case QIFT_LEVELS_SYM: rc = run<QIFT_LEVELS_SYM>(p, st); break;         \
+        case QIFT_LEVELS_INT3: rc = run<QIFT_LEVELS_INT3>(p, st); break;       \
+        default: rc = run<QIFT_LEVELS_INT4>(p, st); break;                     \
+    }
+    if (M <= kGsMaxM) {
+        QIFT_GATED(run_gated_stream)
+    } else if (K % 16 == 0) {
+        QIFT_GATED(run_gated_tc)
+    } else {
+        QIFT_GATED(run_gated_generic)      // rows that a tensor copy cannot take
+    }
+#undef QIFT_GATED
+    return rc != QIFT_OK ? rc : run_ahead(ahead, false, st);
+}
+}  // namespace
+
+extern "C" {
+
+int qift_kv4_pages_begin(const int32_t* rows, const int32_t* first, int R, int32_t* page_table, int max_pages, int num_pages,
+                         int page_tokens, int32_t* free_pages, int32_t* free_count, const int32_t* mask, int mask_words, int total,
+                         int32_t* row_start, int32_t* position, int64_t* slot, int32_t* lost, void* stream) {
+    if (!rows || !first || !row_start || !position || !lost || total <= 0) return QIFT_ERR_INVALID_ARG;
+    PageBeginParams p{};
+    int rc = check_tables(R, page_table, max_pages, num_pages, page_tokens, free_pages, free_count, &p.t);
+    if (rc != QIFT_OK) return rc;
+    if (mask && (mask_words <= 0 || mask_words > 32)) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned4(rows) || !aligned4(first) || !aligned4(mask) || !aligned4(row_start) || !aligned4(position) || !aligned4(lost) ||
+        (reinterpret_cast<uintptr_t>(slot) & 7u) != 0)
+        return QIFT_ERR_ALIGNMENT;
+    p.rows = rows, p.first = first, p.mask = mask, p.mask_words = mask_words, p.total = total, p.row_start = row_start;
+    p.position = position, p.slot = reinterpret_cast<long long*>(slot), p.lost = lost, p.fill_rows = total <= kPtFewRows;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    rc = cuda_status(launch_pdl(pages_begin_kernel, dim3(1), dim3(kPtThreads), 0, st, p));
+    if (rc != QIFT_OK || p.fill_rows) return rc;
+    const long long blocks = (total + 255ll) / 256, most = 8ll * sm_count();
+    return cuda_status(launch_pdl(pages_rows_kernel, dim3(static_cast<unsigned>(std::min(blocks, most))), dim3(256), 0, st, p));
+}
+
+int qift_kv4_pages_end(const int32_t* length, const int32_t* shared, int R, int32_t* page_table, int max_pages, int num_pages,
+                       int page_tokens, int32_t* free_pages, int32_t* free_count, void* stream) {
+    if (!length) return QIFT_ERR_INVALID_ARG;
+    PageEndParams p{};
+    const int rc = check_tables(R, page_table, max_pages, num_pages, page_tokens, free_pages, free_count, &p.t);
+    if (rc != QIFT_OK) return rc;
+    if (!aligned4(length) || !aligned4(shared)) return QIFT_ERR_ALIGNMENT;
+    p.length = length, p.shared = shared;
+    return cuda_status(launch_pdl(pages_end_kernel, dim3(1), dim3(kPtThreads), 0, static_cast<cudaStream_t>(stream), p));
+}
+
+int qift_qk_norm_rope(const void* Q, const void* K, int x_dtype, long long q_stride, long long k_stride, int total, int Hq, int H, int D,
+                      const void* q_weight, const void* k_weight, float eps, const float* inv_freq, int rot, int pairs,
+                      const int32_t* position, void* Q_out, void* K_out, long long q_out_stride, long long k_out_stride, void* stream) {
+    if (!Q || !K || !Q_out || !K_out || !inv_freq || !position || total <= 0 || Hq <= 0 || H <= 0 || D <= 0 || rot <= 0) return QIFT_ERR_INVALID_ARG;
+    if ((x_dtype != QIFT_F32 && x_dtype != QIFT_BF16) || !(eps > 0.0f) || std::isinf(eps)) return QIFT_ERR_INVALID_ARG;
+    if (pairs != QIFT_ROPE_HALVES && pairs != QIFT_ROPE_NEIGHBOURS) return QIFT_ERR_INVALID_ARG;
+    if (D % 16 != 0 || D > kRopeMaxD || rot % 16 != 0 || rot > D || Hq > 65535 || H > 65535 - Hq) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    const long long unit = x_dtype == QIFT_BF16 ? 8 : 4, wide_q = static_cast<long long>(Hq) * D, wide_k = static_cast<long long>(H) * D;
+    if (q_stride < wide_q || q_out_stride < wide_q || k_stride < wide_k || k_out_stride < wide_k) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (q_stride % unit || q_out_stride % unit || k_stride % unit || k_out_stride % unit) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(Q_out) || !aligned16(K_out) || !aligned16(q_weight) || !aligned16(k_weight) ||
+        !aligned4(inv_freq) || !aligned4(position))
+        return QIFT_ERR_ALIGNMENT;
+    RopeParams p{};
+    p.q = Q, p.k = K, p.q_out = Q_out, p.k_out = K_out, p.q_stride = q_stride, p.k_stride = k_stride, p.qo_stride = q_out_stride, p.ko_stride = k_out_stride;
+    p.q_weight = q_weight, p.k_weight = k_weight, p.inv_freq = inv_freq, p.position = position;
+    p.total = total, p.Hq = Hq, p.H = H, p.D = D, p.rot = rot, p.near = pairs == QIFT_ROPE_NEIGHBOURS, p.eps = eps;
+    int lanes = 2;
+    while (lanes * 16 < D) lanes *= 2;
+    // a row's heads are split over warps while the rows alone give an SM fewer than sixteen
+    const int trips = (Hq + H + 32 / lanes - 1) / (32 / lanes);
+    const long long warps = 16ll * sm_count();
+    p.parts = static_cast<int>(std::min(static_cast<long long>(trips), std::max(1ll, warps / total)));
+    const long long blocks = (static_cast<long long>(total) * p.parts + kRopeWarps - 1) / kRopeWarps, most = 64ll * sm_count();
+    const dim3 grid(static_cast<unsigned>(std::min(blocks, most)));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return x_dtype == QIFT_BF16 ? run_qk_rope<true>(p, lanes, grid, st) : run_qk_rope<false>(p, lanes, grid, st);
+}
+
+int qift_gated_levels_min_rows(void) { return kGatedLevelsMinM; }
+
+int qift_gated_linear(const int8_t* q_a, const float* s_a, int M, int K, int levels, const qift_linear_output* gate_up, int activation,
+                      void* H, int h_dtype, void* levels_buf, size_t levels_bytes, int levels_ready, const qift_decode_ahead* ahead,
+                      void* stream) {
+    if (!q_a || !s_a) return QIFT_ERR_INVALID_ARG;
+    const int rc = check_gated(M, K, levels, gate_up, activation, H, h_dtype, levels_buf, levels_bytes, ahead);
+    if (rc != QIFT_OK) return rc;
+    if (!aligned16(q_a) || !aligned16(s_a)) return QIFT_ERR_ALIGNMENT;
+    return gated_impl(q_a, s_a, M, K, levels, gate_up, activation, H, h_dtype, levels_buf, levels_ready, ahead, static_cast<cudaStream_t>(stream));
+}
+
+size_t qift_gated_forward_scratch_bytes(int M, int K) {
+    return M <= 0 || K <= 0 ? 0 : up1k(static_cast<size_t>(M) * K) + up1k(static_cast<size_t>(M) * 4);
+}
+
+int qift_gated_forward(const void* X, int x_dtype, int M, int K, int had_block, float clip_ratio, int levels,
+                       const qift_linear_output* gate_up, int activation, void* H, int h_dtype, void* scratch, size_t scratch_bytes,
+                       void* levels_buf, size_t levels_bytes, int levels_ready, const qift_decode_ahead* ahead, void* stream) {
+    if (!X || (x_dtype != QIFT_F32 && x_dtype != QIFT_BF16)) return QIFT_ERR_INVALID_ARG;
+    int rc = check_gated(M, K, levels, gate_up, activation, H, h_dtype, levels_buf, levels_bytes, ahead);
+    if (rc != QIFT_OK) return rc;
+    if (!scratch || scratch_bytes < qift_gated_forward_scratch_bytes(M, K)) return QIFT_ERR_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return QIFT_ERR_ALIGNMENT;
+    int8_t* q_a = static_cast<int8_t*>(scratch);
+    float* s_a = reinterpret_cast<float*>(q_a + up1k(static_cast<size_t>(M) * K));
+    rc = qift_quantize_act(X, x_dtype, M, K, had_block, clip_ratio, q_a, s_a, stream);
+    if (rc != QIFT_OK) return rc;
+    return gated_impl(q_a, s_a, M, K, levels, gate_up, activation, H, h_dtype, levels_buf, levels_ready, ahead, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

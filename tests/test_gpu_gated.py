@@ -1,0 +1,124 @@
+"""The gated half of a feed-forward block: exact sums, h against 64 bits, on every route."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2606_02823_b200 as qift
+from gated_ref import LEVELS, Case, check
+
+pytestmark = pytest.mark.gpu
+ACTS = [qift.ACT_SILU, qift.ACT_GELU_TANH]
+
+
+def run(c, act=qift.ACT_SILU, dtype=torch.float32, **kw):
+    return qift.qift_gated_linear(c.q, c.s, *c.weights, c.lv, activation=act, out_dtype=dtype, **kw)
+
+
+@pytest.mark.parametrize("levels", list(LEVELS))
+@pytest.mark.parametrize("M, N, K", [
+    (1, 1, 32), (1, 300, 1024), (1, 2400, 4096), (2, 17, 256), (3, 100, 288), (5, 16, 4096), (7, 1000, 2048), (8, 333, 544), (9, 48, 1024),
+    (13, 130, 4128), (16, 260, 4096), (16, 100, 14336), (17, 100, 256), (20, 129, 1056), (31, 300, 1024), (33, 257, 2080), (48, 500, 512), (64, 128, 4096),
+    (65, 31, 1024), (100, 390, 256), (128, 256, 2048), (129, 200, 256), (200, 131, 1056), (300, 700, 1024), (513, 300, 512), (1025, 515, 256)])
+def test_sizes(M, N, K, levels):
+    c = Case(M * 7 + N, M, N, K, levels)
+    act = ACTS[(M + N) % 2]
+    sums = c.sums()
+    h, *accs = run(c, act, want_acc=True)
+    c.check(h, accs, act, sums)
+    b = run(c, act, torch.bfloat16)
+    assert torch.equal(b, h.to(torch.bfloat16))                      # the same fp32 value, rounded once
+
+
+@pytest.mark.parametrize("levels, K", [("mnz", 16), ("mnz", 48), ("pot", 1040), ("sym", 272), ("int4", 8), ("int4", 24), ("int4", 136), ("int4", 4104), ("int3", 96)])
+@pytest.mark.parametrize("M", [1, 6, 16, 40, 140])
+def test_odd_depths(M, K, levels):
+    c = Case(K + M, M, 37, K, levels)
+    h, *accs = run(c, want_acc=True)
+    c.check(h, accs)
+
+
+@pytest.mark.parametrize("M", [1, 30, 150])
+@pytest.mark.parametrize("act", ACTS)
+def test_large_and_small_gates(M, act):
+    """Gates beyond +-100: exp(-z) passes the fp32 range, the activation goes to g and to 0."""
+    c = Case(3, M, 400, 512, "int4", extreme=True)
+    c.s[0] = 40.0
+    c.s[-1] = 0.0
+    h = run(c, act)
+    assert torch.isfinite(h).all()
+    c.check(h, act=act)
+    assert (h[-1] == 0).all()
+
+
+def test_same_rows_same_bits_on_every_route():
+    """A row's results do not depend on how many others there are."""
+    c = Case(5, 700, 333, 512, "mnz")
+    whole = run(c)
+    for M in (1, 2, 9, 20, 60, 128, 200):
+        part = qift.qift_gated_linear(c.q[:M].contiguous(), c.s[:M].contiguous(), *c.weights, c.lv)
+        assert torch.equal(part, whole[:M]), M
+
+
+@pytest.mark.parametrize("M", [1, 4, 40, 200])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_forward_from_activations(M, dtype):
+    c = Case(11, M, 130, 1024, "mnz")
+    x = torch.from_numpy(np.random.default_rng(M).standard_normal((M, 1024)).astype(np.float32)).cuda().to(dtype)
+    q, s = oracle.quantize_act(x.float().cpu().numpy(), 1024, 0.9)
+    c.q, c.s = torch.from_numpy(q).cuda(), torch.from_numpy(s).cuda()
+    h, *accs = qift.qift_gated_forward(x, 1024, *c.weights, c.lv, 0.9, want_acc=True)
+    c.check(h, accs)
+    scratch = torch.empty(qift.lib().qift_gated_forward_scratch_bytes(M, 1024), dtype=torch.uint8, device="cuda")
+    assert torch.equal(h, qift.qift_gated_forward(x, 1024, *c.weights, c.lv, 0.9, scratch=scratch))
+
+
+def test_extremes_of_the_codes():
+    """Largest sums: every code and activation at the end of its range."""
+    for levels, lv in LEVELS.items():
+        K, N, M = 16384, 33, 3
+        top = int(np.argmax(np.abs(oracle.level_table(lv))))
+        packed = torch.from_numpy(oracle.pack(np.full((N, K), top, np.uint8), lv).view(np.int32).ravel()).cuda()
+        s_n, s_a = torch.full((N,), 1e-5, device="cuda"), torch.ones(M, device="cuda")
+        q = torch.full((M, K), -8, dtype=torch.int8, device="cuda")
+        q[1] = 7
+        h, a, b = qift.qift_gated_linear(q, s_a, (packed, s_n), (packed, s_n), lv, want_acc=True)
+        v = int(oracle.level_table(lv)[top])
+        assert (a[0] == -8 * v * K).all() and (a[1] == 7 * v * K).all() and torch.equal(a, b), levels
+        check(h, [a, b], s_a, [s_n, s_n], qift.ACT_SILU)
+
+
+def test_levels_decoded_ahead():
+    """The call in a chain: another call decodes its codes, and it decodes another's."""
+    M = max(300, qift.qift_gated_levels_min_rows())
+    c, d = Case(1, M, 200, 512, "mnz"), Case(2, M, 96, 256, "int3")
+    buf = torch.zeros(qift.qift_levels_bytes(512, c.weights), dtype=torch.uint8, device="cuda")
+    other = torch.zeros(qift.qift_levels_bytes(256, d.weights), dtype=torch.uint8, device="cuda")
+    x = torch.from_numpy(np.random.default_rng(1).standard_normal((M, 512)).astype(np.float32)).cuda()
+    qift.qift_forward_multi(x, 512, c.weights, c.lv, ahead=(c.weights, 512, c.lv, buf))
+    h = run(c, levels_buf=buf, levels_ready=True, ahead=(d.weights, 256, d.lv, other))
+    c.check(h)
+    e = run(d, levels_buf=other, levels_ready=True)
+    d.check(e)
+    small = Case(3, 5, 200, 512, "mnz")                              # few rows decode for later calls all the same
+    buf.zero_()
+    run(small, ahead=(c.weights, 512, c.lv, buf))
+    assert torch.equal(run(c, levels_buf=buf, levels_ready=True), h)
+
+
+@pytest.mark.parametrize("M", [1, 12, 50, 400])
+def test_captured_on_another_stream(M):
+    c = Case(4, M, 500, 1024, "mnz")
+    out = torch.zeros((M, 500), device="cuda")
+    buf = torch.empty(qift.qift_levels_bytes(1024, c.weights), dtype=torch.uint8, device="cuda")
+    run(c, out=out, levels_buf=buf)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(c, out=out, levels_buf=buf)
+    for seed in range(2):
+        c.q.copy_(torch.from_numpy(np.random.default_rng(seed).integers(-8, 8, (M, 1024)).astype(np.int8)))
+        out.zero_()
+        graph.replay()
+        c.check(out)
+    rc, detail = qift.qift_device_status()
+    assert rc == qift.OK, (rc, detail)

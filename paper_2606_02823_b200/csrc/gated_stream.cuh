@@ -17,6 +17,7 @@
 #include "decode.cuh"
 #include "gated.cuh"
 #include "grouped.cuh"
+#include "kv4_tree_tc.cuh"
 
 namespace qift {
 
@@ -51,7 +52,7 @@ __device__ __forceinline__ int gs_result(int S, int sum_q) {
 
 template <int LV, int NT>
 __global__ void __launch_bounds__(kGsThreads, 1)
-gated_stream_kernel(const GatedParams p, int stages) {
+gated_stream_kernel(const __grid_constant__ GatedParams p, int stages) {
     constexpr int PER = codes_per_word(LV), NPL = PER / 4;
     constexpr int NACC = LV == QIFT_LEVELS_POT ? 1 : DecodeTraits<LV>::NACC;
     constexpr int WB = tile_word_bytes(LV), HALF = kChunkWords * WB, UNIT = 2 * HALF;
@@ -79,24 +80,25 @@ gated_stream_kernel(const GatedParams p, int stages) {
 
     if (warp == kGsWarps) {
         // ---------------------------------------------------------------- producer: the weights depend on no kernel before this one
-        if (lane == 0) {
-            int s = 0, k = 0;
-            uint32_t ph = 0;
-            for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
-                const size_t tile = static_cast<size_t>(t) * pitch * WB;
-                for (int c = 0; c < chunks; ++c, ++k) {
-                    if (k >= stages && !mbar_wait(&empty[s], ph, 80)) {
-                        *fail = 1;
-                        return;
-                    }
+        int s = 0, k = 0;
+        uint32_t ph = 0;
+        for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+            const size_t tile = static_cast<size_t>(t) * pitch * WB;
+            for (int c = 0; c < chunks; ++c, ++k) {
+                if (k >= stages && !mbar_wait_near(&empty[s], ph, 80)) {
+                    *fail = 1;
+                    return;
+                }
+                if (elect_one()) {
                     const uint32_t bytes = min(kChunkWords, pitch - c * kChunkWords) * WB;
                     mbar_expect_tx(&full[s], 2 * bytes);
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
                         bulk_g2s(ring + s * UNIT + i * HALF, reinterpret_cast<const unsigned char*>(p.w[i].packed) + tile + static_cast<size_t>(c) * HALF,
                                  bytes, &full[s]);
-                    if (++s == stages) s = 0, ph ^= (k >= stages);
                 }
+                __syncwarp();
+                if (++s == stages) s = 0, ph ^= (k >= stages);
             }
         }
         return;
@@ -152,7 +154,7 @@ gated_stream_kernel(const GatedParams p, int stages) {
         int acc[NT][NACC][4] = {};
         for (int c = 0; c < chunks; ++c) {
             // a wait that has run out once is not tried again; the warp goes on to the barriers that the others wait at
-            if (ok && !mbar_wait(&full[s], ph, 81)) ok = false, *fail = 1;
+            if (ok && !mbar_wait_near(&full[s], ph, 81)) ok = false, *fail = 1;
             const int at = c * (kChunkWords / 16) + slice;       // the slice among the row's
             if (ok && at < slices) {
                 const uint32_t w = smem_u32(ring + s * UNIT + mat * HALF) + slice * (16 * WB) + lane * 16;

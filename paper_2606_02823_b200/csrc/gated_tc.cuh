@@ -4,56 +4,89 @@
 // An item is 128 channels of both matrices times one block of up to 128 token rows (N of the instruction, any multiple of 16: 48 rows
 // cost what 48 cost).  The two matrices are two independent streams over one sequence of activation blocks:
 //
-//   warp 0        activations: per 128-byte k-block the q_a rows of the token block, one tensor copy into a swizzled stage
-//   warps 1, 2    issue the products of the gate's, of the other matrix's operands: D[matrix][128 channels x tokens]
-//   warps 3-10    while the products run, the token sums of the staged activations (an eighth of the rows each); then the epilogue, two
-//                 warps per tensor-memory lane quarter on alternate 16-token pieces: both accumulators, h, stores of 32 channels
-//   warps 11-18   expanders, one per matrix and lane quarter: packed words of their 32 channels by cp.async (kGtSlots slices ahead,
-//                 across items), one to four logic operations per operand word, tcgen05.st into the matrix's four k-blocks of operands
-// Activations come as they are (no prescaling, no launch before this one): the operand bytes are the codes themselves, unsigned, and the
-// affine level map is undone with the token sums; the power-of-two set's bytes are its levels by table lookup, in k order.
+//   warp 0        fills a ring of steps (256 codes deep) with tensor copies: the packed words of both matrices (three dimensions: a row's 64
+//                 bytes of a slice, swizzled; rows; blocks of sixteen rows) and the q_a rows of the token block, two 128-byte k-blocks
+//   warps 1, 2    issue the products D[matrix][128 channels x tokens] of a matrix each, eight a step
+//   warps 4-19    expanders, two per matrix and lane quarter, a k-block of a step each: the packed words of their 32 channels, one to four
+//                 operations per operand word, tcgen05.st into the matrix's ring of two steps; then the epilogue, four per lane
+//                 quarter on 8-token pieces by turns: both accumulators, h, stores of 32 channels
+//
+// Activations come as they are, and there is no launch before this one: the operand bytes are the levels themselves times a power of two, made
+// by moving a code to the top of its byte -- (code << 6) ^ 0xa0 = 32 (2 code - 3) as a signed byte, (code << 6) ^ 0x80 = 64 (code - 2), the
+// four- and three-bit codes 16 and 32 times themselves -- or, for the power-of-two set, by table lookup.  No correction by token sums (which
+// took as long as the products) and no place values; an arithmetic shift takes the factor off.
 // Token blocks of one channel tile are neighbours in the item list, so that its codes come from L2 for all but the first.
 //
-// Bound by the tensor cores from about 64 rows on (a 128 x N x 32 product takes N / 2 cycles, a thread issues one every 50), by the
-// codes' way into an SM below (256 KB an item at about 76 GB/s).
+// Bounds: a 128 x N x 32 product takes N / 2 cycles of the tensor cores, 16 at least; operands enter tensor memory at 128 bytes a cycle
+// (1 MB an item of K = 4096: 4.3 us); their logic is 56 operations per k-block and warp.  A thread that a whole warp has elected issues a
+// product in 16 cycles; one that a comparison of lanes has picked takes 60 (the compiler cannot know it is alone, and tries every
+// lane's operands), which alone set the pace at first: 23 us for 48 rows, 4096 -> 14336.  Waits carry no time hint (with one they
+// are a loop around a sleep) and are bounded by their trips.
 #pragma once
 
 #include "common.cuh"
 #include "decode_tc.cuh"
 #include "gated.cuh"
+#include "kv4_tree_tc.cuh"
 #include "prefill.cuh"
 
 namespace qift {
 
 constexpr int kGtRows = 128;                 // channels of an item
 constexpr int kGtTokens = 128;               // token rows of an item, at most
-constexpr int kGtThreads = 32 * 19;
-constexpr int kGtEpiWarps = 8;
-constexpr int kGtRing = 4;                   // k-blocks of operands in tensor memory, per matrix
+constexpr int kGtExpanders = 16, kGtExpander0 = 4;                   // warps, the first of them
+constexpr int kGtThreads = 32 * (kGtExpander0 + kGtExpanders);
+constexpr int kGtRing = 2;                   // steps of operands in tensor memory, per matrix
 constexpr int kGtOperands = 256;             // first operand column
 constexpr int kGtSmem = 226 * 1024;
 
-__host__ __device__ constexpr int gt_slot_bytes(int lv) { return 32 * (lv == QIFT_LEVELS_INT3 ? 96 : 64); }   // 32 rows of a slice
-__host__ __device__ constexpr int gt_slots(int lv) { return lv == QIFT_LEVELS_INT3 ? 4 : 7; }                  // slices ahead, per expander
+__host__ __device__ constexpr int gt_slices(int lv) { return lv == QIFT_LEVELS_INT4 ? 2 : 1; }            // 16-word slices of a step
+__host__ __device__ constexpr int gt_slice_rows(int lv) { return lv == QIFT_LEVELS_INT3 ? 24 : 16; }      // 64-byte rows of a slice and row block
+__host__ __device__ constexpr int gt_word_bytes(int lv) { return 8 * 64 * gt_slices(lv) * gt_slice_rows(lv); }   // of a step and matrix
 __host__ __device__ inline int gt_stages(int lv, int ntok) {
-    const int left = (kGtSmem - 2048 - 8 * gt_slots(lv) * gt_slot_bytes(lv)) / (ntok * 128);
-    return left < 10 ? left : 10;
+    const int n = (kGtSmem - 3072) / (2 * gt_word_bytes(lv) + ntok * 256);
+    return n < 8 ? n : 8;
 }
 
 struct GatedTcParams {
     GatedParams g;
     int ntok, blocks;        // token rows of a block (a multiple of 16), blocks
-    int stages;
+    int stages;              // steps in shared memory
+};
+struct alignas(64) GatedTcMaps {
+    CUtensorMap act;         // q_a [M, K], box = 128 bytes x ntok rows
+    CUtensorMap words[2];    // [row blocks][rows of a block's slices][64 bytes], box = 8 x a step's rows x 64
 };
 
-// Operand bytes of one k-block (128 codes) of a channel, in k order.  hi: the words of the third bits (INT3).
+// Operand bytes of one k-block (128 codes) of a channel, in k order: level * 2^gt_shift.  hi: the words of the third bits (INT3).
+template <int LV>
+__host__ __device__ constexpr int gt_shift() {
+    return LV == QIFT_LEVELS_MNZ || LV == QIFT_LEVELS_INT3 ? 5 : LV == QIFT_LEVELS_SYM ? 6 : LV == QIFT_LEVELS_INT4 ? 4 : 0;
+}
+// (a & b) ^ c with all three in registers: one instruction (with two immediates it would be two, and the operands' logic is what the
+// expanders' time goes into).
+__device__ __forceinline__ uint32_t and_xor(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+// (a & b) | (c & ~b)
+__device__ __forceinline__ uint32_t select_bits(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xe2;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t in_register(uint32_t v) {
+    asm volatile("" : "+r"(v));
+    return v;
+}
 template <int LV>
 __device__ __forceinline__ void gt_operands(const uint32_t* w, const uint32_t* hi, uint32_t (&o)[32]) {
     if constexpr (LV == QIFT_LEVELS_INT4) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            o[2 * i] = (w[i] & 0x0f0f0f0fu) ^ 0x08080808u;
-            o[2 * i + 1] = ((w[i] >> 4) & 0x0f0f0f0fu) ^ 0x08080808u;
+            o[2 * i] = (w[i] << 4) & 0xf0f0f0f0u;
+            o[2 * i + 1] = w[i] & 0xf0f0f0f0u;
         }
     } else if constexpr (LV == QIFT_LEVELS_POT) {
 #pragma unroll
@@ -63,69 +96,71 @@ __device__ __forceinline__ void gt_operands(const uint32_t* w, const uint32_t* h
             o[4 * i] = __byte_perm(a[0], a[2], 0x6420), o[4 * i + 2] = __byte_perm(a[0], a[2], 0x7531);
             o[4 * i + 1] = __byte_perm(a[1], a[3], 0x6420), o[4 * i + 3] = __byte_perm(a[1], a[3], 0x7531);
         }
-    } else {
+    } else if constexpr (LV == QIFT_LEVELS_INT3) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const uint32_t c = (w[i] >> (2 * t)) & 0x03030303u;
-                if constexpr (LV == QIFT_LEVELS_INT3) {      // the third bit, turned over, to its place: (code ^ 4) = level + 4
-                    const int at = int3_high_shift(i, t);
-                    const uint32_t b = at >= 2 ? hi[i >> 1] >> (at - 2) : hi[i >> 1] << (2 - at);
-                    o[4 * i + t] = c | ((b & 0x04040404u) ^ 0x04040404u);
-                } else {
-                    o[4 * i + t] = c;
-                }
+                const uint32_t c = t < 3 ? w[i] << (5 - 2 * t) : w[i] >> 1, b = hi[i >> 1] << (7 - int3_high_shift(i, t));
+                o[4 * i + t] = select_bits(b, 0x80808080u, c) & 0xe0e0e0e0u;
             }
+    } else {
+        const uint32_t keep = in_register(0xc0c0c0c0u), turn = in_register(LV == QIFT_LEVELS_MNZ ? 0xa0a0a0a0u : 0x80808080u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) o[4 * i + t] = and_xor(w[i] << (6 - 2 * t), keep, turn);
     }
 }
-template <int LV>
-__device__ __forceinline__ int gt_result(int d, int sum_q) {
-    if constexpr (LV == QIFT_LEVELS_POT) return d;
-    if constexpr (LV == QIFT_LEVELS_MNZ) return 2 * d - 3 * sum_q;
-    if constexpr (LV == QIFT_LEVELS_SYM) return d - 2 * sum_q;
-    if constexpr (LV == QIFT_LEVELS_INT3) return d - 4 * sum_q;
-    return d - 8 * sum_q;
+__device__ __forceinline__ void gt_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(taddr)
+                 : "memory");
 }
-
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+                 "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
 template <int LV>
 __global__ void __launch_bounds__(kGtThreads, 1)
-gated_tc_kernel(const __grid_constant__ CUtensorMap map, const GatedTcParams tp) {
-    constexpr int PER = codes_per_word(LV), KPS = PER == 16 ? 2 : 1;   // k-blocks of a 16-word slice
-    constexpr int WB = tile_word_bytes(LV), SLOTS = gt_slots(LV), SLOT = gt_slot_bytes(LV);
+gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant__ GatedTcParams tp) {
+    constexpr int SPS = gt_slices(LV), SROWS = gt_slice_rows(LV), RB = 64 * SPS * SROWS;   // bytes of a row block in a step
+    constexpr uint32_t WORDS = gt_word_bytes(LV);
     const GatedParams& p = tp.g;
     const int ntok = tp.ntok, stages = tp.stages;
-    const uint32_t act_bytes = ntok * 128;
-    // D = s32, A = u8 (the power-of-two set: s8), B = s8, both K-major, M = 128
-    const uint32_t idesc = (2u << 4) | ((LV == QIFT_LEVELS_POT ? 1u : 0u) << 7) | (1u << 10) | (static_cast<uint32_t>(ntok >> 3) << 17) |
+    const uint32_t act_bytes = ntok * 128, stage_bytes = 2 * WORDS + 2 * act_bytes;        // a stage: both matrices' words, two k-blocks
+    // D = s32, A = B = s8, both K-major, M = 128
+    const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(ntok >> 3) << 17) |
                            (static_cast<uint32_t>(kGtRows >> 4) << 24);
-    const int sets = ntok <= 32 ? 4 : ntok <= 64 ? 2 : 1;              // accumulators of a matrix, by turns: 2 * sets * ntok <= 256
 
     extern __shared__ unsigned char smem_raw[];
-    unsigned char* act = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    unsigned char* words = act + stages * act_bytes;
-    uint64_t* act_full = reinterpret_cast<uint64_t*>(words + 8 * SLOTS * SLOT);
-    uint64_t* act_empty = act_full + stages;
-    uint64_t* a_full = act_empty + stages;           // [matrix][kGtRing]
+    unsigned char* staged = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* full = reinterpret_cast<uint64_t*>(staged + stages * stage_bytes);
+    uint64_t* empty = full + stages;
+    uint64_t* a_full = empty + stages;               // [matrix][kGtRing]
     uint64_t* a_empty = a_full + 2 * kGtRing;
     uint64_t* d_full = a_empty + 2 * kGtRing;
     uint64_t* d_empty = d_full + 1;
-    int* sum_q = reinterpret_cast<int*>(d_empty + 1);                 // [kGtTokens]
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sum_q + kGtTokens);
+    float* scale = reinterpret_cast<float*>(d_empty + 1);             // [kGtTokens] of the tokens
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(scale + kGtTokens);
     volatile int* fail = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int pitch = packed_pitch(p.K, LV), slices = pitch / 16, kblocks = slices * KPS;
+    const int steps = (packed_pitch(p.K, LV) / 16 + SPS - 1) / SPS;
     const int items = ((p.N + kGtRows - 1) / kGtRows) * tp.blocks;
+    // CTAs begin at different steps (the sums are integers, their order is free): all of them read the same activations, and a line
+    // that a hundred of them ask for at once takes as long as a hundred lines
+    const int first_step = blockIdx.x % steps;
 
     pdl_launch_dependents();
-    if (tid == 0) {
-        for (int s = 0; s < stages; ++s) mbar_init(&act_full[s], 1), mbar_init(&act_empty[s], 2 + kGtEpiWarps);
-        for (int s = 0; s < 2 * kGtRing; ++s) mbar_init(&a_full[s], 4), mbar_init(&a_empty[s], 1);
-        mbar_init(d_full, 2), mbar_init(d_empty, kGtEpiWarps);
+    if (warp == 0 && lane == 0) {
+        for (int s = 0; s < stages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 2 + kGtExpanders);
+        for (int s = 0; s < 2 * kGtRing; ++s) mbar_init(&a_full[s], 8), mbar_init(&a_empty[s], 1);
+        mbar_init(d_full, 2), mbar_init(d_empty, kGtExpanders);
         *fail = 0;
         mbar_fence_init();
-        tma_prefetch_desc(&map);
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
@@ -137,211 +172,178 @@ gated_tc_kernel(const __grid_constant__ CUtensorMap map, const GatedTcParams tp)
     const uint32_t tmem = *tmem_slot;
 
     if (warp == 0) {
-        // ------------------------------------------------------------------ activations
+        // ------------------------------------------------------------------ words and activations
+        auto words = [&](int s, int item, int step) {
+            const int rb = (item / tp.blocks) * 8;
+            mbar_expect_tx(&full[s], stage_bytes);
+            tma_load_3d(staged + s * stage_bytes, &maps.words[0], 0, step * (SPS * SROWS), rb, &full[s]);
+            tma_load_3d(staged + s * stage_bytes + WORDS, &maps.words[1], 0, step * (SPS * SROWS), rb, &full[s]);
+        };
+        auto activations = [&](int s, int item, int step) {
+            unsigned char* to = staged + s * stage_bytes + 2 * WORDS;
+            const int m0 = (item % tp.blocks) * ntok;
+            tma_load_2d(to, &maps.act, step * 256, m0, &full[s]);
+            tma_load_2d(to + act_bytes, &maps.act, step * 256 + 128, m0, &full[s]);
+        };
+        // the words depend on no kernel before this one: the first stages' are asked for before the wait for it
+        const int early = min(stages, steps);
+        for (int i = 0, step = first_step; i < early; ++i, step = step + 1 == steps ? 0 : step + 1)
+            if (elect_one()) words(i, blockIdx.x, step);
         pdl_wait();
-        if (lane == 0) {
-            int s = 0;
-            uint32_t ph = 1;                                           // the first round finds the stages empty
-            bool ok = true;
-            for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
-                const int m0 = (item % tp.blocks) * ntok;
-                for (int kb = 0; kb < kblocks; ++kb) {
-                    if (!mbar_wait(&act_empty[s], ph, 82)) {
-                        *fail = 1, ok = false;
-                        break;
-                    }
-                    mbar_expect_tx(&act_full[s], act_bytes);
-                    tma_load_2d(act + s * act_bytes, &map, kb * 128, m0, &act_full[s]);
-                    if (++s == stages) s = 0, ph ^= 1;
+        int s = 0, k = 0;
+        uint32_t ph = 1;                                               // the first round finds the stages empty
+        bool ok = true;
+        for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
+            for (int i = 0, step = first_step; i < steps; ++i, ++k) {
+                if (!mbar_wait_near(&empty[s], ph, 82)) {
+                    *fail = 1, ok = false;
+                    break;
                 }
+                if (elect_one()) {
+                    if (k >= early) words(s, item, step);
+                    activations(s, item, step);
+                }
+                __syncwarp();
+                if (++s == stages) s = 0, ph ^= 1;
+                if (++step == steps) step = 0;
             }
         }
     } else if (warp <= 2) {
-        // ------------------------------------------------------------------ products of one matrix
-        if (lane == 0) {
-            const int mat = warp - 1;
-            const uint64_t desc0 = make_kmajor_sw128_desc(smem_u32(act));
-            const uint32_t d = tmem + mat * sets * ntok, a = tmem + kGtOperands + mat * kGtRing * 32;
-            int s = 0, slot = 0, count = 0;
-            uint32_t ph = 0, slot_ph = 0;
-            bool ok = true;
-            for (int item = blockIdx.x; item < items && ok; item += gridDim.x, ++count) {
-                if (count > 0 && !mbar_wait(d_empty, (count - 1) & 1, 83)) {
-                    *fail = 1;
-                    break;
-                }
+        // ------------------------------------------------------------------ products of a matrix
+        const int mat = warp - 1;
+        const uint64_t desc0 = make_kmajor_sw128_desc(smem_u32(staged) + 2 * WORDS);
+        const uint32_t d = tmem + mat * ntok, a = tmem + kGtOperands + mat * kGtRing * 64;
+        int s = 0, count = 0;
+        uint32_t ph = 0, turn = 0, turn_ph = 0;                        // turn: the step's slot of operands, the parity of its running number
+        bool ok = true;
+        for (int item = blockIdx.x; item < items && ok; item += gridDim.x, ++count) {
+            if (count > 0) ok = mbar_wait_near(d_empty, (count - 1) & 1, 83);
+            tc_fence_after();
+            for (int i = 0; i < steps; ++i) {
+                if (ok) ok = mbar_wait_near(&full[s], ph, 84);
+                if (ok) ok = mbar_wait_near(&a_full[mat * kGtRing + turn], turn_ph, 85);
+                if (!ok) break;
                 tc_fence_after();
-                for (int kb = 0; kb < kblocks; ++kb) {
-                    if (!mbar_wait(&act_full[s], ph, 84) || !mbar_wait(&a_full[mat * kGtRing + slot], slot_ph, 85)) {
-                        *fail = 1, ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint64_t b = desc0 + s * (act_bytes >> 4);
+                if (elect_one()) {
+                    const uint64_t b = desc0 + s * (stage_bytes >> 4);
+                    const uint32_t at = a + turn * 64;
 #pragma unroll
-                    for (int k4 = 0; k4 < 4; ++k4)
-                        tc_mma_i8_ts(d + (k4 & (sets - 1)) * ntok, a + slot * 32 + 8 * k4, b + 2 * k4, idesc, kb > 0 || k4 >= sets);
-                    tc_commit(&a_empty[mat * kGtRing + slot]);
-                    tc_commit(&act_empty[s]);
-                    if (++s == stages) s = 0, ph ^= 1;
-                    if (++slot == kGtRing) slot = 0, slot_ph ^= 1;
+                    for (int k = 0; k < 8; ++k) tc_mma_i8_ts(d, at + 8 * k, b + (k >> 2) * (act_bytes >> 4) + 2 * (k & 3), idesc, i | k);
+                    tc_commit(&a_empty[mat * kGtRing + turn]);
+                    tc_commit(&empty[s]);
+                    if (i + 1 == steps) tc_commit(d_full);
                 }
-                if (ok) tc_commit(d_full);
+                __syncwarp();
+                if (++s == stages) s = 0, ph ^= 1;
+                if ((turn ^= 1) == 0) turn_ph ^= 1;
             }
         }
-    } else if (warp <= 2 + kGtEpiWarps) {
-        // ------------------------------------------------------------------ token sums, epilogue
-        const int e = warp - 3, quarter = warp & 3, eg = e >> 2;       // two warps of each lane quarter
-        const int per_warp = ntok / kGtEpiWarps;                       // rows whose sums this warp takes: 2 .. 16
+        if (!ok) *fail = 1;
+    } else if (warp >= kGtExpander0) {
+        // ------------------------------------------------------------------ operands, then the epilogue
+        const int quarter = warp & 3;                                  // the lanes of tensor memory that this warp can reach
+        const int e = warp - kGtExpander0, mat = (e >> 2) & 1, half = e >> 3;   // its matrix, its k-block of a step
+        // its words of a step: two 16-byte pieces of a row (INT4: all four of a slice); pieces are exclusive-ored by (row >> 1) & 3
+        constexpr int PIECES = SPS == 2 ? 4 : 2;
+        const uint32_t rows64 = smem_u32(staged) + mat * WORDS + (2 * quarter + (lane >> 4)) * RB;
+        const uint32_t get = rows64 + (SPS == 2 ? half * 1024 : 0) + (lane & 15) * 64;
+        const uint32_t put = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + kGtOperands + mat * kGtRing * 64 + half * 32;
+        const uint32_t get_hi = rows64 + 1024 + (lane & 7) * 64 + ((lane >> 3) & 1) * 8;   // INT3: rows 16 .. 23: {third bits of row r, of row r + 8}
+        uint32_t at[PIECES];
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) at[j] = ((SPS == 2 ? j : 2 * half + j) ^ ((lane >> 1) & 3)) << 4;
+        const GateFunction act(p.act);
         pdl_wait();
-        bool ok = true;       // a wait that has run out is not tried again; the warp keeps coming to the barriers of the eight
+        // a wait that has run out is not tried again: the warp goes through the motions, keeps coming to the barriers of the sixteen and stores nothing
+        bool ok = true;
         int s = 0, count = 0;
-        uint32_t ph = 0;
+        uint32_t ph = 0, turn = 0, a_ph = 1;
         for (int item = blockIdx.x; item < items; item += gridDim.x, ++count) {
             const int m0 = (item % tp.blocks) * ntok, n0 = (item / tp.blocks) * kGtRows;
             const int rows = min(ntok, p.M - m0);
-            if constexpr (LV != QIFT_LEVELS_POT) {
-                int sum[4] = {};
-                for (int kb = 0; kb < kblocks; ++kb) {
-                    if (ok && !mbar_wait(&act_full[s], ph, 86)) ok = false, *fail = 1;
+            const int r = 32 * e + lane;
+            if (r < ntok) scale[r] = r < rows ? p.s_a[m0 + r] : 0.0f;
+            for (int i = 0; i < steps; ++i) {
+                if (ok) ok = mbar_wait_near(&full[s], ph, 87);
+                uint32_t w[4 * PIECES], hi[4] = {};
+                const uint32_t from = get + s * stage_bytes;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int r = 4 * j + (lane >> 3);             // eight lanes read a row's 128 bytes, in whatever order they stand
-                        if (ok && r < per_warp) {
-                            const uint4 v = lds128(smem_u32(act) + s * act_bytes + (e * per_warp + r) * 128 + (lane & 7) * 16);
-                            sum[j] = __dp4a(static_cast<int>(v.x), 0x01010101, __dp4a(static_cast<int>(v.y), 0x01010101, sum[j]));
-                            sum[j] = __dp4a(static_cast<int>(v.z), 0x01010101, __dp4a(static_cast<int>(v.w), 0x01010101, sum[j]));
-                        }
+                for (int j = 0; j < PIECES; ++j) {
+                    const uint4 v = lds128(from + at[j]);
+                    w[4 * j] = v.x, w[4 * j + 1] = v.y, w[4 * j + 2] = v.z, w[4 * j + 3] = v.w;
+                    if constexpr (LV == QIFT_LEVELS_INT3) {
+                        const uint2 u = lds64(get_hi + s * stage_bytes + at[j]);
+                        hi[2 * j] = u.x, hi[2 * j + 1] = u.y;
                     }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&act_empty[s]);
-                    if (++s == stages) s = 0, ph ^= 1;
                 }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-#pragma unroll
-                    for (int o = 4; o > 0; o >>= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
-                    if ((lane & 7) == 0 && 4 * j + (lane >> 3) < per_warp) sum_q[e * per_warp + 4 * j + (lane >> 3)] = sum[j];
-                }
-                asm volatile("bar.sync 1, %0;" ::"n"(32 * kGtEpiWarps) : "memory");
-            } else {
-                for (int kb = 0; kb < kblocks; ++kb) {
-                    if (ok && !mbar_wait(&act_full[s], ph, 86)) ok = false, *fail = 1;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&act_empty[s]);
-                    if (++s == stages) s = 0, ph ^= 1;
-                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&empty[s]);
+                uint32_t o[32];
+                gt_operands<LV>(w, hi, o);
+                if (ok) ok = mbar_wait_near(&a_empty[mat * kGtRing + turn], a_ph, 88);
+                tc_fence_after();
+                tc_st32(put + turn * 64, o);
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&a_full[mat * kGtRing + turn]);
+                if (++s == stages) s = 0, ph ^= 1;
+                if ((turn ^= 1) == 0) a_ph ^= 1;
             }
-            if (ok && !mbar_wait(d_full, count & 1, 87)) ok = false, *fail = 1;
+            if (!ok) *fail = 1;
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kGtExpanders) : "memory");      // the scales are there
+            if (ok && !mbar_wait_near(d_full, count & 1, 89)) ok = false, *fail = 1;
             if (ok) {
                 tc_fence_after();
                 const int n = n0 + quarter * 32 + lane;
                 float sg = 0.0f, su = 0.0f;
                 if (n < p.N) sg = __ldg(p.w[0].s_n + n), su = __ldg(p.w[1].s_n + n);
                 const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-                for (int c = 16 * eg; c < rows; c += 32) {
-                    int v[2][16];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t x[16];
-                        tc_ld16(lanes + i * sets * ntok + c, x);
+                // a loop of eight tokens a trip, not more: code that runs once has to be fetched first, which took longer than running it
+#pragma unroll 1
+                for (int c = 8 * (e >> 2); c < rows; c += 8 * (kGtExpanders / 4)) {
+                    int v[2][8];
+                    {
+                        uint32_t x[8], y[8];
+                        gt_ld8(lanes + c, x);
+                        gt_ld8(lanes + ntok + c, y);
                         tc_wait_ld();
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) v[i][j] = static_cast<int>(x[j]);
-                        for (int k = 1; k < sets; ++k) {
-                            tc_ld16(lanes + (i * sets + k) * ntok + c, x);
-                            tc_wait_ld();
+                        for (int j = 0; j < 8; ++j) v[0][j] = static_cast<int>(x[j]), v[1][j] = static_cast<int>(y[j]);
+                    }
+                    float h[8];
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) v[i][j] += static_cast<int>(x[j]);
-                        }
+                    for (int j = 0; j < 8; ++j) {
+                        v[0][j] >>= gt_shift<LV>(), v[1][j] >>= gt_shift<LV>();
+                        h[j] = gated_value(v[0][j], v[1][j], scale[c + j], sg, su, act);
                     }
                     if (n < p.N) {
+                        const size_t at = static_cast<size_t>(m0 + c) * p.N + n;
+                        if (p.h_bf16) {
+                            uint16_t* to = static_cast<uint16_t*>(p.H) + at;
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            if (c + j < rows) {
-                                const int m = m0 + c + j, sq = LV == QIFT_LEVELS_POT ? 0 : sum_q[c + j];
-                                gated_store(p, static_cast<size_t>(m) * p.N + n, gt_result<LV>(v[0][j], sq), gt_result<LV>(v[1][j], sq),
-                                            __ldg(p.s_a + m), sg, su);
-                            }
+                            for (int j = 0; j < 8; ++j, to += p.N)
+                                if (c + j < rows) *to = f32_to_bf16_bits(h[j]);
+                        } else {
+                            float* to = static_cast<float*>(p.H) + at;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j, to += p.N)
+                                if (c + j < rows) *to = h[j];
                         }
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            if (p.w[i].acc_debug) {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    if (c + j < rows) p.w[i].acc_debug[at + static_cast<size_t>(j) * p.N] = v[i][j];
+                            }
                     }
                 }
                 tc_fence_before();
             }
-            if constexpr (LV != QIFT_LEVELS_POT)
-                asm volatile("bar.sync 1, %0;" ::"n"(32 * kGtEpiWarps) : "memory");   // the sums have been read
-            __syncwarp();
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kGtExpanders) : "memory");       // and have been read
             if (lane == 0) mbar_arrive(d_empty);
         }
-    } else {
-        // ------------------------------------------------------------------ expanders
-        const int e = warp - 11, q = warp & 3, mat = e >> 2;           // q: the lane quarter this warp's tcgen05.st can reach
-        const uint32_t ring = smem_u32(words + e * SLOTS * SLOT);
-        const unsigned char* base = reinterpret_cast<const unsigned char*>(p.w[mat].packed);
-        const size_t rb_bytes = static_cast<size_t>(pitch) * WB;
-        const int row_blocks = (p.N + 15) / 16;
-        int f_item = blockIdx.x, f_slice = 0;
-        auto fetch = [&](int slot) {                                   // the next slice -> ring slot; always commits a group
-            if (f_item < items) {
-                const int rb0 = (f_item / tp.blocks) * 8 + 2 * q;
-                const unsigned char* src = base + rb0 * rb_bytes + static_cast<size_t>(f_slice) * (16 * WB) + lane * 16;
-#pragma unroll
-                for (int h = 0; h < 4; ++h)                            // row h * 8 + lane / 4: 16-byte pieces exclusive-ored by (row >> 1) & 3
-                    if (rb0 + (h >> 1) < row_blocks)
-                        cp_async16(ring + slot * SLOT + (h * 8 + (lane >> 2)) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4),
-                                   src + (h >> 1) * rb_bytes + (h & 1) * 512);
-                if constexpr (LV == QIFT_LEVELS_INT3) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)                        // third bits of eight rows and the eight behind them: as they stand
-                        if (rb0 + h < row_blocks) cp_async16(ring + slot * SLOT + 2048 + h * 512 + lane * 16, src + h * rb_bytes + 1024);
-                }
-                if (++f_slice == slices) f_slice = 0, f_item += gridDim.x;
-            }
-            cp_async_commit();
-        };
-        for (int s = 0; s < SLOTS; ++s) fetch(s);
-        int slot = 0, a_slot = 0;
-        uint32_t a_ph = 1;
-        bool ok = true;
-        for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
-            const bool row_valid = (item / tp.blocks) * 8 + 2 * q + (lane >> 4) < row_blocks;
-            for (int sl = 0; sl < slices && ok; ++sl) {
-                cp_async_wait<SLOTS - 1>();
-                __syncwarp();
-                uint32_t w[16], hi[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (row_valid) v = lds128(ring + slot * SLOT + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4));
-                    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
-                    if constexpr (LV == QIFT_LEVELS_INT3) {
-                        uint2 u = make_uint2(0, 0);
-                        if (row_valid) u = lds64(ring + slot * SLOT + 2048 + (lane >> 4) * 512 + ((lane & 7) * 4 + i) * 16 + ((lane >> 3) & 1) * 8);
-                        hi[2 * i] = u.x, hi[2 * i + 1] = u.y;
-                    }
-                }
-                __syncwarp();                                          // every lane has read the slot before it is filled again
-                fetch(slot);
-                if (++slot == SLOTS) slot = 0;
-#pragma unroll
-                for (int j = 0; j < KPS; ++j) {
-                    if (!mbar_wait(&a_empty[mat * kGtRing + a_slot], a_ph, 88)) {
-                        *fail = 1, ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    uint32_t o[32];
-                    gt_operands<LV>(w + (PER == 16 ? 8 * j : 0), hi + 4 * j, o);
-                    tc_st32(tmem + (static_cast<uint32_t>(q * 32) << 16) + kGtOperands + (mat * kGtRing + a_slot) * 32, o);
-                    tc_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&a_full[mat * kGtRing + a_slot]);
-                    if (++a_slot == kGtRing) a_slot = 0, a_ph ^= 1;
-                }
-            }
-        }
-        cp_async_wait<0>();
     }
 
     tc_fence_before();

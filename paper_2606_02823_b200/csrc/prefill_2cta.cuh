@@ -314,45 +314,61 @@ gemm_i8_pair_kernel(const __grid_constant__ PairParams p) {
             const float sa = (m < p.M) ? p.s_a[m] : 0.0f;
             if constexpr (GATED) {
                 const PairSegment& U = p.seg[1];
+                const GateFunction act(p.act);
+#pragma unroll 1
                 for (int c0 = 0; c0 < BN / 2; c0 += 16) {
                     uint32_t vg[16], vu[16];
                     const uint32_t at = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BN + c0;
                     tc_ld16(at, vg);
                     tc_ld16(at + BN / 2, vu);
-                    tc_wait_ld();
                     const int n = g * (BN / 2) + c0;
-                    if (m >= p.M || n >= N) continue;
-                    const size_t o = static_cast<size_t>(m) * N + n;
-                    const int live = min(16, N - n);
-                    if (S.acc_debug)
-                        for (int j = 0; j < live; ++j) S.acc_debug[o + j] = static_cast<int>(vg[j]);
-                    if (U.acc_debug)
-                        for (int j = 0; j < live; ++j) U.acc_debug[o + j] = static_cast<int>(vu[j]);
-                    float h[16];
+                    const bool whole = n + 16 <= N && (N & 7) == 0;
+                    float sg[16], su[16];
+                    if (whole) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (j < live)
-                            h[j] = gated_value(static_cast<int>(vg[j]), static_cast<int>(vu[j]), sa, __ldg(S.s_n + n + j), __ldg(U.s_n + n + j), p.act);
-                    if (live == 16 && (N & 7) == 0) {
-                        if (p.y_bf16) {
-                            uint32_t b[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                b[j] = static_cast<uint32_t>(f32_to_bf16_bits(h[2 * j])) | (static_cast<uint32_t>(f32_to_bf16_bits(h[2 * j + 1])) << 16);
-                            uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.H) + o);
-                            dst[0] = make_uint4(b[0], b[1], b[2], b[3]), dst[1] = make_uint4(b[4], b[5], b[6], b[7]);
-                        } else {
-                            float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.H) + o);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) dst[j] = make_float4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+                        for (int j = 0; j < 4; ++j) {
+                            const float4 a = __ldg(reinterpret_cast<const float4*>(S.s_n + n) + j), b = __ldg(reinterpret_cast<const float4*>(U.s_n + n) + j);
+                            sg[4 * j] = a.x, sg[4 * j + 1] = a.y, sg[4 * j + 2] = a.z, sg[4 * j + 3] = a.w;
+                            su[4 * j] = b.x, su[4 * j + 1] = b.y, su[4 * j + 2] = b.z, su[4 * j + 3] = b.w;
                         }
                     } else {
 #pragma unroll
+                        for (int j = 0; j < 16; ++j) sg[j] = n + j < N ? __ldg(S.s_n + n + j) : 0.0f, su[j] = n + j < N ? __ldg(U.s_n + n + j) : 0.0f;
+                    }
+                    tc_wait_ld();
+                    float h[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) h[j] = gated_value(static_cast<int>(vg[j]), static_cast<int>(vu[j]), sa, sg[j], su[j], act);
+                    if (m >= p.M) continue;
+                    const size_t o = static_cast<size_t>(m) * N + n;
+                    if (whole && p.y_bf16) {
+                        uint32_t b[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            b[j] = static_cast<uint32_t>(f32_to_bf16_bits(h[2 * j])) | (static_cast<uint32_t>(f32_to_bf16_bits(h[2 * j + 1])) << 16);
+                        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.H) + o);
+                        dst[0] = make_uint4(b[0], b[1], b[2], b[3]), dst[1] = make_uint4(b[4], b[5], b[6], b[7]);
+                    } else if (whole) {
+                        float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.H) + o);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) dst[j] = make_float4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+                    } else {
+#pragma unroll
                         for (int j = 0; j < 16; ++j)
-                            if (j < live) {
+                            if (n + j < N) {
                                 if (p.y_bf16) static_cast<uint16_t*>(p.H)[o + j] = f32_to_bf16_bits(h[j]);
                                 else static_cast<float*>(p.H)[o + j] = h[j];
                             }
+                    }
+                    if (S.acc_debug) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (n + j < N) S.acc_debug[o + j] = static_cast<int>(vg[j]);
+                    }
+                    if (U.acc_debug) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (n + j < N) U.acc_debug[o + j] = static_cast<int>(vu[j]);
                     }
                 }
             } else

@@ -2001,6 +2001,20 @@ int run_gated_stream(GatedParams p, cudaStream_t st) {
     return QIFT_OK;
 }
 
+// Packed words as rows of 64 bytes: [row blocks][slices x rows of a slice][64], a box of eight row blocks and `slices` slices, whose 16-byte
+// pieces are exclusive-ored by (row >> 1) & 3 in shared memory; what lies beyond the matrix arrives as zeros.
+bool make_words_map(CUtensorMap* map, const uint32_t* packed, int N, int pitch, int slice_rows, int slices) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t rows = static_cast<cuuint64_t>(pitch / 16) * slice_rows;
+    const cuuint64_t dims[3] = {64, rows, static_cast<cuuint64_t>((N + 15) / 16)};
+    const cuuint64_t strides[2] = {64, rows * 64};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(slices * slice_rows), 8};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint32_t*>(packed), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int LV>
 int run_gated_tc(const GatedParams& p, cudaStream_t st) {
     GatedTcParams tp{};
@@ -2008,13 +2022,15 @@ int run_gated_tc(const GatedParams& p, cudaStream_t st) {
     tp.ntok = ((p.M + tp.blocks - 1) / tp.blocks + 15) / 16 * 16;
     tp.blocks = (p.M + tp.ntok - 1) / tp.ntok;
     tp.stages = gt_stages(LV, tp.ntok);
-    CUtensorMap map;
-    if (!make_i8_map(&map, p.q_a, p.M, p.K, tp.ntok)) return QIFT_ERR_CUDA;
+    GatedTcMaps maps;
+    if (!make_i8_map(&maps.act, p.q_a, p.M, p.K, tp.ntok)) return QIFT_ERR_CUDA;
+    for (int i = 0; i < 2; ++i)
+        if (!make_words_map(&maps.words[i], p.w[i].packed, p.N, packed_pitch(p.K, LV), gt_slice_rows(LV), gt_slices(LV))) return QIFT_ERR_CUDA;
     auto kernel = gated_tc_kernel<LV>;
     const cudaError_t e = allow_smem(kernel, kGtSmem);
     if (e != cudaSuccess) return cuda_status(e);
     const long long items = static_cast<long long>((p.N + kGtRows - 1) / kGtRows) * tp.blocks;
-    return cuda_status(launch_pdl(kernel, dim3(static_cast<unsigned>(std::min<long long>(items, sm_count()))), dim3(kGtThreads), kGtSmem, st, map, tp));
+    return cuda_status(launch_pdl(kernel, dim3(static_cast<unsigned>(std::min<long long>(items, sm_count()))), dim3(kGtThreads), kGtSmem, st, maps, tp));
 }
 
 template <int LV>

@@ -1,16 +1,15 @@
 // The gated products of up to sixteen token rows: a stream of packed weights.
 //
 // Bound by HBM: 2 N K bits / 8 bytes of codes (4096 -> 14336 in two bits: 29.4 MB, 4.6 us at the copy rate) against next to nothing
-// else.  One call has few 128-row items, so the unit here is small: 16 channels of both matrices, 128 words deep (2 x 8 KB, two bulk
-// copies), and a CTA's share of a call is about what its shared memory holds -- nearly all of it is asked for before the CTA
-// does anything else, the wait for the preceding kernel included.
+// else.  One call has few rows of tiles (896 of 16 channels there), so hand-overs between warps are what has to be avoided: a pair of warps
+// takes a tile, one the gate's rows, one the other matrix's, each with a ring of its own that it fills by bulk copies itself, 64
+// words deep (4 KB) a slot.  A CTA's share of a call is about what its shared memory holds, so nearly all of it is asked for before
+// anything else happens, the wait for the preceding kernel included.  Packed words become operands with one logic operation each
+// (mma_tile_step) against activations that stand in shared memory for the whole kernel; at the end of a tile one warp of the pair hands its
+// sums to the other (64-thread barrier, two buffers by turns), which writes h.
 //
-//   warp 16     producer: fills a ring of units
-//   warps 0-15  one (matrix, 16-word slice) of a unit each: packed words become operands with one logic operation each
-//               (mma_tile_step) against activations that stand in shared memory for the whole kernel
 // The CTA itself turns q_a into the operands' order (even planes times four, or table order) and sums each token's values, so there is no
-// launch before this one and no workspace.  After a tile's last chunk the eight slices' sums of each matrix meet in shared memory (two
-// buffers by turns, one barrier a tile): an integer per output, since the place values divide each warp's sum exactly.
+// launch before this one and no workspace.
 #pragma once
 
 #include "common.cuh"
@@ -21,21 +20,22 @@
 
 namespace qift {
 
-constexpr int kGsWarps = 16, kGsConsumers = 32 * kGsWarps, kGsThreads = kGsConsumers + 32;
+constexpr int kGsPairs = 8, kGsThreads = 64 * kGsPairs;
 constexpr int kGsMaxM = 16;
+constexpr int kGsWords = 64, kGsMaxSlots = 8;               // packed words per row of a slot; slots of a warp
 constexpr int kGsSmem = 226 * 1024;
 
-__host__ __device__ constexpr int gs_unit_bytes(int lv) { return 2 * kChunkWords * tile_word_bytes(lv); }
-// activations, two reduction buffers, sums and scales of the tokens, and a flag
+__host__ __device__ constexpr int gs_slot_bytes(int lv) { return kGsWords * tile_word_bytes(lv); }
+__host__ __device__ constexpr int gs_exchange_bytes(int M) { return 2 * 32 * (M > 8 ? 8 : 4) * 4; }   // of a pair: two buffers
+// activations, and the tokens' sums and a flag; then, per pair, the exchange, two rings and their barriers
 __host__ __device__ inline size_t gs_fixed_bytes(int M, int K, int lv) {
-    return static_cast<size_t>(M) * packed_pitch(K, lv) * codes_per_word(lv) + 2 * static_cast<size_t>(kGsWarps) * M * 64 + 256;
+    return static_cast<size_t>(M) * packed_pitch(K, lv) * codes_per_word(lv) + 128;
 }
-__host__ __device__ inline int gs_stages(int M, int K, int lv) {
-    const size_t fixed = gs_fixed_bytes(M, K, lv);
-    return fixed >= kGsSmem ? 0 : static_cast<int>((kGsSmem - fixed) / (gs_unit_bytes(lv) + 16));
+__host__ __device__ inline size_t gs_pair_bytes(int M, int lv, int slots) {
+    return gs_exchange_bytes(M) + 2 * static_cast<size_t>(slots) * (gs_slot_bytes(lv) + 8);
 }
 
-// A warp's sum of level * q over its slices, up to the correction by sum q (gs_result).
+// A warp's sum of level * q, up to the correction by sum q (gs_result).
 template <int LV, int NACC>
 __device__ __forceinline__ int gs_partial(const int (&v)[NACC]) {
     if constexpr (LV == QIFT_LEVELS_POT) return v[0];           // table lookup: the operands were the levels
@@ -52,63 +52,56 @@ __device__ __forceinline__ int gs_result(int S, int sum_q) {
 
 template <int LV, int NT>
 __global__ void __launch_bounds__(kGsThreads, 1)
-gated_stream_kernel(const __grid_constant__ GatedParams p, int stages) {
+gated_stream_kernel(const __grid_constant__ GatedParams p, int pairs, int slots) {
     constexpr int PER = codes_per_word(LV), NPL = PER / 4;
     constexpr int NACC = LV == QIFT_LEVELS_POT ? 1 : DecodeTraits<LV>::NACC;
-    constexpr int WB = tile_word_bytes(LV), HALF = kChunkWords * WB, UNIT = 2 * HALF;
+    constexpr int WB = tile_word_bytes(LV), SLOT = gs_slot_bytes(LV);
     constexpr int SLICE = 16 * PER;                             // activation bytes of a slice and token
+    constexpr int KS = NT == 1 && LV != QIFT_LEVELS_INT3 ? 2 : 1;   // accumulators by turns: shorter chains of products
     extern __shared__ __align__(128) unsigned char smem[];
     const int M = p.M, pitch = packed_pitch(p.K, LV), slices = pitch / 16;
-    const int tiles = (p.N + 15) / 16, chunks = (pitch + kChunkWords - 1) / kChunkWords;
-    unsigned char* ring = smem;
-    unsigned char* act = ring + static_cast<size_t>(stages) * UNIT;               // [slice][token][SLICE], pieces permuted (swizzled_group)
-    int* red = reinterpret_cast<int*>(act + static_cast<size_t>(M) * slices * SLICE);   // [2][warp][token][row]
-    uint64_t* full = reinterpret_cast<uint64_t*>(red + 2 * kGsWarps * M * 16);
-    uint64_t* empty = full + stages;
-    int* sum_q = reinterpret_cast<int*>(empty + stages);                          // [16]
-    volatile int* fail = sum_q + kGsMaxM;
+    const int tiles = (p.N + 15) / 16, chunks = (pitch + kGsWords - 1) / kGsWords;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int pair = warp >> 1, mat = warp & 1;
+    unsigned char* ring = smem + static_cast<size_t>(warp) * slots * SLOT;
+    unsigned char* act = smem + static_cast<size_t>(2 * pairs) * slots * SLOT;    // [slice][token][SLICE], pieces permuted (swizzled_group)
+    int* exchange = reinterpret_cast<int*>(act + static_cast<size_t>(M) * slices * SLICE) + pair * (gs_exchange_bytes(M) / 4);
+    uint64_t* full = reinterpret_cast<uint64_t*>(act + static_cast<size_t>(M) * slices * SLICE + pairs * gs_exchange_bytes(M)) + warp * slots;
+    int* sum_q = reinterpret_cast<int*>(full - warp * slots + 2 * pairs * slots);  // [16]
+    volatile int* fail = sum_q + kGsMaxM;
 
     pdl_launch_dependents();
-    if (tid == 0) {
-        for (int s = 0; s < stages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], kGsWarps);
-        mbar_fence_init();
-        *fail = 0;
-    }
-    if (tid < kGsMaxM) sum_q[tid] = 0;
-    __syncthreads();
-
-    if (warp == kGsWarps) {
-        // ---------------------------------------------------------------- producer: the weights depend on no kernel before this one
-        int s = 0, k = 0;
-        uint32_t ph = 0;
-        for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
-            const size_t tile = static_cast<size_t>(t) * pitch * WB;
-            for (int c = 0; c < chunks; ++c, ++k) {
-                if (k >= stages && !mbar_wait_near(&empty[s], ph, 80)) {
-                    *fail = 1;
-                    return;
-                }
-                if (elect_one()) {
-                    const uint32_t bytes = min(kChunkWords, pitch - c * kChunkWords) * WB;
-                    mbar_expect_tx(&full[s], 2 * bytes);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        bulk_g2s(ring + s * UNIT + i * HALF, reinterpret_cast<const unsigned char*>(p.w[i].packed) + tile + static_cast<size_t>(c) * HALF,
-                                 bytes, &full[s]);
-                }
-                __syncwarp();
-                if (++s == stages) s = 0, ph ^= (k >= stages);
-            }
+    // this warp's copies run over its tiles, chunk by chunk
+    int f_tile = blockIdx.x + pair * gridDim.x, f_chunk = 0;
+    const int step = pairs * gridDim.x;
+    const unsigned char* base = reinterpret_cast<const unsigned char*>(p.w[mat].packed);
+    auto fetch = [&](int slot) {                                // one thread: the next chunk -> slot
+        if (f_tile < tiles) {
+            const uint32_t bytes = min(kGsWords, pitch - f_chunk * kGsWords) * WB;
+            mbar_expect_tx(&full[slot], bytes);
+            bulk_g2s(ring + slot * SLOT, base + static_cast<size_t>(f_tile) * pitch * WB + static_cast<size_t>(f_chunk) * SLOT, bytes, &full[slot]);
         }
-        return;
+    };
+    auto advance = [&]() {
+        if (++f_chunk == chunks) f_chunk = 0, f_tile += step;
+    };
+    if (pair < pairs) {
+        if (elect_one()) {
+            for (int s = 0; s < slots; ++s) mbar_init(&full[s], 1);
+            mbar_fence_init();
+        }
+        __syncwarp();
+        for (int s = 0; s < slots; ++s, advance())              // the weights depend on no kernel before this one
+            if (elect_one()) fetch(s);
     }
-
-    // -------------------------------------------------------------------- consumers: first the activations
+    if (tid <= kGsMaxM) sum_q[tid] = 0;                         // and the flag behind them
+    __syncthreads();
     pdl_wait();
+
+    // -------------------------------------------------------------------- the activations
     {
         const int pieces = slices * (SLICE / 16), all = M * pieces;
-        for (int i0 = 0; i0 < all; i0 += kGsConsumers) {         // eight neighbouring threads are always at the same token
+        for (int i0 = 0; i0 < all; i0 += kGsThreads) {          // eight neighbouring threads are always at the same token
             const int i = i0 + tid, m = i / pieces, q = i - m * pieces;
             int sum = 0;
             if (i < all) {
@@ -129,73 +122,118 @@ gated_stream_kernel(const __grid_constant__ GatedParams p, int stages) {
                 const int sl = q / (SLICE / 16), piece = q - sl * (SLICE / 16);
                 *reinterpret_cast<uint4*>(act + (static_cast<size_t>(sl) * M + m) * SLICE + 16 * swizzled_group(piece, m, PER == 16)) = v;
             }
+            if constexpr (LV != QIFT_LEVELS_POT && LV != QIFT_LEVELS_INT3) {
 #pragma unroll
-            for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            if ((lane & 7) == 0 && i < all) atomicAdd(&sum_q[m], sum);
+                for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if ((lane & 7) == 0 && i < all) atomicAdd(&sum_q[m], sum);
+            }
         }
     }
-    const int e_row = tid & 15, e_m = tid >> 4;                  // this thread's output of a tile
-    const float e_sa = e_m < M ? p.s_a[e_m] : 0.0f;
-    asm volatile("bar.sync 1, %0;" ::"n"(kGsConsumers) : "memory");
-    const int e_sq = e_m < M ? sum_q[e_m] : 0;
+    __syncthreads();
+    if (pair >= pairs) return;
 
-    const int g = lane >> 2, cq = lane & 3, mat = warp >> 3, slice = warp & 7;
-    int tok[NT];
+    // -------------------------------------------------------------------- a tile's rows of one matrix
+    const int g = lane >> 2, cq = lane & 3;
+    uint32_t q_at[NT][NPL];                                     // the lane's pieces of a slice; columns beyond M repeat the last token, nobody reads them
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) tok[nt] = min(nt * 8 + g, M - 1);   // columns beyond M repeat the last token, nobody reads them
+    for (int nt = 0; nt < NT; ++nt) {
+        const int tok = min(nt * 8 + g, M - 1);
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) q_at[nt][i] = smem_u32(act) + tok * SLICE + 16 * swizzled_group(NPL * cq + i, tok, PER == 16);
+    }
+    float sa[NT][2];
+    int sq[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int m = min(nt * 8 + 2 * cq + j, M - 1);
+            sa[nt][j] = p.s_a[m], sq[nt][j] = sum_q[m];
+        }
+    const GateFunction function(p.act);
     bool ok = true;
     int s = 0;
     uint32_t ph = 0, turn = 0;
-    for (int t = blockIdx.x; t < tiles; t += gridDim.x, turn ^= 1) {
-        const int n = t * 16 + e_row;
-        const bool on = e_m < M && n < p.N;
-        float sg = 0.0f, su = 0.0f;
-        if (on) sg = __ldg(p.w[0].s_n + n), su = __ldg(p.w[1].s_n + n);
-        int acc[NT][NACC][4] = {};
+    for (int t = blockIdx.x + pair * gridDim.x; t < tiles; t += step, turn ^= 1) {
+        float sg[2] = {}, su[2] = {};
+        if (mat == 0) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int n = t * 16 + g + 8 * j;
+                if (n < p.N) sg[j] = __ldg(p.w[0].s_n + n), su[j] = __ldg(p.w[1].s_n + n);
+            }
+        }
+        int acc[KS][NT][NACC][4] = {};
         for (int c = 0; c < chunks; ++c) {
-            // a wait that has run out once is not tried again; the warp goes on to the barriers that the others wait at
-            if (ok && !mbar_wait_near(&full[s], ph, 81)) ok = false, *fail = 1;
-            const int at = c * (kChunkWords / 16) + slice;       // the slice among the row's
-            if (ok && at < slices) {
-                const uint32_t w = smem_u32(ring + s * UNIT + mat * HALF) + slice * (16 * WB) + lane * 16;
-                const uint32_t q = smem_u32(act) + static_cast<uint32_t>(at) * M * SLICE;
+            // a wait that has run out once is not tried again; the warp goes on to the barriers that its partner waits at
+            if (ok) ok = mbar_wait_near(&full[s], ph, 81);
+            const uint32_t w0 = smem_u32(ring + s * SLOT) + lane * 16;
+            auto slice = [&](int sl, auto ks) {
+                const uint32_t w = w0 + sl * (16 * WB), q = static_cast<uint32_t>((c * (kGsWords / 16) + sl) * M * SLICE);
                 uint32_t qb[NT][4 * NPL];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < NPL; ++i) {
-                        const uint4 v = lds128(q + tok[nt] * SLICE + 16 * swizzled_group(NPL * cq + i, tok[nt], PER == 16));
+                        const uint4 v = lds128(q_at[nt][i] + q);
                         qb[nt][4 * i] = v.x, qb[nt][4 * i + 1] = v.y, qb[nt][4 * i + 2] = v.z, qb[nt][4 * i + 3] = v.w;
                     }
                 const uint4 wa = lds128(w), wb = lds128(w + 512);
-                if constexpr (LV == QIFT_LEVELS_INT3) mma_tile_step_int3<NT>(acc, wa, wb, lds128(w + 1024), qb);
-                else if constexpr (LV == QIFT_LEVELS_POT) mma_tile_step_pot_lut<NT>(acc, wa, wb, qb);
-                else mma_tile_step<LV, NT, true>(acc, wa, wb, qb);
+                constexpr int k = decltype(ks)::value;
+                if constexpr (LV == QIFT_LEVELS_INT3) mma_tile_step_int3<NT>(acc[k], wa, wb, lds128(w + 1024), qb);
+                else if constexpr (LV == QIFT_LEVELS_POT) mma_tile_step_pot_lut<NT>(acc[k], wa, wb, qb);
+                else mma_tile_step<LV, NT, true>(acc[k], wa, wb, qb);
+            };
+            const int here = min(kGsWords / 16, slices - c * (kGsWords / 16));
+            if (here == kGsWords / 16) {
+#pragma unroll
+                for (int sl = 0; sl < kGsWords / 16; sl += 2) {
+                    slice(sl, std::integral_constant<int, 0>{});
+                    slice(sl + 1, std::integral_constant<int, KS - 1>{});
+                }
+            } else {
+                for (int sl = 0; sl < here; ++sl) slice(sl, std::integral_constant<int, 0>{});
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&empty[s]);
-            if (++s == stages) s = 0, ph ^= 1;
+            __syncwarp();                                       // every lane has read the slot before it is filled again
+            if (ok && elect_one()) fetch(s);
+            advance();
+            if (++s == slots) s = 0, ph ^= 1;
         }
-        int* mine = red + (turn * kGsWarps + warp) * M * 16;
+        int sum[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int m = nt * 8 + 2 * cq + (i & 1);
                 int v[NACC];
 #pragma unroll
-                for (int a = 0; a < NACC; ++a) v[a] = acc[nt][a][i];
-                if (m < M) mine[m * 16 + g + ((i & 2) ? 8 : 0)] = gs_partial<LV, NACC>(v);
+                for (int a = 0; a < NACC; ++a) v[a] = KS == 2 ? acc[0][nt][a][i] + acc[KS - 1][nt][a][i] : acc[0][nt][a][i];
+                sum[nt][i] = gs_result<LV>(gs_partial<LV, NACC>(v), sq[nt][i & 1]);
             }
-        asm volatile("bar.sync 1, %0;" ::"n"(kGsConsumers) : "memory");
-        if (on && !*fail) {
-            const int* from = red + turn * kGsWarps * M * 16 + e_m * 16 + e_row;
-            int S[2] = {};
+        int* buffer = exchange + turn * 32 * NT * 4 + lane;
+        if (mat == 1) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int w = 0; w < 8; ++w) S[i] += from[(8 * i + w) * M * 16];
-            gated_store(p, static_cast<size_t>(e_m) * p.N + n, gs_result<LV>(S[0], e_sq), gs_result<LV>(S[1], e_sq), e_sa, sg, su);
+                for (int i = 0; i < 4; ++i) buffer[(nt * 4 + i) * 32] = sum[nt][i];
+        }
+        if (!ok) *fail = 1;
+        asm volatile("bar.sync %0, 64;" ::"r"(1 + pair) : "memory");
+        if (mat == 0 && !*fail) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int m = nt * 8 + 2 * cq + (i & 1), n = t * 16 + g + 8 * (i >> 1);
+                    const int up = buffer[(nt * 4 + i) * 32];
+                    const float h = gated_value(sum[nt][i], up, sa[nt][i & 1], sg[i >> 1], su[i >> 1], function);
+                    if (m < M && n < p.N) {
+                        const size_t at = static_cast<size_t>(m) * p.N + n;
+                        if (p.h_bf16) static_cast<uint16_t*>(p.H)[at] = f32_to_bf16_bits(h);
+                        else static_cast<float*>(p.H)[at] = h;
+                        if (p.w[0].acc_debug) p.w[0].acc_debug[at] = sum[nt][i];
+                        if (p.w[1].acc_debug) p.w[1].acc_debug[at] = up;
+                    }
+                }
         }
     }
 }

@@ -7,7 +7,9 @@ missing, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+import struct
 
 import torch
 
@@ -830,26 +832,33 @@ def qift_qk_norm_rope(q, k, position, inv_freq, q_weight=None, k_weight=None, ep
 
 
 # ---------------------------------------------------------------------------------------- gated feed-forward block
+@functools.cache
 def qift_gated_levels_min_rows() -> int:
     """Token rows from which on the gated calls need a levels buffer."""
     return int(lib().qift_gated_levels_min_rows())
 
 
-def _gated(X, M, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready):
-    """What the gated calls have in common: (result, accumulators, descriptors of the two outputs, levels buffer, its bytes)."""
+_GATE_UP = struct.Struct("@PPPPiiPPPPii")      # two qift_linear_output
+
+
+def _gated(fn, X, dtype, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation, before, after):
+    """What the gated calls have in common: fn(*before, descriptors of the two outputs, activation, result, *after, levels buffer, ...)."""
     (pg, sg), (pu, su) = gate, up
-    N = sg.shape[0]
-    _same_device(X, pg, sg, pu, su, out, levels_buf)
+    M, N = X.shape[0], sg.shape[0]
     if out is None:
         out = torch.empty((M, N), dtype=out_dtype, device=X.device)
-    accs = [torch.empty((M, N), dtype=torch.int32, device=X.device) if want_acc else None for _ in range(2)]
-    arr = _outputs_array([gate, up], [out, out], accs)
+    accs = [torch.empty((M, N), dtype=torch.int32, device=X.device) for _ in range(2)] if want_acc else ()
     if levels_buf is None:
         assert not levels_ready
         if M >= qift_gated_levels_min_rows() and K % 16 == 0:
-            levels_buf = torch.empty(int(lib().qift_levels_bytes(K, ctypes.addressof(arr), 2)), dtype=torch.uint8, device=X.device)
+            levels_buf = torch.empty(qift_levels_bytes(K, [gate, up]), dtype=torch.uint8, device=X.device)
+    _same_device(X, pg, sg, pu, su, out, levels_buf)
+    f32, ag, au = torch.float32, *([a.data_ptr() for a in accs] or (0, 0))
+    outputs = _GATE_UP.pack(_on(pg, pg.dtype), _on(sg, f32), 0, ag, N, 0, _on(pu, pu.dtype), _on(su, f32), 0, au, su.shape[0], 0)
     buf = (None, 0) if levels_buf is None else _space(levels_buf)
-    return out, accs, arr, levels_buf, buf
+    ah, keep = _ahead_chain(ahead)
+    _call(X, fn, _on(X, dtype), *before, outputs, activation, _on(out, out.dtype, M, N), _float_type(out), *after, *buf, 1 if levels_ready else 0, ah)
+    return (out, *accs) if want_acc else out
 
 
 def qift_gated_linear(q_a, s_a, gate, up, levels: int, activation: int = ACT_SILU, out_dtype=torch.float32, out=None, want_acc: bool = False,
@@ -857,26 +866,22 @@ def qift_gated_linear(q_a, s_a, gate, up, levels: int, activation: int = ACT_SIL
     """q_a int8 [M, K], s_a fp32 [M], gate = up = (packed, s_n) -> h [M, N] = activation(gate product) * up product; with want_acc
     (h, gate accumulators, up accumulators).  levels_buf, levels_ready, ahead: as for qift_forward_multi."""
     M, K = q_a.shape
-    out, accs, arr, levels_buf, buf = _gated(q_a, M, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready)
     _same_device(q_a, s_a)
-    ah, keep = _ahead_chain(ahead)
-    _call(q_a, lib().qift_gated_linear, _on(q_a, torch.int8), _on(s_a, torch.float32), M, K, levels, ctypes.addressof(arr), activation,
-          _on(out, out.dtype, M, arr[0].N), _float_type(out), *buf, 1 if levels_ready else 0, ah)
-    return (out, *accs) if want_acc else out
+    assert s_a.numel() >= M, "a scale for every row"
+    return _gated(lib().qift_gated_linear, q_a, torch.int8, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation,
+                  (_on(s_a, torch.float32), M, K, levels), ())
 
 
 def qift_gated_forward(X, had_block: int, gate, up, levels: int, clip_ratio: float = 0.9, activation: int = ACT_SILU, out_dtype=torch.float32,
                        out=None, want_acc: bool = False, scratch=None, levels_buf=None, levels_ready: bool = False, ahead=None):
     """The same from X fp32 or bf16 [M, K], which is rotated and quantized first."""
     M, K = X.shape
-    out, accs, arr, levels_buf, buf = _gated(X, M, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready)
+    L = lib()
     if scratch is None:
-        scratch = torch.empty(lib().qift_gated_forward_scratch_bytes(M, K), dtype=torch.uint8, device=X.device)
+        scratch = torch.empty(L.qift_gated_forward_scratch_bytes(M, K), dtype=torch.uint8, device=X.device)
     _same_device(X, scratch)
-    ah, keep = _ahead_chain(ahead)
-    _call(X, lib().qift_gated_forward, _on(X, X.dtype), _float_type(X), M, K, had_block, clip_ratio, levels, ctypes.addressof(arr), activation,
-          _on(out, out.dtype, M, arr[0].N), _float_type(out), *_space(scratch), *buf, 1 if levels_ready else 0, ah)
-    return (out, *accs) if want_acc else out
+    return _gated(L.qift_gated_forward, X, X.dtype, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation,
+                  (_float_type(X), M, K, had_block, clip_ratio, levels), _space(scratch))
 
 
 # ---------------------------------------------------------------------------------------- resident decoded weights

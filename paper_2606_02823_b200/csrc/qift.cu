@@ -1971,18 +1971,25 @@ int run_qk_rope(const RopeParams& p, int lanes, dim3 grid, cudaStream_t st) {
 
 constexpr int kGatedLevelsMinM = 513;   // token rows from which on the codes are decoded to int8 first
 
-// Pairs of warps and slots of their rings: a pair for every tile that a CTA has, as many as eight, with what shared memory leaves them.
+// Slots of a warp's ring that shared memory has room for.
 inline int gs_slots(int M, int K, int lv, int pairs) {
     int slots = kGsMaxSlots;
     while (slots > 0 && gs_fixed_bytes(M, K, lv) + pairs * gs_pair_bytes(M, lv, slots) > kGsSmem) --slots;
     return slots;
 }
+// Pairs of warps: one for every tile that a CTA has, as many as eight, but four where more would leave a warp less than two slots.
+inline int gs_pairs(int M, int N, int K, int lv) {
+    const int tiles = (N + 15) / 16, grid = std::min(tiles, sm_count());
+    int pairs = std::min((tiles + grid - 1) / grid, kGsPairs);
+    while (pairs > 4 && gs_slots(M, K, lv, pairs) < 2) --pairs;
+    return pairs;
+}
 template <int LV, int NT>
 int launch_gated_stream(const GatedParams& p, cudaStream_t st) {
     auto kernel = gated_stream_kernel<LV, NT>;
     const int tiles = (p.N + 15) / 16, grid = std::min(tiles, sm_count()), chunks = (packed_pitch(p.K, LV) + kGsWords - 1) / kGsWords;
-    const int each = (tiles + grid - 1) / grid, pairs = std::min(each, kGsPairs);
-    const int slots = static_cast<int>(std::min<long long>(gs_slots(p.M, p.K, LV, pairs), static_cast<long long>((each + pairs - 1) / pairs) * chunks));
+    const int pairs = gs_pairs(p.M, p.N, p.K, LV), each = (tiles + grid * pairs - 1) / (grid * pairs);
+    const int slots = static_cast<int>(std::min<long long>(gs_slots(p.M, p.K, LV, pairs), static_cast<long long>(each) * chunks));
     const size_t smem = gs_fixed_bytes(p.M, p.K, LV) + pairs * gs_pair_bytes(p.M, LV, slots);
     const cudaError_t e = allow_smem(kernel, kGsSmem);
     if (e != cudaSuccess) return cuda_status(e);
@@ -1992,7 +1999,7 @@ template <int LV>
 int run_gated_stream(GatedParams p, cudaStream_t st) {
     // rows of long activations are taken in blocks that leave every warp two slots
     int block = std::min(p.M, kGsMaxM);
-    while (block > 1 && gs_slots(block, p.K, LV, kGsPairs) < 2) --block;
+    while (block > 1 && gs_slots(block, p.K, LV, gs_pairs(block, p.N, p.K, LV)) < 2) --block;
     const int M = p.M, size = p.h_bf16 ? 2 : 4;
     const GatedParams all = p;
     for (int m0 = 0; m0 < M; m0 += block) {

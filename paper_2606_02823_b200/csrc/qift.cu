@@ -2139,11 +2139,14 @@ int qift_kv4_pages_begin(const int32_t* rows, const int32_t* first, int R, int32
         (reinterpret_cast<uintptr_t>(slot) & 7u) != 0)
         return QIFT_ERR_ALIGNMENT;
     p.rows = rows, p.first = first, p.mask = mask, p.mask_words = mask_words, p.total = total, p.row_start = row_start;
-    p.position = position, p.slot = reinterpret_cast<long long*>(slot), p.lost = lost, p.fill_rows = total <= kPtFewRows;
+    p.position = position, p.slot = reinterpret_cast<long long*>(slot), p.lost = lost;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    rc = cuda_status(launch_pdl(pages_begin_kernel, dim3(1), dim3(kPtThreads), 0, st, p));
+    const bool few = total / page_tokens + 2ll * R <= 2 * kPtFewThreads * kPtPer;   // entries that the rows can fall into: two trips of one CTA
+    p.fill_rows = few && total <= kPtFewRows;
+    rc = few ? cuda_status(launch_pdl(pages_begin_kernel<1>, dim3(1), dim3(kPtFewThreads), 0, st, p))
+             : cuda_status(launch_pdl_cluster(pages_begin_kernel<kPtCluster>, kPtCluster, dim3(kPtCluster), dim3(kPtManyThreads), 0, st, p));
     if (rc != QIFT_OK || p.fill_rows) return rc;
-    const long long blocks = (total + 255ll) / 256, most = 8ll * sm_count();
+    const long long blocks = (total + 1023ll) / 1024, most = 8ll * sm_count();
     return cuda_status(launch_pdl(pages_rows_kernel, dim3(static_cast<unsigned>(std::min(blocks, most))), dim3(256), 0, st, p));
 }
 
@@ -2155,7 +2158,10 @@ int qift_kv4_pages_end(const int32_t* length, const int32_t* shared, int R, int3
     if (rc != QIFT_OK) return rc;
     if (!aligned4(length) || !aligned4(shared)) return QIFT_ERR_ALIGNMENT;
     p.length = length, p.shared = shared;
-    return cuda_status(launch_pdl(pages_end_kernel, dim3(1), dim3(kPtThreads), 0, static_cast<cudaStream_t>(stream), p));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (static_cast<long long>(R) * max_pages <= 2 * kPtFewThreads * kPtPer)
+        return cuda_status(launch_pdl(pages_end_kernel<1>, dim3(1), dim3(kPtFewThreads), 0, st, p));
+    return cuda_status(launch_pdl_cluster(pages_end_kernel<kPtCluster>, kPtCluster, dim3(kPtCluster), dim3(kPtManyThreads), 0, st, p));
 }
 
 int qift_qk_norm_rope(const void* Q, const void* K, int x_dtype, long long q_stride, long long k_stride, int total, int Hq, int H, int D,

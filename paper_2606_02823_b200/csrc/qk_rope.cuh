@@ -8,10 +8,14 @@
 // the heads of one row, as many at once as D / 16 threads each allow; it works the row's sines and cosines out once, rot / 2 of them
 // over its lanes, and keeps each lane's eight in registers over all heads.  Angles: the product in fp64 (position up to 2^31 times
 // an fp32 frequency), its whole turns taken off there, then sincospif of what is left -- far positions lose nothing.
-// Bound by HBM for many rows (every element in and out once); by latency for single tokens, whose rows are split over several warps.
+//
+// Bound by HBM for many rows, every element in and out once: 18000 rows of 32 + 8 heads in bf16 take 61 us (5.4 TB/s), 68 with norms; a lane
+// asks for the next heads' pieces before it works on these, and fp32 pairs are worked on two at a time (110 us before; pieces on
+// their way through shared memory, four trips ahead, were slower: 81).  By latency for single tokens.
 #pragma once
 
 #include "common.cuh"
+#include "kv4_paged.cuh"
 
 namespace qift {
 
@@ -28,117 +32,163 @@ struct RopeParams {
     const void* k_weight;
     const float* inv_freq;          // [rot / 2]
     const int32_t* position;        // [total]
-    int total, Hq, H, D, rot, near; // near: neighbouring dimensions are pairs
+    int total, Hq, H, D, rot;
     int parts;                      // warps that share a row's heads
     float eps;
 };
 
-// Eight consecutive elements as fp32 and back (one 16-byte access, or two).
+// Eight consecutive elements: as they are (one 16-byte access, or two), as four fp32 pairs, and back.
 template <bool BF16>
-__device__ __forceinline__ void rope_load(const void* base, long long at, float (&v)[8]) {
-    if constexpr (BF16) {
-        const uint4 w = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(u[i] << 16), v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    } else {
-        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
-        const float4 a = src[0], b = src[1];
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+struct RopePiece {
+    uint4 w[BF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const void* base, long long at) {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(base) + at * (BF16 ? 2 : 4));
+        w[0] = src[0];
+        if constexpr (!BF16) w[1] = src[1];
     }
-}
+    __device__ __forceinline__ void values(uint64_t (&v)[4]) const {
+        if constexpr (BF16) {
+            const uint32_t u[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = pair_of(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                v[2 * i] = pair_of(__uint_as_float(w[i].x), __uint_as_float(w[i].y));
+                v[2 * i + 1] = pair_of(__uint_as_float(w[i].z), __uint_as_float(w[i].w));
+            }
+        }
+    }
+};
 template <bool BF16>
-__device__ __forceinline__ void rope_store(void* base, long long at, const float (&v)[8]) {
+__device__ __forceinline__ void rope_store(void* base, long long at, const uint64_t (&v)[4]) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pair_to(v[i], f[2 * i], f[2 * i + 1]);
     if constexpr (BF16) {
         uint32_t u[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = f32_to_bf16_bits(v[2 * i]) | static_cast<uint32_t>(f32_to_bf16_bits(v[2 * i + 1])) << 16;
+        for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
         *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + at) = make_uint4(u[0], u[1], u[2], u[3]);
     } else {
         float4* dst = reinterpret_cast<float4*>(static_cast<float*>(base) + at);
-        dst[0] = make_float4(v[0], v[1], v[2], v[3]), dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+        dst[0] = make_float4(f[0], f[1], f[2], f[3]), dst[1] = make_float4(f[4], f[5], f[6], f[7]);
     }
 }
 
 // LANES: threads of a head, a power of two >= D / 16 (those beyond D / 16 have nothing to do).
-template <bool BF16, int LANES>
-__global__ void __launch_bounds__(kRopeThreads)
-qk_norm_rope_kernel(const RopeParams p) {
-    __shared__ float2 turns[kRopeWarps][kRopeMaxD / 2];   // cosine, sine of the warp's row
+template <bool BF16, int LANES, bool NORM, bool NEAR>
+__global__ void __launch_bounds__(kRopeThreads, 4)
+qk_norm_rope_kernel(const __grid_constant__ RopeParams p) {
+    constexpr int GROUPS = 32 / LANES;
+    constexpr int MAX_D = 16 * LANES;
+    __shared__ __align__(16) float2 turns[kRopeWarps][MAX_D / 4][2];     // of the warp's row: two cosines, two sines, so that a lane reads pairs
+    __shared__ __align__(16) float weights[2][NORM ? MAX_D : 4];         // of queries, of keys; ones where there is none
     pdl_launch_dependents();
     pdl_wait();
+    if constexpr (NORM) {
+        for (int i = threadIdx.x; i < 2 * p.D; i += kRopeThreads) {
+            const void* w = i < p.D ? p.q_weight : p.k_weight;
+            const int d = i < p.D ? i : i - p.D;
+            weights[i < p.D ? 0 : 1][d] = !w ? 1.0f : BF16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(w)[d]) << 16) : static_cast<const float*>(w)[d];
+        }
+        __syncthreads();
+    }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int c = lane % LANES, group = lane / LANES, groups = 32 / LANES;
+    const int c = lane % LANES, group = lane / LANES;
     const bool on = 16 * c < p.D;
     // the two pieces of the lane: pieces of the rotated part that are pairs of one another, or two of the rest
     const int pairs = p.rot / 2, heads = p.Hq + p.H;
     const bool turned = 16 * c < p.rot;
-    const int a = turned && !p.near ? 8 * c : 16 * c, b = turned && !p.near ? pairs + 8 * c : 16 * c + 8;
-    float wq[2][8], wk[2][8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) wq[0][i] = wq[1][i] = wk[0][i] = wk[1][i] = 1.0f;
-    if (on && p.q_weight) rope_load<BF16>(p.q_weight, a, wq[0]), rope_load<BF16>(p.q_weight, b, wq[1]);
-    if (on && p.k_weight) rope_load<BF16>(p.k_weight, a, wk[0]), rope_load<BF16>(p.k_weight, b, wk[1]);
+    const int a = turned && !NEAR ? 8 * c : 16 * c, b = turned && !NEAR ? pairs + 8 * c : 16 * c + 8;
     const float inv_d = 1.0f / p.D;
     const long long tasks = static_cast<long long>(p.total) * p.parts, step = static_cast<long long>(gridDim.x) * kRopeWarps;
-    for (long long task = blockIdx.x * static_cast<long long>(kRopeWarps) + warp; task < tasks; task += step) {
+    long long task = blockIdx.x * static_cast<long long>(kRopeWarps) + warp;
+    int position = task < tasks ? p.position[task / p.parts] : -1;
+    for (; task < tasks; task += step) {
         const int row = static_cast<int>(task / p.parts), part = static_cast<int>(task - static_cast<long long>(row) * p.parts);
-        const int position = p.position[row];
-        if (position < 0) continue;            // the row belongs to nobody
+        const int here = position;
+        if (task + step < tasks) position = p.position[(task + step) / p.parts];   // asked for a row ahead
+        if (here < 0) continue;                // the row belongs to nobody
+        RopePiece<BF16> next[2];
+        const long long q_row = row * p.q_stride, k_row = row * p.k_stride - static_cast<long long>(p.Hq) * p.D;
+        auto fetch = [&](int h) {              // the lane's pieces of head h
+            if (!on || h >= heads) return;
+            const bool is_q = h < p.Hq;
+            const long long at = (is_q ? q_row : k_row) + h * p.D;
+            next[0].load(is_q ? p.q : p.k, at + a), next[1].load(is_q ? p.q : p.k, at + b);
+        };
+        const int first = part * GROUPS + group, stride = p.parts * GROUPS;
+        fetch(first);
         __syncwarp();
         for (int i = lane; i < pairs; i += 32) {
-            double turn = static_cast<double>(position) * static_cast<double>(p.inv_freq[i]) * 0.15915494309189533577;
+            double turn = static_cast<double>(here) * static_cast<double>(p.inv_freq[i]) * 0.15915494309189533577;
             turn -= rint(turn);
             float s, co;
             sincospif(2.0f * static_cast<float>(turn), &s, &co);
-            turns[warp][i] = make_float2(co, s);
+            float* to = &turns[warp][i >> 1][0].x + (i & 1);
+            to[0] = co, to[2] = s;
         }
         __syncwarp();
-        float cs[8], sn[8];
+        uint64_t cs[4], sn[4];                 // cosines, sines of the lane's eight pairs, two by two
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 t = turned ? turns[warp][8 * c + i] : make_float2(1.0f, 0.0f);   // (not used where nothing turns)
-            cs[i] = t.x, sn[i] = t.y;
+        for (int i = 0; i < 4; ++i) {
+            const float4 t = turned ? *reinterpret_cast<const float4*>(&turns[warp][4 * c + i][0]) : make_float4(1.0f, 1.0f, 0.0f, 0.0f);   // (not used where nothing turns)
+            cs[i] = pair_of(t.x, t.y), sn[i] = pair_of(t.z, t.w);
         }
-        for (int h0 = part * groups; h0 < heads; h0 += p.parts * groups) {
-            const int h = h0 + group;
-            const bool is_q = h < p.Hq, here = on && h < heads;
-            float x[2][8] = {};
-            if (here) {
-                const void* src = is_q ? p.q : p.k;
-                const long long at = row * (is_q ? p.q_stride : p.k_stride) + static_cast<long long>(is_q ? h : h - p.Hq) * p.D;
-                rope_load<BF16>(src, at + a, x[0]), rope_load<BF16>(src, at + b, x[1]);
-            }
-            if (p.q_weight || p.k_weight) {     // the same for all lanes
-                float sum = 0.0f;
+        const long long qo_row = row * p.qo_stride, ko_row = row * p.ko_stride - static_cast<long long>(p.Hq) * p.D;
+        for (int h = first; h - group < heads; h += stride) {
+            const bool is_q = h < p.Hq, live = on && h < heads;
+            uint64_t x[2][4] = {};
+            if (live) next[0].values(x[0]), next[1].values(x[1]);
+            fetch(h + stride);                 // the next heads are on their way while these are worked on
+            if constexpr (NORM) {
+                uint64_t squares = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += x[0][i] * x[0][i] + x[1][i] * x[1][i];
+                for (int i = 0; i < 4; ++i) squares = pair_fma(x[1][i], x[1][i], pair_fma(x[0][i], x[0][i], squares));
+                float even, odd;
+                pair_to(squares, even, odd);
+                float sum = even + odd;
 #pragma unroll
                 for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                const float r = (is_q ? p.q_weight : p.k_weight) ? 1.0f / sqrtf(sum * inv_d + p.eps) : 1.0f;
+                if ((is_q ? p.q_weight : p.k_weight) && live) {
+                    const float r = 1.0f / sqrtf(sum * inv_d + p.eps);
+                    const uint64_t rr = pair_of(r, r);
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                    for (int j = 0; j < 2; ++j) {
+                        const float4* w = reinterpret_cast<const float4*>(&weights[is_q ? 0 : 1][j ? b : a]);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[j][i] *= r * (is_q ? wq[j][i] : wk[j][i]);
+                        for (int i = 0; i < 2; ++i) {
+                            const float4 v = w[i];
+                            x[j][2 * i] = pair_mul(pair_mul(x[j][2 * i], rr), pair_of(v.x, v.y));
+                            x[j][2 * i + 1] = pair_mul(pair_mul(x[j][2 * i + 1], rr), pair_of(v.z, v.w));
+                        }
+                    }
+                }
             }
-            if (!here) continue;
-            if (turned && p.near) {
+            if (!live) continue;
+            if (turned) {
+                if constexpr (NEAR) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float u, v, c0, c1, s0, s1;
+                            pair_to(x[j][i], u, v), pair_to(cs[2 * j + (i >> 1)], c0, c1), pair_to(sn[2 * j + (i >> 1)], s0, s1);
+                            const float co = i & 1 ? c1 : c0, si = i & 1 ? s1 : s0;
+                            x[j][i] = pair_of(u * co - v * si, v * co + u * si);
+                        }
+                } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float u = x[j][2 * i], v = x[j][2 * i + 1], co = cs[4 * j + i], si = sn[4 * j + i];
-                        x[j][2 * i] = u * co - v * si, x[j][2 * i + 1] = v * co + u * si;
+                        const uint64_t u = x[0][i], v = x[1][i];
+                        const uint64_t minus = pair_mul(v, sn[i]) ^ 0x8000000080000000ull;
+                        x[0][i] = pair_fma(u, cs[i], minus), x[1][i] = pair_fma(v, cs[i], pair_mul(u, sn[i]));
                     }
-            } else if (turned) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float u = x[0][i], v = x[1][i];
-                    x[0][i] = u * cs[i] - v * sn[i], x[1][i] = v * cs[i] + u * sn[i];
                 }
             }
             void* dst = is_q ? p.q_out : p.k_out;
-            const long long to = row * (is_q ? p.qo_stride : p.ko_stride) + static_cast<long long>(is_q ? h : h - p.Hq) * p.D;
+            const long long to = (is_q ? qo_row : ko_row) + h * p.D;
             rope_store<BF16>(dst, to + a, x[0]), rope_store<BF16>(dst, to + b, x[1]);
         }
     }

@@ -778,8 +778,14 @@ class Kv4Rows:
 
     @classmethod
     def empty(cls, R: int, total: int, device="cuda"):
-        new = lambda n, t: torch.empty(n, dtype=t, device=device)  # noqa: E731
-        return cls(new(R + 1, torch.int32), new(total, torch.int32), new(total, torch.int64), new(1, torch.int32))
+        new = torch.empty
+        return cls(new(R + 1, dtype=torch.int32, device=device), new(total, dtype=torch.int32, device=device),
+                   new(total, dtype=torch.int64, device=device), new(1, dtype=torch.int32, device=device))
+
+    @classmethod
+    def _beside(cls, rows, total):
+        new = rows.new_empty
+        return cls(new(rows.shape[0] + 1), new(total), new(total, dtype=torch.int64), new(1))
 
 
 def _tables(pages: Kv4Pages, free: Kv4FreePages):
@@ -792,7 +798,7 @@ def qift_kv4_pages_begin(pages: Kv4Pages, free: Kv4FreePages, rows, first, total
     """rows, first int32 [R]: rows[r] new tokens behind first[r] cached ones -> pages for them (pages.page_table, free) and a Kv4Rows of
     `total` rows; mask int32 [total, words]: drafted trees, whose tokens' positions are their depths."""
     if out is None:
-        out = Kv4Rows.empty(pages.R, total, rows.device)
+        out = Kv4Rows._beside(rows, total)
     _same_device(pages.page_table, rows, first, mask, out.row_start, out.position, out.slot, out.lost)
     words = 0 if mask is None else mask.shape[1]
     _call(rows, lib().qift_kv4_pages_begin, _on(rows, torch.int32, pages.R), _on(first, torch.int32, pages.R), pages.R, *_tables(pages, free),
@@ -816,18 +822,22 @@ def qift_qk_norm_rope(q, k, position, inv_freq, q_weight=None, k_weight=None, ep
     weights [D] of the rows' type or None -> (q_out, k_out): normed and rotated.  q_out / k_out may be q / k; rows with a negative position
     are left as they are there."""
     total, Hq, D = q.shape
-    H = k.shape[1]
-    assert k.shape == (total, H, D) and q.dtype == k.dtype, "q and k have the same rows, head size and type"
+    H, dtype = k.shape[1], q.dtype
     if q_out is None:
-        q_out = torch.empty((total, Hq, D), dtype=q.dtype, device=q.device)
+        q_out = q.new_empty((total, Hq, D))
     if k_out is None:
-        k_out = torch.empty((total, H, D), dtype=k.dtype, device=k.device)
-    assert q_out.shape == q.shape and k_out.shape == k.shape and q_out.dtype == q.dtype and k_out.dtype == q.dtype
+        k_out = k.new_empty((total, H, D))
     _same_device(q, k, position, inv_freq, q_weight, k_weight, q_out, k_out)
-    weights = [None if w is None else _on(w, q.dtype, D) for w in (q_weight, k_weight)]
-    _call(q, lib().qift_qk_norm_rope, q.data_ptr(), k.data_ptr(), _float_type(q), _rows(q), _rows(k), total, Hq, H, D, *weights, eps,
+    strides = []
+    for t, heads in ((q, Hq), (k, H), (q_out, Hq), (k_out, H)):
+        assert t.shape == (total, heads, D) and t.dtype == dtype, "rows, heads and type of the tensors differ"
+        rows, inner, one = t.stride()
+        assert one == 1 and inner == D, "the heads of a row are not contiguous"
+        strides.append(rows if total > 1 else heads * D)      # a single row has no distance to the next one
+    _call(q, lib().qift_qk_norm_rope, q.data_ptr(), k.data_ptr(), _float_type(q), strides[0], strides[1], total, Hq, H, D,
+          None if q_weight is None else _on(q_weight, dtype, D), None if k_weight is None else _on(k_weight, dtype, D), eps,
           _on(inv_freq, torch.float32), 2 * inv_freq.numel(), pairs, _on(position, torch.int32, total), q_out.data_ptr(), k_out.data_ptr(),
-          _rows(q_out), _rows(k_out))
+          strides[2], strides[3])
     return q_out, k_out
 
 
@@ -846,8 +856,8 @@ def _gated(fn, X, dtype, K, gate, up, out, out_dtype, want_acc, levels_buf, leve
     (pg, sg), (pu, su) = gate, up
     M, N = X.shape[0], sg.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=X.device)
-    accs = [torch.empty((M, N), dtype=torch.int32, device=X.device) for _ in range(2)] if want_acc else ()
+        out = X.new_empty((M, N), dtype=out_dtype)
+    accs = [X.new_empty((M, N), dtype=torch.int32) for _ in range(2)] if want_acc else ()
     if levels_buf is None:
         assert not levels_ready
         if M >= qift_gated_levels_min_rows() and K % 16 == 0:
@@ -878,7 +888,7 @@ def qift_gated_forward(X, had_block: int, gate, up, levels: int, clip_ratio: flo
     M, K = X.shape
     L = lib()
     if scratch is None:
-        scratch = torch.empty(L.qift_gated_forward_scratch_bytes(M, K), dtype=torch.uint8, device=X.device)
+        scratch = X.new_empty(L.qift_gated_forward_scratch_bytes(M, K), dtype=torch.uint8)
     _same_device(X, scratch)
     return _gated(L.qift_gated_forward, X, X.dtype, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation,
                   (_float_type(X), M, K, had_block, clip_ratio, levels), _space(scratch))

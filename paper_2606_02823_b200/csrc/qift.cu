@@ -359,7 +359,7 @@ struct PairCall {
 template <int BN, bool GATED = false>
 int launch_gemm_pairs(const PairParams& pp, int tiles, cudaStream_t st) {
     auto kernel = gemm_i8_pair_kernel<BN, GATED>;
-    const size_t smem = pair_smem_bytes<BN>();
+    const size_t smem = pair_smem_bytes<BN, GATED>();
     cudaError_t e = allow_smem(kernel, smem);
     if (e != cudaSuccess) return cuda_status(e);
     int pairs = sm_count() / 2;

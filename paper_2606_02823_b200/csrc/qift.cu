@@ -2190,7 +2190,7 @@ int qift_qk_norm_rope(const void* Q, const void* K, int x_dtype, long long q_str
     while (lanes * 16 < D) lanes *= 2;
     // A row's heads are split over warps while the rows alone do not fill the SMs; beyond, a warp takes one row, and the next CTA the next ones
     // (18000 rows dealt to resident warps, three or four each, took 5 % longer).
-    const int trips = (Hq + H + 32 / lanes - 1) / (32 / lanes);
+    const int trips = (Hq + 32 / lanes - 1) / (32 / lanes) + (H + 32 / lanes - 1) / (32 / lanes);
     const long long warps = 4ll * kRopeWarps * sm_count();
     p.parts = static_cast<int>(std::min(static_cast<long long>(trips), (warps + total - 1) / total));
     const long long blocks = (static_cast<long long>(total) * p.parts + kRopeWarps - 1) / kRopeWarps, most = 64ll * sm_count();

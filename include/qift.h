@@ -511,6 +511,7 @@ int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16
  *   shared      in  [R] int32, or NULL: entries before shared[r] are not given back (a prefix that others hold, too)
  * The first page given back, request by request in ascending order, ends on top: a begin that is taken back leaves the stack as it was.
  * A page that two entries hold goes back twice unless `shared` says otherwise; what would not fit on the stack is dropped.
+ * Calls that change the tables of one pool have to follow one another in stream order.
  * Both: int32 arrays 4-byte aligned, slot 8.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_tokens, mask_words, R * max_pages >= 2^31),
  * ALIGNMENT, CUDA. */
 int qift_kv4_pages_begin(const int32_t* rows, const int32_t* first, int R, int32_t* page_table, int max_pages, int num_pages,
@@ -549,7 +550,8 @@ int qift_qk_norm_rope(const void* Q, const void* K, int x_dtype, long long q_str
  *               when K % 16 == 0.  levels_ready, ahead: as for qift_linear_multi / qift_forward_multi, in whose chains the call can stand
  * qift_gated_forward takes the activation itself, X [M,K], and rotates and quantizes it first (qift_quantize_act);
  *   scratch     dev, >= qift_gated_forward_scratch_bytes(M, K), 256-byte aligned: q_a and s_a
- * No other workspace.  The sums are exact: h follows from the accumulators in fp32, and does not depend on the route.
+ * No other workspace.  The sums are exact: h follows from the accumulators in fp32, and does not depend on the route.  Scales have to be such that g
+ * and u are finite.
  * Errors: INVALID_ARG (null pointers, different N, enums, ahead), UNSUPPORTED_SHAPE, ALIGNMENT, WORKSPACE, CUDA. */
 typedef enum { QIFT_ACT_SILU = 0, QIFT_ACT_GELU_TANH = 1 } qift_activation;
 int qift_gated_levels_min_rows(void);

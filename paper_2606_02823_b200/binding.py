@@ -851,7 +851,7 @@ def qift_gated_levels_min_rows() -> int:
 _GATE_UP = struct.Struct("@PPPPiiPPPPii")      # two qift_linear_output
 
 
-def _gated(fn, X, dtype, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation, before, after):
+def _gated(fn, X, dtype, K, levels, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation, before, after):
     """What the gated calls have in common: fn(*before, descriptors of the two outputs, activation, result, *after, levels buffer, ...)."""
     (pg, sg), (pu, su) = gate, up
     M, N = X.shape[0], sg.shape[0]
@@ -863,6 +863,9 @@ def _gated(fn, X, dtype, K, gate, up, out, out_dtype, want_acc, levels_buf, leve
         if M >= qift_gated_levels_min_rows() and K % 16 == 0:
             levels_buf = torch.empty(qift_levels_bytes(K, [gate, up]), dtype=torch.uint8, device=X.device)
     _same_device(X, pg, sg, pu, su, out, levels_buf)
+    words = K // (8 if levels == INT4 else 16)
+    need = (N + 15) // 16 * ((words + 15) // 16) * (1536 if levels == INT3 else 1024)
+    assert pg.numel() * pg.element_size() >= need and pu.numel() * pu.element_size() >= need, "packed weights of another size"
     f32, ag, au = torch.float32, *([a.data_ptr() for a in accs] or (0, 0))
     outputs = _GATE_UP.pack(_on(pg, pg.dtype), _on(sg, f32), 0, ag, N, 0, _on(pu, pu.dtype), _on(su, f32), 0, au, su.shape[0], 0)
     buf = (None, 0) if levels_buf is None else _space(levels_buf)
@@ -878,7 +881,7 @@ def qift_gated_linear(q_a, s_a, gate, up, levels: int, activation: int = ACT_SIL
     M, K = q_a.shape
     _same_device(q_a, s_a)
     assert s_a.numel() >= M, "a scale for every row"
-    return _gated(lib().qift_gated_linear, q_a, torch.int8, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation,
+    return _gated(lib().qift_gated_linear, q_a, torch.int8, K, levels, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation,
                   (_on(s_a, torch.float32), M, K, levels), ())
 
 
@@ -890,7 +893,7 @@ def qift_gated_forward(X, had_block: int, gate, up, levels: int, clip_ratio: flo
     if scratch is None:
         scratch = X.new_empty(L.qift_gated_forward_scratch_bytes(M, K), dtype=torch.uint8)
     _same_device(X, scratch)
-    return _gated(L.qift_gated_forward, X, X.dtype, K, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation,
+    return _gated(L.qift_gated_forward, X, X.dtype, K, levels, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation,
                   (_float_type(X), M, K, had_block, clip_ratio, levels), _space(scratch))
 
 

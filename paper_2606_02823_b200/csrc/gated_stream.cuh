@@ -197,7 +197,7 @@ gated_stream_kernel(const __grid_constant__ GatedParams p, int pairs, int slots)
             __syncwarp();                                       // every lane has read the slot before it is filled again
             if (ok && elect_one()) fetch(s);
             advance();
-            if (++s == slots) s = 0, ph ^= 1;
+            if (ok && ++s == slots) s = 0, ph ^= 1;
         }
         int sum[NT][4];
 #pragma unroll
@@ -236,6 +236,8 @@ gated_stream_kernel(const __grid_constant__ GatedParams p, int pairs, int slots)
                 }
         }
     }
+    // given up: what has been asked for still arrives before the warp ends (slots behind the one that failed, their next fill)
+    for (int i = 0; !ok && i < slots; ++i) mbar_wait(&full[(s + i) % slots], s + i < slots ? ph : ph ^ 1, 81, 1000000ull);
 }
 
 }  // namespace qift

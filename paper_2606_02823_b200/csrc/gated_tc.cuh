@@ -208,6 +208,8 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
                 if (++step == steps) step = 0;
             }
         }
+        // given up: what has been asked for still arrives before the CTA ends
+        for (int i = 0; !ok && i < min(k > early ? k : early, stages); ++i) mbar_wait(&full[i], ((max(k, early) - 1 - i) / stages) & 1, 82, 1000000ull);
     } else if (warp <= 2) {
         // ------------------------------------------------------------------ products of a matrix
         const int mat = warp - 1;

@@ -122,3 +122,14 @@ def test_captured_on_another_stream(M):
         c.check(out)
     rc, detail = qift.qift_device_status()
     assert rc == qift.OK, (rc, detail)
+
+
+def test_weights_of_another_size_are_refused():
+    c = Case(1, 3, 40, 512, "mnz")
+    (pg, sg), up = c.weights
+    with pytest.raises(AssertionError, match="another size"):
+        qift.qift_gated_linear(c.q, c.s, (pg[:-8], sg), up, c.lv)
+    with pytest.raises(AssertionError, match="another size"):
+        qift.qift_gated_linear(torch.zeros((3, 1024), dtype=torch.int8, device="cuda"), c.s, *c.weights, c.lv)
+    with pytest.raises(qift.QiftError):
+        qift.qift_gated_linear(c.q, c.s, (pg, sg), (up[0], up[1][:32]), c.lv)

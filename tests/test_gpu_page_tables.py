@@ -45,7 +45,7 @@ def fresh(r, R, most, page, pages):
     return Both(np.full((R, most), -1), r.permutation(pages), pages, page, pages)
 
 
-@pytest.mark.parametrize("R, page, rows, total_more", [(1, 32, 1, 0), (1, 64, 5000, 3), (3, 96, 40, 0), (33, 32, 200, 11), (700, 64, 3, 1),
+@pytest.mark.parametrize("R, page, rows, total_more", [(1, 32, 1, 0), (1, 64, 5000, 3), (3, 96, 40, 0), (33, 32, 200, 11), (700, 64, 3, 1), (600, 32, 2000, 5),
                                                       (2500, 32, 90, 0), (5, 1024, 3000, 0)])
 def test_steps(R, page, rows, total_more):
     """Several steps: rows come, some stay, some requests end; pools that are large enough and that are not."""

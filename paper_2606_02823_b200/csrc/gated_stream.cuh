@@ -3,8 +3,8 @@
 // Bound by HBM: 2 N K bits / 8 bytes of codes (4096 -> 14336 in two bits: 29.4 MB, 4.6 us at the copy rate) against next to nothing
 // else.  One call has few rows of tiles (896 of 16 channels there), so hand-overs between warps are what has to be avoided: a pair of warps
 // takes a tile, one the gate's rows, one the other matrix's, each with a ring of its own that it fills by bulk copies itself, 64
-// words deep (4 KB) a slot.  A CTA's share of a call is about what its shared memory holds, so nearly all of it is asked for before
-// anything else happens, the wait for the preceding kernel included.  Packed words become operands with one logic operation each
+// words deep (4 KB) a slot.  A CTA's share of a call is about what its shared memory holds: two slots a warp are asked for before anything else
+// happens, the wait for the preceding kernel included, the rest behind the activations.  Packed words become operands with one logic operation each
 // (mma_tile_step) against activations that stand in shared memory for the whole kernel; at the end of a tile one warp of the pair hands its
 // sums to the other (64-thread barrier, two buffers by turns), which writes h.
 //
@@ -23,6 +23,7 @@ namespace qift {
 constexpr int kGsPairs = 8, kGsThreads = 64 * kGsPairs;
 constexpr int kGsMaxM = 16;
 constexpr int kGsWords = 64, kGsMaxSlots = 8;               // packed words per row of a slot; slots of a warp
+constexpr int kGsEarly = 2;          // slots that are asked for before the activations (8 rows, 4096 -> 14336: all three 11.2 us, two 10.6, one 10.4; 1 row: 10.0, 9.6, 9.6)
 constexpr int kGsSmem = 226 * 1024;
 
 __host__ __device__ constexpr int gs_slot_bytes(int lv) { return kGsWords * tile_word_bytes(lv); }
@@ -91,7 +92,7 @@ gated_stream_kernel(const __grid_constant__ GatedParams p, int pairs, int slots)
             mbar_fence_init();
         }
         __syncwarp();
-        for (int s = 0; s < slots; ++s, advance())              // the weights depend on no kernel before this one
+        for (int s = 0; s < min(slots, kGsEarly); ++s, advance())   // the weights depend on no kernel before this one
             if (elect_one()) fetch(s);
     }
     if (tid <= kGsMaxM) sum_q[tid] = 0;                         // and the flag behind them
@@ -100,32 +101,50 @@ gated_stream_kernel(const __grid_constant__ GatedParams p, int pairs, int slots)
 
     // -------------------------------------------------------------------- the activations
     {
+        // Asked for four pieces a thread at a time, and before the rest of the weights: behind those they arrived 2 us later.  Eight neighbouring
+        // threads are always at the same token.
+        constexpr int BATCH = 4;
         const int pieces = slices * (SLICE / 16), all = M * pieces;
-        for (int i0 = 0; i0 < all; i0 += kGsThreads) {          // eight neighbouring threads are always at the same token
-            const int i = i0 + tid, m = i / pieces, q = i - m * pieces;
-            int sum = 0;
-            if (i < all) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                const int8_t* src = p.q_a + static_cast<size_t>(m) * p.K + 16 * q;
-                if (PER == 16 || p.K % 16 == 0) {
-                    if (16 * q < p.K) v = *reinterpret_cast<const uint4*>(src);
-                } else {                                        // rows of eight-byte alignment
-                    if (16 * q < p.K) *reinterpret_cast<uint2*>(&v.x) = *reinterpret_cast<const uint2*>(src);
-                    if (16 * q + 8 < p.K) *reinterpret_cast<uint2*>(&v.z) = *reinterpret_cast<const uint2*>(src + 8);
+        for (int i0 = 0; i0 < all; i0 += BATCH * kGsThreads) {
+            uint4 v[BATCH];
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const int i = i0 + b * kGsThreads + tid, m = i / pieces, q = i - m * pieces;
+                v[b] = make_uint4(0, 0, 0, 0);
+                if (i < all) {
+                    const int8_t* src = p.q_a + static_cast<size_t>(m) * p.K + 16 * q;
+                    if (PER == 16 || p.K % 16 == 0) {
+                        if (16 * q < p.K) v[b] = *reinterpret_cast<const uint4*>(src);
+                    } else {                                    // rows of eight-byte alignment
+                        if (16 * q < p.K) *reinterpret_cast<uint2*>(&v[b].x) = *reinterpret_cast<const uint2*>(src);
+                        if (16 * q + 8 < p.K) *reinterpret_cast<uint2*>(&v[b].z) = *reinterpret_cast<const uint2*>(src + 8);
+                    }
                 }
-                const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+            }
+            if (i0 + BATCH * kGsThreads >= all && pair < pairs) {   // the last of them are on their way
+                for (int s = min(slots, kGsEarly); s < slots; ++s, advance())
+                    if (elect_one()) fetch(s);
+            }
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const int i = i0 + b * kGsThreads + tid, m = i / pieces, q = i - m * pieces;
+                const uint32_t u[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
+                int sum = 0;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum = __dp4a(static_cast<int>(u[j]), 0x01010101, sum);
-                if constexpr (LV == QIFT_LEVELS_POT) v = pot_lut_order(v);
-                else if constexpr (LV == QIFT_LEVELS_INT4) v.x = (v.x << 4) & 0xf0f0f0f0u, v.z = (v.z << 4) & 0xf0f0f0f0u;
-                else v.x = (v.x << 2) & 0xfcfcfcfcu, v.z = (v.z << 2) & 0xfcfcfcfcu;   // |q| <= 8: the products fit a byte
-                const int sl = q / (SLICE / 16), piece = q - sl * (SLICE / 16);
-                *reinterpret_cast<uint4*>(act + (static_cast<size_t>(sl) * M + m) * SLICE + 16 * swizzled_group(piece, m, PER == 16)) = v;
-            }
-            if constexpr (LV != QIFT_LEVELS_POT && LV != QIFT_LEVELS_INT3) {
+                if constexpr (LV == QIFT_LEVELS_POT) v[b] = pot_lut_order(v[b]);
+                else if constexpr (LV == QIFT_LEVELS_INT4) v[b].x = (v[b].x << 4) & 0xf0f0f0f0u, v[b].z = (v[b].z << 4) & 0xf0f0f0f0u;
+                else v[b].x = (v[b].x << 2) & 0xfcfcfcfcu, v[b].z = (v[b].z << 2) & 0xfcfcfcfcu;   // |q| <= 8: the products fit a byte
+                if (i < all) {
+                    const int sl = q / (SLICE / 16), piece = q - sl * (SLICE / 16);
+                    *reinterpret_cast<uint4*>(act + (static_cast<size_t>(sl) * M + m) * SLICE + 16 * swizzled_group(piece, m, PER == 16)) = v[b];
+                }
+                if constexpr (LV != QIFT_LEVELS_POT && LV != QIFT_LEVELS_INT3) {
+                    if (i0 + b * kGsThreads >= all) break;      // the same for all threads
 #pragma unroll
-                for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                if ((lane & 7) == 0 && i < all) atomicAdd(&sum_q[m], sum);
+                    for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                    if ((lane & 7) == 0 && i < all) atomicAdd(&sum_q[m], sum);
+                }
             }
         }
     }

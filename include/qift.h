@@ -512,7 +512,7 @@ int qift_lora_linear(const void* X, int x_dtype, const uint16_t* A, const uint16
  * The first page given back, request by request in ascending order, ends on top: a begin that is taken back leaves the stack as it was.
  * A page that two entries hold goes back twice unless `shared` says otherwise; what would not fit on the stack is dropped.
  * Calls that change the tables of one pool have to follow one another in stream order.
- * Both: int32 arrays 4-byte aligned, slot 8.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_tokens, mask_words, R * max_pages >= 2^31),
+ * Both: int32 arrays 4-byte aligned, slot 8.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_tokens, mask_words, R > 2^30, R * max_pages >= 2^31),
  * ALIGNMENT, CUDA. */
 int qift_kv4_pages_begin(const int32_t* rows, const int32_t* first, int R, int32_t* page_table, int max_pages, int num_pages,
                          int page_tokens, int32_t* free_pages, int32_t* free_count, const int32_t* mask, int mask_words, int total,
@@ -547,7 +547,8 @@ int qift_qk_norm_rope(const void* Q, const void* K, int x_dtype, long long q_str
  *   activation  QIFT_ACT_SILU: g / (1 + exp(-g)); QIFT_ACT_GELU_TANH: g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2
  *   H           out [M,N] fp32 or bf16 (rounded once)
  *   levels_buf  dev, >= qift_levels_bytes(K, gate_up, 2), 256-byte aligned; needed from qift_gated_levels_min_rows() token rows on
- *               when K % 16 == 0.  levels_ready, ahead: as for qift_linear_multi / qift_forward_multi, in whose chains the call can stand
+ *               when K % 16 == 0, and with levels_ready.  levels_ready, ahead: as for qift_linear_multi / qift_forward_multi, in
+ *               whose chains the call can stand (levels that are there are used from fewer rows on than it would decode them for)
  * qift_gated_forward takes the activation itself, X [M,K], and rotates and quantizes it first (qift_quantize_act);
  *   scratch     dev, >= qift_gated_forward_scratch_bytes(M, K), 256-byte aligned: q_a and s_a
  * No other workspace.  The sums are exact: h follows from the accumulators in fp32, and does not depend on the route.  Scales have to be such that g

@@ -66,7 +66,7 @@ gated_generic_kernel(const GatedParams p) {
     const int pitch = round_up16(words);
     const uint32_t* q32 = reinterpret_cast<const uint32_t*>(p.q_a);
     const size_t qpitch = p.K / 4;
-    for (int m0 = blockIdx.y * kGatedTokens; m0 < p.M; m0 += gridDim.y * kGatedTokens) {
+    for (long long m0 = blockIdx.y * kGatedTokens; m0 < p.M; m0 += gridDim.y * kGatedTokens) {
         int S[2][kGatedTokens] = {}, Sb[2][kGatedTokens] = {}, Sq[kGatedTokens] = {};
         for (int j = lane; j < words; j += 32) {
             uint32_t w[2], wh[2] = {0, 0};
@@ -119,7 +119,7 @@ gated_generic_kernel(const GatedParams p) {
                 }
                 acc[i] = combine_generic<LV>(S[i][mm], Sb[i][mm], Sq[mm]);
             }
-            const int m = m0 + mm;
+            const long long m = m0 + mm;
             if (lane == 0 && m < p.M)
                 gated_store(p, static_cast<size_t>(m) * p.N + n, acc[0], acc[1], p.s_a[m], p.w[0].s_n[n], p.w[1].s_n[n]);
         }

@@ -39,6 +39,7 @@ constexpr int kGtThreads = 32 * (kGtExpander0 + kGtExpanders);
 constexpr int kGtRing = 2;                   // steps of operands in tensor memory, per matrix
 constexpr int kGtOperands = 256;             // first operand column
 constexpr int kGtSmem = 226 * 1024;
+constexpr int kGtMaxK = 1 << 21;              // K < this: operands up to 128 times activations up to 8 add up within 32 bits
 
 __host__ __device__ constexpr int gt_slices(int lv) { return lv == QIFT_LEVELS_INT4 ? 2 : 1; }            // 16-word slices of a step
 __host__ __device__ constexpr int gt_slice_rows(int lv) { return lv == QIFT_LEVELS_INT3 ? 24 : 16; }      // 64-byte rows of a slice and row block

@@ -16,6 +16,7 @@ constexpr int kPtPer = 4;           // entries of a thread in a trip
 constexpr int kPtBatch = 2048;      // requests whose sums are held in shared memory at a time
 constexpr int kPtCluster = 8;
 constexpr int kPtFewThreads = 256, kPtManyThreads = 1024;
+constexpr int kPtMaxRequests = 1 << 30;   // sums of two of their numbers stay within 32 bits
 constexpr int kPtFewRows = 1024;    // rows that the first kernel fills in itself
 
 struct PageTables {

@@ -358,30 +358,32 @@ gemm_i8_pair_kernel(const __grid_constant__ PairParams p) {
                         }
                         __syncwarp();
                     }
-                    if (m >= p.M) continue;
-                    const size_t o = static_cast<size_t>(m) * N + n;
-                    if (whole && p.y_bf16) {
-                        uint32_t b[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            b[j] = static_cast<uint32_t>(f32_to_bf16_bits(h[2 * j])) | (static_cast<uint32_t>(f32_to_bf16_bits(h[2 * j + 1])) << 16);
-                        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.H) + o);
-                        dst[0] = make_uint4(b[0], b[1], b[2], b[3]), dst[1] = make_uint4(b[4], b[5], b[6], b[7]);
-                    } else if (whole) {
-                        float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.H) + o);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) dst[j] = make_float4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+                    if (m < p.M) {
+                        const size_t o = static_cast<size_t>(m) * N + n;
+                        if (whole && p.y_bf16) {
+                            uint32_t b[8];
+    #pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                b[j] = static_cast<uint32_t>(f32_to_bf16_bits(h[2 * j])) | (static_cast<uint32_t>(f32_to_bf16_bits(h[2 * j + 1])) << 16);
+                            uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.H) + o);
+                            dst[0] = make_uint4(b[0], b[1], b[2], b[3]), dst[1] = make_uint4(b[4], b[5], b[6], b[7]);
+                        } else if (whole) {
+                            float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.H) + o);
+    #pragma unroll
+                            for (int j = 0; j < 4; ++j) dst[j] = make_float4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+                        }
+                        if (S.acc_debug) {
+    #pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                if (n + j < N) S.acc_debug[o + j] = static_cast<int>(vg[j]);
+                        }
+                        if (U.acc_debug) {
+    #pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                if (n + j < N) U.acc_debug[o + j] = static_cast<int>(vu[j]);
+                        }
                     }
-                    if (S.acc_debug) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (n + j < N) S.acc_debug[o + j] = static_cast<int>(vg[j]);
-                    }
-                    if (U.acc_debug) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (n + j < N) U.acc_debug[o + j] = static_cast<int>(vu[j]);
-                    }
+                    __syncwarp();              // the next loads take the whole warp
                 }
             } else
             for (int c0 = 0; c0 < BN; c0 += 32) {

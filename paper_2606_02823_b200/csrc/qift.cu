@@ -1952,7 +1952,8 @@ namespace {
 int check_tables(int R, const int32_t* page_table, int max_pages, int num_pages, int page_tokens, int32_t* free_pages, int32_t* free_count,
                  PageTables* t) {
     if (!page_table || !free_pages || !free_count || R <= 0 || max_pages <= 0 || num_pages <= 0) return QIFT_ERR_INVALID_ARG;
-    if (qift_kv4_page_bytes(page_tokens, 1, kKvD) == 0 || static_cast<long long>(R) * max_pages > 0x7fffffffll) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (qift_kv4_page_bytes(page_tokens, 1, kKvD) == 0 || R > kPtMaxRequests || static_cast<long long>(R) * max_pages > 0x7fffffffll)
+        return QIFT_ERR_UNSUPPORTED_SHAPE;
     if (!aligned4(page_table) || !aligned4(free_pages) || !aligned4(free_count)) return QIFT_ERR_ALIGNMENT;
     *t = PageTables{const_cast<int32_t*>(page_table), free_pages, free_count, R, max_pages, num_pages, page_tokens};
     return QIFT_OK;
@@ -1974,7 +1975,12 @@ int run_qk_rope(const RopeParams& p, bool near, int lanes, dim3 grid, cudaStream
     }
 }
 
-constexpr int kGatedLevelsMinM = 513;   // token rows from which on the codes are decoded to int8 first
+// Token rows from which on products of int8 levels, by CTA pairs, are faster than the codes as they are.  With decoding (microseconds, codes as they
+// are and decoded; 4096 -> 14336 in two bits: 768 rows 75 and 98, 1024 rows 104 and 112, 1536 rows 151 to 181 and 164, 4096 rows 479 and 352;
+// three bits: 1024 rows 124 and 120; 8192 -> 28672: 1024 rows 365 and 421, 1536 rows 614 and 582, 2048 rows 806 and 744) and with levels that are
+// there already (384 rows 47 and 48, 512 rows 60 and 50, 1024 rows 104 and 83; 8192 -> 28672: 384 rows 136 and 177, 512 rows 199 and 165).
+constexpr int kGatedLevelsMinM = 1025, kGatedReadyMinM = 449;
+inline bool gated_by_levels(int M, int K, int levels_ready) { return K % 16 == 0 && M >= (levels_ready ? kGatedReadyMinM : kGatedLevelsMinM); }
 
 // Slots of a warp's ring that shared memory has room for.
 inline int gs_slots(int M, int K, int lv, int pairs) {
@@ -1989,6 +1995,10 @@ inline int gs_pairs(int M, int N, int K, int lv) {
     while (pairs > 4 && gs_slots(M, K, lv, pairs) < 2) --pairs;
     return pairs;
 }
+// The stream kernel takes calls whose rows leave every warp two slots.  Longer activations go to the tcgen05 kernel, which reads the codes once
+// for all rows: 16 rows of 16384 in blocks that fit, 53248 channels, took 195 us against 111 (INT4 305 and 137); 8 rows of 28672, 8192 channels,
+// 62 and 73 (INT4 95 and 67).
+inline bool gs_applies(int M, int N, int K, int lv) { return M <= kGsMaxM && gs_slots(M, K, lv, gs_pairs(M, N, K, lv)) >= 2; }
 template <int LV, int NT>
 int launch_gated_stream(const GatedParams& p, cudaStream_t st) {
     auto kernel = gated_stream_kernel<LV, NT>;
@@ -2001,21 +2011,8 @@ int launch_gated_stream(const GatedParams& p, cudaStream_t st) {
     return cuda_status(launch_pdl(kernel, dim3(grid), dim3(kGsThreads), smem, st, p, pairs, slots));
 }
 template <int LV>
-int run_gated_stream(GatedParams p, cudaStream_t st) {
-    // rows of long activations are taken in blocks that leave every warp two slots
-    int block = std::min(p.M, kGsMaxM);
-    while (block > 1 && gs_slots(block, p.K, LV, gs_pairs(block, p.N, p.K, LV)) < 2) --block;
-    const int M = p.M, size = p.h_bf16 ? 2 : 4;
-    const GatedParams all = p;
-    for (int m0 = 0; m0 < M; m0 += block) {
-        p.M = std::min(block, M - m0), p.q_a = all.q_a + static_cast<size_t>(m0) * p.K, p.s_a = all.s_a + m0;
-        p.H = static_cast<unsigned char*>(all.H) + static_cast<size_t>(m0) * p.N * size;
-        for (int i = 0; i < 2; ++i)
-            if (p.w[i].acc_debug) p.w[i].acc_debug = all.w[i].acc_debug + static_cast<size_t>(m0) * p.N;
-        const int rc = p.M > 8 ? launch_gated_stream<LV, 2>(p, st) : launch_gated_stream<LV, 1>(p, st);
-        if (rc != QIFT_OK) return rc;
-    }
-    return QIFT_OK;
+int run_gated_stream(const GatedParams& p, cudaStream_t st) {
+    return p.M > 8 ? launch_gated_stream<LV, 2>(p, st) : launch_gated_stream<LV, 1>(p, st);
 }
 
 // Packed words as rows of 64 bytes: [row blocks][slices x rows of a slice][64], a box of eight row blocks and `slices` slices, whose 16-byte
@@ -2052,20 +2049,20 @@ int run_gated_tc(const GatedParams& p, cudaStream_t st) {
 
 template <int LV>
 int run_gated_generic(const GatedParams& p, cudaStream_t st) {
-    const dim3 grid((p.N + kGenericWarps - 1) / kGenericWarps, static_cast<unsigned>(std::min((p.M + kGatedTokens - 1) / kGatedTokens, 4096)));
+    const dim3 grid((p.N + kGenericWarps - 1) / kGenericWarps, static_cast<unsigned>(std::min((p.M - 1) / kGatedTokens + 1, 4096)));
     return cuda_status(launch_pdl(gated_generic_kernel<LV>, grid, dim3(kGenericWarps * 32), 0, st, p));
 }
 
 // Everything that can be wrong with a call, found before anything is launched.
 int check_gated(int M, int K, int levels, const qift_linear_output* gate_up, int activation, const void* H, int h_dtype, const void* levels_buf,
-                size_t levels_bytes, const qift_decode_ahead* ahead) {
+                size_t levels_bytes, int levels_ready, const qift_decode_ahead* ahead) {
     if (!gate_up || !H || gate_up[0].N != gate_up[1].N) return QIFT_ERR_INVALID_ARG;
     if (activation != QIFT_ACT_SILU && activation != QIFT_ACT_GELU_TANH) return QIFT_ERR_INVALID_ARG;
     qift_linear_output o[2] = {gate_up[0], gate_up[1]};
     for (auto& x : o) x.Y = const_cast<void*>(H);      // the outputs' own Y are not used
     const int rc = check_outputs_and_ahead(M, K, levels, o, 2, h_dtype, ahead);
     if (rc != QIFT_OK) return rc;
-    if (M >= kGatedLevelsMinM && K % 16 == 0) {
+    if (gated_by_levels(M, K, levels_ready)) {
         if (!levels_buf || levels_bytes < qift_levels_bytes(K, o, 2)) return QIFT_ERR_WORKSPACE;
         if ((reinterpret_cast<uintptr_t>(levels_buf) & 255u) != 0) return QIFT_ERR_ALIGNMENT;
     }
@@ -2091,7 +2088,7 @@ int gated_impl(const int8_t* q_a, const float* s_a, int M, int K, int levels, co
     for (int i = 0; i < 2; ++i) p.w[i] = GatedMatrix{gate_up[i].packed, gate_up[i].s_n, gate_up[i].acc_debug};
     p.q_a = q_a, p.s_a = s_a, p.H = H, p.M = M, p.N = gate_up[0].N, p.K = K, p.h_bf16 = h_dtype == QIFT_BF16, p.act = activation;
     int rc;
-    if (M >= kGatedLevelsMinM && K % 16 == 0) {
+    if (gated_by_levels(M, K, levels_ready)) {
         PairCall c = {};
         c.q_a = q_a, c.s_a = s_a, c.M = M, c.K = K, c.y_bf16 = p.h_bf16, c.nseg = 2, c.H = H, c.act = activation;
         for (int i = 0; i < 2; ++i) {
@@ -2118,12 +2115,12 @@ int gated_impl(const int8_t* q_a, const float* s_a, int M, int K, int levels, co
         case QIFT_LEVELS_INT3: rc = run<QIFT_LEVELS_INT3>(p, st); break;       \
         default: rc = run<QIFT_LEVELS_INT4>(p, st); break;                     \
     }
-    if (M <= kGsMaxM) {
+    if (gs_applies(M, p.N, K, levels)) {
         QIFT_GATED(run_gated_stream)
-    } else if (K % 16 == 0) {
+    } else if (K % 16 == 0 && K < kGtMaxK) {
         QIFT_GATED(run_gated_tc)
     } else {
-        QIFT_GATED(run_gated_generic)      // rows that a tensor copy cannot take
+        QIFT_GATED(run_gated_generic)      // rows that a tensor copy cannot take, sums that the tensor cores' factors would carry past 32 bits
     }
 #undef QIFT_GATED
     return rc != QIFT_OK ? rc : run_ahead(ahead, false, st);
@@ -2207,7 +2204,7 @@ int qift_gated_linear(const int8_t* q_a, const float* s_a, int M, int K, int lev
                       void* H, int h_dtype, void* levels_buf, size_t levels_bytes, int levels_ready, const qift_decode_ahead* ahead,
                       void* stream) {
     if (!q_a || !s_a) return QIFT_ERR_INVALID_ARG;
-    const int rc = check_gated(M, K, levels, gate_up, activation, H, h_dtype, levels_buf, levels_bytes, ahead);
+    const int rc = check_gated(M, K, levels, gate_up, activation, H, h_dtype, levels_buf, levels_bytes, levels_ready, ahead);
     if (rc != QIFT_OK) return rc;
     if (!aligned16(q_a) || !aligned16(s_a)) return QIFT_ERR_ALIGNMENT;
     return gated_impl(q_a, s_a, M, K, levels, gate_up, activation, H, h_dtype, levels_buf, levels_ready, ahead, static_cast<cudaStream_t>(stream));
@@ -2221,7 +2218,7 @@ int qift_gated_forward(const void* X, int x_dtype, int M, int K, int had_block, 
                        const qift_linear_output* gate_up, int activation, void* H, int h_dtype, void* scratch, size_t scratch_bytes,
                        void* levels_buf, size_t levels_bytes, int levels_ready, const qift_decode_ahead* ahead, void* stream) {
     if (!X || (x_dtype != QIFT_F32 && x_dtype != QIFT_BF16)) return QIFT_ERR_INVALID_ARG;
-    int rc = check_gated(M, K, levels, gate_up, activation, H, h_dtype, levels_buf, levels_bytes, ahead);
+    int rc = check_gated(M, K, levels, gate_up, activation, H, h_dtype, levels_buf, levels_bytes, levels_ready, ahead);
     if (rc != QIFT_OK) return rc;
     if (!scratch || scratch_bytes < qift_gated_forward_scratch_bytes(M, K)) return QIFT_ERR_WORKSPACE;
     if ((reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return QIFT_ERR_ALIGNMENT;

@@ -133,3 +133,51 @@ def test_weights_of_another_size_are_refused():
         qift.qift_gated_linear(torch.zeros((3, 1024), dtype=torch.int8, device="cuda"), c.s, *c.weights, c.lv)
     with pytest.raises(qift.QiftError):
         qift.qift_gated_linear(c.q, c.s, (pg, sg), (up[0], up[1][:32]), c.lv)
+
+
+@pytest.mark.parametrize("levels, M, N, K", [
+    ("mnz", 5, 40, 28672), ("mnz", 16, 40, 28672), ("int3", 16, 130, 16384), ("int4", 12, 40, 20008), ("int4", 7, 33, 16384), ("pot", 1, 20, 225280),
+    ("sym", 1, 20, 231424), ("mnz", 2, 300, 240000), ("int4", 1, 9, 240008), ("int4", 3, 20, 1 << 21)])
+def test_long_rows(levels, M, N, K):
+    """Few rows whose activations, beside the rings of codes, pass what shared memory holds."""
+    c = Case(M + K, M, N, K, levels)
+    h, *accs = run(c, want_acc=True)
+    c.check(h, accs)
+    assert qift.qift_device_status()[0] == qift.OK
+
+
+def test_longest_sums():
+    """Every operand at the end of its range over 2^21 codes: beyond 32 bits once the factors of the tensor cores' operands are on."""
+    for K in ((1 << 21) - 16, 1 << 21):
+        table = oracle.level_table(qift.INT4)
+        low = int(np.min(table))
+        packed = torch.from_numpy(oracle.pack(np.full((2, K), int(np.argmin(table)), np.uint8), qift.INT4).view(np.int32).ravel()).cuda()
+        s_n, s_a = torch.full((2,), 1e-9, device="cuda"), torch.ones(20, device="cuda")
+        q = torch.full((20, K), -8, dtype=torch.int8, device="cuda")
+        h, a, b = qift.qift_gated_linear(q, s_a, (packed, s_n), (packed, s_n), qift.INT4, want_acc=True)
+        assert (a == -8 * low * K).all() and torch.equal(a, b)
+        check(h, [a, b], s_a, [s_n, s_n], qift.ACT_SILU)
+
+
+@pytest.mark.parametrize("levels", list(LEVELS))
+@pytest.mark.parametrize("M, N, K", [(450, 150, 512), (512, 257, 256), (700, 96, 1056), (1025, 264, 288), (1300, 131, 544)])
+def test_decoded_by_an_earlier_call(M, N, K, levels):
+    """Levels that are there, from the fewest rows on that use them: the same bits as from the codes."""
+    c = Case(M + N, M, N, K, levels)
+    buf = torch.zeros(qift.qift_levels_bytes(K, c.weights), dtype=torch.uint8, device="cuda")
+    few = qift.qift_gated_linear(c.q[:40].contiguous(), c.s[:40].contiguous(), *c.weights, c.lv, ahead=(c.weights, K, c.lv, buf))
+    h, *accs = run(c, levels_buf=buf, levels_ready=True, want_acc=True)
+    c.check(h, accs)
+    assert torch.equal(h, run(c)) and torch.equal(h[:40], few)
+    assert torch.equal(run(c, dtype=torch.bfloat16, levels_buf=buf, levels_ready=True), h.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("N", [120, 131])
+def test_many_rows_same_bits(N):
+    """Rows of a call that decodes the codes first against calls of fewer rows."""
+    c = Case(N, qift.qift_gated_levels_min_rows() + 70, N, 512, "sym")
+    whole = run(c, qift.ACT_GELU_TANH)
+    c.check(whole, act=qift.ACT_GELU_TANH)
+    for M in (1, 30, 300, 600):
+        part = qift.qift_gated_linear(c.q[-M:].clone(), c.s[-M:].clone(), *c.weights, c.lv, activation=qift.ACT_GELU_TANH)
+        assert torch.equal(part, whole[-M:]), M

@@ -96,3 +96,12 @@ def test_sizes(L):
     assert 129 <= qift.qift_gated_levels_min_rows() <= 4096
     ahead = binding.DecodeAhead(ctypes.addressof(outputs()), 2, 256, 0, 0, None, 0, None)
     assert linear(L, ahead=ctypes.addressof(ahead)) == ARG
+
+
+def test_more_requests_than_their_numbers_have_room_for(L):
+    assert begin(L, R=(1 << 30) + 1, most=1) == SHAPE and end(L, R=(1 << 30) + 1, most=1) == SHAPE
+
+
+@pytest.mark.parametrize("bad, status", [(dict(buf=NULL), SPACE), (dict(buf_bytes=2 * 64 * 256 - 1), SPACE), (dict(buf=4224), ALIGN)])
+def test_levels_that_are_there_have_to_be_given(L, bad, status):
+    assert linear(L, M=1000, ready=1, **bad) == status

@@ -40,14 +40,15 @@ class Case:
 
 
 def check(h, sums, s_a, s_n, act):
-    """g and u are two rounded multiplies of the exact sums.  From there on: exp within 2 ulp and the sum, the quotient and the last product
-    one rounding each: 6 U of h (a unit in the last place is 2 U).  The GELU's argument z takes six roundings, 6 |z| U of
-    exp(-z), of which the quotient passes on at most all.  Where exp(-z) passes the range, or the quotient is denormal, 2^-126 of the rest."""
+    """g and u are two rounded multiplies of the exact sums.  From there on, a unit in the last place being 2 U: exp within 2 ulp, of which the
+    quotient passes on at most all (4 U), the sum one rounding (U), the quotient, by way of a reciprocal, within 2 ulp (4 U), the last product one
+    rounding (U): 10 U of h.  The GELU's argument z takes six roundings, 6 |z| U of exp(-z), of which the quotient passes on sigmoid(-z).
+    Where exp(-z) passes the range, or the quotient is denormal, 2^-126 of the rest."""
     g, u = (a.float() * s_a[:, None] * s for a, s in zip(sums, s_n))
     g, u = g.double(), u.double()
     z = g if act == qift.ACT_SILU else 2 * np.sqrt(2 / np.pi) * (g + 0.044715 * g ** 3)
     want = g * torch.sigmoid(z) * u
-    off = 7 * U + (6 * U * z.abs() * torch.sigmoid(-z) if act != qift.ACT_SILU else 0)
+    off = 10 * U + (6 * U * z.abs() * torch.sigmoid(-z) if act != qift.ACT_SILU else 0)
     bound = want.abs() * off + (g * u).abs() * 2.0 ** -126 + (1 + u.abs()) * 2.0 ** -148
     if h.dtype == torch.bfloat16:
         bound = bound + (want.abs() + bound) * 2.0 ** -8

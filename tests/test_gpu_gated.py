@@ -181,3 +181,18 @@ def test_many_rows_same_bits(N):
     for M in (1, 30, 300, 600):
         part = qift.qift_gated_linear(c.q[-M:].clone(), c.s[-M:].clone(), *c.weights, c.lv, activation=qift.ACT_GELU_TANH)
         assert torch.equal(part, whole[-M:]), M
+
+
+@pytest.mark.parametrize("M, N", [(64, 33_600_016), (1100, 1_960_008)])
+def test_more_results_than_32_bits_count(M, N):
+    """Row by row the same as calls of one row."""
+    K = 32
+    assert M * N > 1 << 31
+    g = torch.Generator("cuda").manual_seed(N)
+    weights = [(torch.randint(-2 ** 31, 2 ** 31 - 1, ((N + 15) // 16 * 256,), dtype=torch.int32, device="cuda", generator=g),
+                torch.rand(N, device="cuda", generator=g)) for _ in range(2)]
+    q = torch.randint(-8, 8, (M, K), dtype=torch.int8, device="cuda", generator=g)
+    s = torch.rand(M, device="cuda", generator=g)
+    whole = qift.qift_gated_linear(q, s, *weights, qift.MNZ, out_dtype=torch.bfloat16)
+    for m in (0, M // 2, M - 1):
+        assert torch.equal(whole[m], qift.qift_gated_linear(q[m:m + 1].clone(), s[m:m + 1].clone(), *weights, qift.MNZ, out_dtype=torch.bfloat16)[0]), m

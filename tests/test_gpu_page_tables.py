@@ -173,3 +173,25 @@ def test_captured_and_replayed_on_another_stream(total):
             assert np.array_equal(x.cpu().numpy(), y)
         b.same()
         f = keep
+
+
+def test_places_beyond_32_bits():
+    """Requests that end at 2^31 - 1 tokens, in a pool of 2^32 (whose memory the calls do not touch)."""
+    page, most, pages = 1024, 2 ** 21, 2 ** 22
+    plain = Tables(np.full((2, most), -1), np.arange(pages), pages, page, pages)
+    table, free, count = ints(plain.table), ints(plain.free), ints([pages])
+    rows, first, total = ints([3000, 2]), ints([2 ** 31 - 2500, 2 ** 31 - 2]), 3010
+    start, position, lost = ints(np.zeros(3)), ints(np.zeros(total)), ints([0])
+    slot = torch.zeros(total, dtype=torch.int64, device="cuda")
+    at = [t.data_ptr() for t in (rows, first, table, free, count, start, position, slot, lost)]
+    stream = torch.cuda.current_stream().cuda_stream
+    assert qift.lib().qift_kv4_pages_begin(at[0], at[1], 2, at[2], most, pages, page, at[3], at[4], None, 0, total, at[5], at[6], at[7], at[8], stream) == qift.OK
+    want = plain.begin([3000, 2], [2 ** 31 - 2500, 2 ** 31 - 2], total)
+    for x, y in zip((start, position, slot), want):
+        assert np.array_equal(x.cpu().numpy(), y)
+    assert int(lost) == want[3] == 500 and int(slot.max()) > 2 ** 31
+    assert np.array_equal(table.cpu().numpy(), plain.table) and int(count) == plain.count
+    length = ints([2 ** 31 - 2000, 0])
+    assert qift.lib().qift_kv4_pages_end(length.data_ptr(), None, 2, at[2], most, pages, page, at[3], at[4], stream) == qift.OK
+    plain.end([2 ** 31 - 2000, 0], None)
+    assert np.array_equal(table.cpu().numpy(), plain.table) and int(count) == plain.count and np.array_equal(free.cpu().numpy(), plain.free)

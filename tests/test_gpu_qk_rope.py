@@ -123,3 +123,15 @@ def test_captured_on_another_stream():
         graph.replay()
         check(oq, q, position, inv, None, 1e-6, False)
         check(ok, k, position, inv, None, 1e-6, False)
+
+
+def test_rows_far_apart():
+    """Strides whose multiples pass 2^31 elements, in and out."""
+    step, position, inv = 2 ** 30 + 8, torch.tensor([5, -1, 70], dtype=torch.int32, device="cuda"), frequencies(64)
+    q, k, w = normal(1, (3, 2, 64), torch.bfloat16), normal(2, (3, 1, 64), torch.bfloat16), normal(3, (64,), torch.bfloat16)
+    space = torch.empty(2 * step + 4096, dtype=torch.bfloat16, device="cuda")
+    fq, fk = space.as_strided((3, 2, 64), (step, 64, 1)), space.as_strided((3, 1, 64), (step, 64, 1), 1024)
+    fq.copy_(q), fk.copy_(k)
+    qift.qift_qk_norm_rope(fq, fk, position, inv, w, w, q_out=fq, k_out=fk)
+    check(fq, q, position, inv, w, 1e-6, False, q)
+    check(fk, k, position, inv, w, 1e-6, False, k)

@@ -7,9 +7,9 @@
 //   warp 0        fills a ring of steps (256 codes deep) with tensor copies: the packed words of both matrices (three dimensions: a row's 64
 //                 bytes of a slice, swizzled; rows; blocks of sixteen rows) and the q_a rows of the token block, two 128-byte k-blocks
 //   warps 1, 2    issue the products D[matrix][128 channels x tokens] of a matrix each, eight a step
-//   warps 4-19    expanders, two per matrix and lane quarter, a k-block of a step each: the packed words of their 32 channels, one to four
-//                 operations per operand word, tcgen05.st into the matrix's ring of two steps; then the epilogue, four per lane
-//                 quarter on 8-token pieces by turns: both accumulators, h, stores of 32 channels
+//   warps 4-19    expanders, two per matrix and lane quarter, for the even and the odd steps: the packed words of their 32 channels, one to
+//                 four operations per operand word, tcgen05.st into their slot of the matrix's operands; then the epilogue, four per
+//                 lane quarter on 8-token pieces by turns: both accumulators, h, stores of 32 channels
 //
 // Activations come as they are, and there is no launch before this one: the operand bytes are the levels themselves times a power of two, made
 // by moving a code to the top of its byte -- (code << 6) ^ 0xa0 = 32 (2 code - 3) as a signed byte, (code << 6) ^ 0x80 = 64 (code - 2), the
@@ -18,10 +18,14 @@
 // Token blocks of one channel tile are neighbours in the item list, so that its codes come from L2 for all but the first.
 //
 // Bounds: a 128 x N x 32 product takes N / 2 cycles of the tensor cores, 16 at least; operands enter tensor memory at 128 bytes a cycle
-// (1 MB an item of K = 4096: 4.3 us); their logic is 56 operations per k-block and warp.  A thread that a whole warp has elected issues a
-// product in 16 cycles; one that a comparison of lanes has picked takes 60 (the compiler cannot know it is alone, and tries every
-// lane's operands), which alone set the pace at first: 23 us for 48 rows, 4096 -> 14336.  Waits carry no time hint (with one they
-// are a loop around a sleep) and are bounded by their trips.
+// (1 MB an item of K = 4096: 4.3 us); their logic is 56 operations per k-block and warp.  What sets the pace is handing over: with logic,
+// tensor memory stores and seven of eight products left out, 48 rows, 4096 -> 14336, still took 13.5 of 15.6 us.  So a step passes
+// through as few barriers as there are roles: an expander waits twice for its 256 codes of every second step, and its partner's
+// step is expanded meanwhile (each step shared between both: 8 to 15 % longer over 8192 codes; a hand-over per 128 codes: 15 to 25 %).  A
+// thread that a whole warp has elected issues a product in 16 cycles; one that a comparison of lanes has picked takes 60 (the compiler
+// cannot know it is alone, and tries every lane's operands), which alone set the pace at first: 23 us for 48 rows.  Waits carry no time
+// hint (with one they are a loop around a sleep) and are bounded by their trips.  4096 -> 14336 in two bits: 17 rows 13.9 us, 48 rows
+// 15.6, 128 rows 20; one CTA's item takes 11 us from launch to end, of which the epilogue of 48 rows 1.5 (issue: 35 instructions an output).
 #pragma once
 
 #include "common.cuh"
@@ -157,8 +161,8 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
 
     pdl_launch_dependents();
     if (warp == 0 && lane == 0) {
-        for (int s = 0; s < stages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 2 + kGtExpanders);
-        for (int s = 0; s < 2 * kGtRing; ++s) mbar_init(&a_full[s], 8), mbar_init(&a_empty[s], 1);
+        for (int s = 0; s < stages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 2 + kGtExpanders / 2);
+        for (int s = 0; s < 2 * kGtRing; ++s) mbar_init(&a_full[s], 4), mbar_init(&a_empty[s], 1);
         mbar_init(d_full, 2), mbar_init(d_empty, kGtExpanders);
         *fail = 0;
         mbar_fence_init();
@@ -174,35 +178,34 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
 
     if (warp == 0) {
         // ------------------------------------------------------------------ words and activations
-        auto words = [&](int s, int item, int step) {
-            const int rb = (item / tp.blocks) * 8;
+        auto words = [&](int s, int rb, int step) {
             mbar_expect_tx(&full[s], stage_bytes);
             tma_load_3d(staged + s * stage_bytes, &maps.words[0], 0, step * (SPS * SROWS), rb, &full[s]);
             tma_load_3d(staged + s * stage_bytes + WORDS, &maps.words[1], 0, step * (SPS * SROWS), rb, &full[s]);
         };
-        auto activations = [&](int s, int item, int step) {
+        auto activations = [&](int s, int m0, int step) {
             unsigned char* to = staged + s * stage_bytes + 2 * WORDS;
-            const int m0 = (item % tp.blocks) * ntok;
             tma_load_2d(to, &maps.act, step * 256, m0, &full[s]);
             tma_load_2d(to + act_bytes, &maps.act, step * 256 + 128, m0, &full[s]);
         };
         // the words depend on no kernel before this one: the first stages' are asked for before the wait for it
         const int early = min(stages, steps);
         for (int i = 0, step = first_step; i < early; ++i, step = step + 1 == steps ? 0 : step + 1)
-            if (elect_one()) words(i, blockIdx.x, step);
+            if (elect_one()) words(i, (blockIdx.x / tp.blocks) * 8, step);
         pdl_wait();
         int s = 0, k = 0;
         uint32_t ph = 1;                                               // the first round finds the stages empty
         bool ok = true;
         for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
+            const int rb = (item / tp.blocks) * 8, m0 = (item % tp.blocks) * ntok;
             for (int i = 0, step = first_step; i < steps; ++i, ++k) {
                 if (!mbar_wait_near(&empty[s], ph, 82)) {
                     *fail = 1, ok = false;
                     break;
                 }
                 if (elect_one()) {
-                    if (k >= early) words(s, item, step);
-                    activations(s, item, step);
+                    if (k >= early) words(s, rb, step);
+                    activations(s, m0, step);
                 }
                 __syncwarp();
                 if (++s == stages) s = 0, ph ^= 1;
@@ -245,62 +248,70 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
     } else if (warp >= kGtExpander0) {
         // ------------------------------------------------------------------ operands, then the epilogue
         const int quarter = warp & 3;                                  // the lanes of tensor memory that this warp can reach
-        const int e = warp - kGtExpander0, mat = (e >> 2) & 1, half = e >> 3;   // its matrix, its k-block of a step
-        // its words of a step: two 16-byte pieces of a row (INT4: all four of a slice); pieces are exclusive-ored by (row >> 1) & 3
+        const int e = warp - kGtExpander0, mat = (e >> 2) & 1, odd = e >> 3;    // its matrix; the even or the odd steps
+        // its words of a k-block: two 16-byte pieces of a row (INT4: all four of a slice); pieces are exclusive-ored by (row >> 1) & 3
         constexpr int PIECES = SPS == 2 ? 4 : 2;
         const uint32_t rows64 = smem_u32(staged) + mat * WORDS + (2 * quarter + (lane >> 4)) * RB;
-        const uint32_t get = rows64 + (SPS == 2 ? half * 1024 : 0) + (lane & 15) * 64;
-        const uint32_t put = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + kGtOperands + mat * kGtRing * 64 + half * 32;
+        const uint32_t get = rows64 + (lane & 15) * 64;
+        const uint32_t put = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + kGtOperands + (mat * kGtRing + odd) * 64;
         const uint32_t get_hi = rows64 + 1024 + (lane & 7) * 64 + ((lane >> 3) & 1) * 8;   // INT3: rows 16 .. 23: {third bits of row r, of row r + 8}
-        uint32_t at[PIECES];
+        uint32_t at[4];
 #pragma unroll
-        for (int j = 0; j < PIECES; ++j) at[j] = ((SPS == 2 ? j : 2 * half + j) ^ ((lane >> 1) & 3)) << 4;
+        for (int j = 0; j < 4; ++j) at[j] = (j ^ ((lane >> 1) & 3)) << 4;
+        uint64_t* const mine_empty = &a_empty[mat * kGtRing + odd];
+        uint64_t* const mine_full = &a_full[mat * kGtRing + odd];
         const GateFunction act(p.act);
         pdl_wait();
         // a wait that has run out is not tried again: the warp goes through the motions, keeps coming to the barriers of the sixteen and stores nothing
         bool ok = true;
         int s = 0, count = 0;
-        uint32_t ph = 0, turn = 0, a_ph = 1;
+        uint32_t ph = 0, turn = 0, a_ph = 1;                           // turn: the running step's parity
         for (int item = blockIdx.x; item < items; item += gridDim.x, ++count) {
             const int m0 = (item % tp.blocks) * ntok, n0 = (item / tp.blocks) * kGtRows;
-            const int rows = min(ntok, p.M - m0);
+            const int rows = min(ntok, p.M - m0), n = n0 + quarter * 32 + lane;
+            float sg = 0.0f, su = 0.0f;                                // asked for long before they are needed
+            if (n < p.N) sg = __ldg(p.w[0].s_n + n), su = __ldg(p.w[1].s_n + n);
             const int r = 32 * e + lane;
             if (r < ntok) scale[r] = r < rows ? p.s_a[m0 + r] : 0.0f;
-            for (int i = 0; i < steps; ++i) {
-                if (ok) ok = mbar_wait_near(&full[s], ph, 87);
-                uint32_t w[4 * PIECES], hi[4] = {};
-                const uint32_t from = get + s * stage_bytes;
+            for (int i = 0; i < steps; ++i, turn ^= 1) {
+                if (turn == odd) {
+                    if (ok) ok = mbar_wait_near(&full[s], ph, 87);
+                    uint32_t w[2][4 * PIECES], hi[2][4] = {};
+                    const uint32_t from = get + s * stage_bytes;
 #pragma unroll
-                for (int j = 0; j < PIECES; ++j) {
-                    const uint4 v = lds128(from + at[j]);
-                    w[4 * j] = v.x, w[4 * j + 1] = v.y, w[4 * j + 2] = v.z, w[4 * j + 3] = v.w;
-                    if constexpr (LV == QIFT_LEVELS_INT3) {
-                        const uint2 u = lds64(get_hi + s * stage_bytes + at[j]);
-                        hi[2 * j] = u.x, hi[2 * j + 1] = u.y;
-                    }
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int j = 0; j < PIECES; ++j) {
+                            const uint32_t piece = at[SPS == 2 ? j : 2 * half + j];
+                            const uint4 v = lds128(from + (SPS == 2 ? half * 1024 : 0) + piece);
+                            w[half][4 * j] = v.x, w[half][4 * j + 1] = v.y, w[half][4 * j + 2] = v.z, w[half][4 * j + 3] = v.w;
+                            if constexpr (LV == QIFT_LEVELS_INT3) {
+                                const uint2 u = lds64(get_hi + s * stage_bytes + piece);
+                                hi[half][2 * j] = u.x, hi[half][2 * j + 1] = u.y;
+                            }
+                        }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&empty[s]);
+                    uint32_t o[32];
+                    gt_operands<LV>(w[0], hi[0], o);
+                    if (ok) ok = mbar_wait_near(mine_empty, a_ph, 88);
+                    tc_fence_after();
+                    tc_st32(put, o);
+                    gt_operands<LV>(w[1], hi[1], o);
+                    tc_st32(put + 32, o);
+                    tc_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(mine_full);
+                    a_ph ^= 1;
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&empty[s]);
-                uint32_t o[32];
-                gt_operands<LV>(w, hi, o);
-                if (ok) ok = mbar_wait_near(&a_empty[mat * kGtRing + turn], a_ph, 88);
-                tc_fence_after();
-                tc_st32(put + turn * 64, o);
-                tc_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&a_full[mat * kGtRing + turn]);
                 if (++s == stages) s = 0, ph ^= 1;
-                if ((turn ^= 1) == 0) a_ph ^= 1;
             }
             if (!ok) *fail = 1;
             asm volatile("bar.sync 1, %0;" ::"n"(32 * kGtExpanders) : "memory");      // the scales are there
             if (ok && !mbar_wait_near(d_full, count & 1, 89)) ok = false, *fail = 1;
             if (ok) {
                 tc_fence_after();
-                const int n = n0 + quarter * 32 + lane;
-                float sg = 0.0f, su = 0.0f;
-                if (n < p.N) sg = __ldg(p.w[0].s_n + n), su = __ldg(p.w[1].s_n + n);
                 const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
                 // a loop of eight tokens a trip, not more: code that runs once has to be fetched first, which took longer than running it
 #pragma unroll 1

@@ -1997,8 +1997,13 @@ inline int gs_pairs(int M, int N, int K, int lv) {
 }
 // The stream kernel takes calls whose rows leave every warp two slots.  Longer activations go to the tcgen05 kernel, which reads the codes once
 // for all rows: 16 rows of 16384 in blocks that fit, 53248 channels, took 195 us against 111 (INT4 305 and 137); 8 rows of 28672, 8192 channels,
-// 62 and 73 (INT4 95 and 67).
-inline bool gs_applies(int M, int N, int K, int lv) { return M <= kGsMaxM && gs_slots(M, K, lv, gs_pairs(M, N, K, lv)) >= 2; }
+// 62 and 73 (INT4 95 and 67).  From nine rows on, two tiles of tokens, it keeps calls of few tiles of channels an SM and the power-of-two set,
+// whose operands cost the other kernel a table lookup (9 rows, stream and tcgen05; 4096 -> 9472, 592 tiles: 8.7 and 10.1, INT4 12.8 and 10.7;
+// -> 14336: 13.0 and 11.4, INT4 15.3 and 12.7, PoT 14.7 and 15.9; 2048 -> 5120: 5.3 and 6.5, INT4 6.5 both).
+inline bool gs_applies(int M, int N, int K, int lv) {
+    if (M > kGsMaxM || gs_slots(M, K, lv, gs_pairs(M, N, K, lv)) < 2) return false;
+    return M <= 8 || lv == QIFT_LEVELS_POT || (N + 15) / 16 <= (lv == QIFT_LEVELS_INT4 ? 2 : 4) * sm_count() || K % 16 != 0;
+}
 template <int LV, int NT>
 int launch_gated_stream(const GatedParams& p, cudaStream_t st) {
     auto kernel = gated_stream_kernel<LV, NT>;

@@ -196,3 +196,13 @@ def test_more_results_than_32_bits_count(M, N):
     whole = qift.qift_gated_linear(q, s, *weights, qift.MNZ, out_dtype=torch.bfloat16)
     for m in (0, M // 2, M - 1):
         assert torch.equal(whole[m], qift.qift_gated_linear(q[m:m + 1].clone(), s[m:m + 1].clone(), *weights, qift.MNZ, out_dtype=torch.bfloat16)[0]), m
+
+
+@pytest.mark.parametrize("levels", list(LEVELS))
+@pytest.mark.parametrize("M, K", [(9, 512), (16, 1040), (13, 264)])
+def test_some_rows_of_many_channels(M, K, levels):
+    """More tiles of channels than a few for every SM."""
+    K = K if levels == "int4" else K // 32 * 32
+    c = Case(M + K, M, 9600, K, levels)
+    h, *accs = run(c, qift.ACT_GELU_TANH, want_acc=True)
+    c.check(h, accs, act=qift.ACT_GELU_TANH)

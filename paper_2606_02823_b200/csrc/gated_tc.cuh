@@ -19,13 +19,14 @@
 //
 // Bounds: a 128 x N x 32 product takes N / 2 cycles of the tensor cores, 16 at least; operands enter tensor memory at 128 bytes a cycle
 // (1 MB an item of K = 4096: 4.3 us); their logic is 56 operations per k-block and warp.  What sets the pace is handing over: with logic,
-// tensor memory stores and seven of eight products left out, 48 rows, 4096 -> 14336, still took 13.5 of 15.6 us.  So a step passes
+// tensor memory stores and seven of eight products left out, 48 rows, 4096 -> 14336, still took 13.5 of 15.6 us (launches one after the
+// other).  So a step passes
 // through as few barriers as there are roles: an expander waits twice for its 256 codes of every second step, and its partner's
 // step is expanded meanwhile (each step shared between both: 8 to 15 % longer over 8192 codes; a hand-over per 128 codes: 15 to 25 %).  A
 // thread that a whole warp has elected issues a product in 16 cycles; one that a comparison of lanes has picked takes 60 (the compiler
 // cannot know it is alone, and tries every lane's operands), which alone set the pace at first: 23 us for 48 rows.  Waits carry no time
-// hint (with one they are a loop around a sleep) and are bounded by their trips.  4096 -> 14336 in two bits: 17 rows 13.9 us, 48 rows
-// 15.6, 128 rows 20; one CTA's item takes 11 us from launch to end, of which the epilogue of 48 rows 1.5 (issue: 35 instructions an output).
+// hint (with one they are a loop around a sleep) and are bounded by their trips.  4096 -> 14336 in two bits: 9 rows 11.3 us, 48 rows
+// 13.0, 128 rows 17.8, 512 rows 57; of 48 rows 1.5 us are the epilogue (issue: 35 instructions an output).
 #pragma once
 
 #include "common.cuh"

@@ -6,6 +6,9 @@
 // end and needs no second pass.  What bounds them is a chain of dependent loads and barriers (rows, sums over requests, entries, sums over
 // entries, the stack), not bytes: one CTA of 256 threads where that covers the list, clusters of eight CTAs of 1024 that exchange
 // their sums through distributed shared memory otherwise, 4 entries a thread and trip.  Many rows are a second kernel over all SMs.
+// Begin and end together: 64 single tokens behind up to 8000 10.7 us (15.4 in the first form), 192 trees of up to 64 behind
+// 2000 18.5, 256 prompts, 580 000 rows, 23.2 (60).  Cold, under the profiler, the last took 12.1 (begin), 9.5 (rows) and 10.5
+// us (end); what the first and the last of them wait for most is one another's warps, at barriers.
 #pragma once
 
 #include "common.cuh"

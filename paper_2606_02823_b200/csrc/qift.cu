@@ -2191,10 +2191,13 @@ int qift_qk_norm_rope(const void* Q, const void* K, int x_dtype, long long q_str
     int lanes = 2;
     while (lanes * 16 < D) lanes *= 2;
     // A row's heads are split over warps while the rows alone do not fill the SMs; beyond, a warp takes one row, and the next CTA the next ones
-    // (18000 rows dealt to resident warps, three or four each, took 5 % longer).
-    const int trips = (Hq + 32 / lanes - 1) / (32 / lanes) + (H + 32 / lanes - 1) / (32 / lanes);
-    const long long warps = 4ll * kRopeWarps * sm_count();
-    p.parts = static_cast<int>(std::min(static_cast<long long>(trips), (warps + total - 1) / total));
+    // (18000 rows dealt to resident warps, three or four each, took 5 % longer).  Over the fewest warps that fill them, or one less, which is less
+    // than one round of the warps that the SMs hold, where that makes hardly more trips (rows of 32 + 8 heads: 600 over 8 warps 6.8 us,
+    // over 7 5.1; 800 over 6 6.9, over 5 5.7; where trips are more, rows of nobody often leave one round anyway: 1237 rows, 137 of them such, over 4
+    // 18.2, over 3 22.4).
+    const long long trips = (Hq + 32 / lanes - 1) / (32 / lanes) + (H + 32 / lanes - 1) / (32 / lanes), warps = 4ll * kRopeWarps * sm_count();
+    const long long more = std::min(trips, (warps + total - 1) / total), fewer = std::max(1ll, std::min(trips, warps / total));
+    p.parts = static_cast<int>(4 * ((trips + fewer - 1) / fewer) <= 5 * ((trips + more - 1) / more) ? fewer : more);
     const long long blocks = (static_cast<long long>(total) * p.parts + kRopeWarps - 1) / kRopeWarps, most = 64ll * sm_count();
     const dim3 grid(static_cast<unsigned>(std::min(blocks, most)));
     cudaStream_t st = static_cast<cudaStream_t>(stream);

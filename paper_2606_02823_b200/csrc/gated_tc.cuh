@@ -50,7 +50,7 @@ __host__ __device__ constexpr int gt_slices(int lv) { return lv == QIFT_LEVELS_I
 __host__ __device__ constexpr int gt_slice_rows(int lv) { return lv == QIFT_LEVELS_INT3 ? 24 : 16; }      // 64-byte rows of a slice and row block
 __host__ __device__ constexpr int gt_word_bytes(int lv) { return 8 * 64 * gt_slices(lv) * gt_slice_rows(lv); }   // of a step and matrix
 __host__ __device__ inline int gt_stages(int lv, int ntok) {
-    const int n = (kGtSmem - 3072) / (2 * gt_word_bytes(lv) + ntok * 256);
+    const int n = (kGtSmem - 3 * 1024) / (2 * gt_word_bytes(lv) + ntok * 256);
     return n < 8 ? n : 8;
 }
 

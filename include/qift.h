@@ -625,6 +625,15 @@ int qift_device_status(void* stream, uint32_t* detail);
  * QIFT_OK on the next call.  INVALID_ARG for other arguments. */
 int qift_selftest_wait_timeout(int which, unsigned int limit_us, void* stream);
 
+/* The same for the gated calls' kernels: a product of real operands (MNZ codes, SiLU, fp32 H) in which one warp of every CTA, after its first
+ * `waits` waits, waits for what nobody signals.  What depends on that warp stays unwritten in H, what does not is right.
+ *   kernel      0: the one of few rows (M <= 8; warps 0 .. 15), 1: the tcgen05 one (fewer rows than qift_gated_levels_min_rows(); warps
+ *               0 .. 19); the site byte is 81, or one of 82 .. 89
+ *   limit_us    bound of every wait, 1 .. 1 000 000 microseconds
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (what the kernel does not take), ALIGNMENT, WORKSPACE (more rows), CUDA. */
+int qift_selftest_gated_wait(int kernel, int warp, int waits, unsigned int limit_us, const int8_t* q_a, const float* s_a, int M, int K,
+                             const qift_linear_output* gate_up, float* H, void* stream);
+
 /* Measurement helpers (no counterpart in the paper; used by the benchmark to calibrate its roofline
  * denominators on the GPU it runs on; neither touches the quantized layer).
  *   qift_calib_hbm_read   streams `bytes` of device memory at `buf` through 128-bit loads, writes nothing

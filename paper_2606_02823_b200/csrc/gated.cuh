@@ -15,6 +15,7 @@
 
 #include "common.cuh"
 #include "decode.cuh"
+#include "kv4_tree.cuh"
 
 namespace qift {
 
@@ -38,12 +39,35 @@ struct GatedMatrix {
     const float* s_n;       // [N]
     int32_t* acc_debug;     // [M][N] or null
 };
+struct GatedProbe {         // self-test alone (qift_selftest_gated_wait): a warp whose waits, after the first few, are for what nobody signals
+    int warp, waits;
+    uint32_t trips;         // bound of every wait
+};
 struct GatedParams {
     GatedMatrix w[2];       // gate, up
     const int8_t* q_a;      // [M][K]
     const float* s_a;       // [M]
     void* H;                // [M][N]
     int M, N, K, h_bf16, act;
+    GatedProbe probe;
+};
+
+// The bounded waits of a thread.  Lanes have to agree on whether a wait has run out before an instruction of the whole warp depends on it.
+template <bool PROBE>
+struct GatedWait {
+    const GatedProbe& probe;
+    uint64_t* never;        // PROBE: a barrier that nobody arrives at
+    int left;
+    __device__ __forceinline__ GatedWait(const GatedProbe& p, uint64_t* nobody, int warp)
+        : probe(p), never(nobody), left(warp == p.warp ? p.waits : 0x7fffffff) {}
+    __device__ __forceinline__ bool operator()(uint64_t* bar, uint32_t parity, unsigned int site) {
+        if constexpr (PROBE) {
+            const bool held = left-- <= 0;
+            return mbar_wait_near(held ? never : bar, held ? 0u : parity, site, probe.trips);
+        } else {
+            return mbar_wait_near(bar, parity, site);
+        }
+    }
 };
 
 __device__ __forceinline__ void gated_store(const GatedParams& p, size_t at, int acc_g, int acc_u, float s_a, float s_gate, float s_up) {

@@ -55,7 +55,7 @@ __device__ __forceinline__ int gs_result(int S, int sum_q) {
     return S;
 }
 
-template <int LV, int NT>
+template <int LV, int NT, bool PROBE = false>
 __global__ void __launch_bounds__(kGsThreads, 1)
 gated_stream_kernel(const __grid_constant__ GatedParams p, int pairs, int slots) {
     constexpr int PER = codes_per_word(LV), NPL = PER / 4;
@@ -74,6 +74,7 @@ gated_stream_kernel(const __grid_constant__ GatedParams p, int pairs, int slots)
     uint64_t* full = reinterpret_cast<uint64_t*>(act + static_cast<size_t>(M) * slices * SLICE + pairs * gs_exchange_bytes(M)) + warp * slots;
     int* sum_q = reinterpret_cast<int*>(full - warp * slots + 2 * pairs * slots);  // [16]
     volatile int* fail = sum_q + kGsMaxM;
+    uint64_t* never = reinterpret_cast<uint64_t*>(sum_q + kGsMaxM + 2);            // (self-test)
 
     pdl_launch_dependents();
     // this warp's copies run over its tiles, chunk by chunk
@@ -93,6 +94,7 @@ gated_stream_kernel(const __grid_constant__ GatedParams p, int pairs, int slots)
     if (pair < pairs) {
         if (elect_one()) {
             for (int s = 0; s < slots; ++s) mbar_init(&full[s], 1);
+            if (PROBE && warp == 0) mbar_init(never, 1);
             mbar_fence_init();
         }
         __syncwarp();
@@ -174,6 +176,7 @@ gated_stream_kernel(const __grid_constant__ GatedParams p, int pairs, int slots)
             sa[nt][j] = p.s_a[m], sq[nt][j] = sum_q[m];
         }
     const GateFunction function(p.act);
+    GatedWait<PROBE> wait(p.probe, never, warp);
     bool ok = true;
     int s = 0;
     uint32_t ph = 0, turn = 0;
@@ -189,7 +192,7 @@ gated_stream_kernel(const __grid_constant__ GatedParams p, int pairs, int slots)
         int acc[KS][NT][NACC][4] = {};
         for (int c = 0; c < chunks; ++c) {
             // a wait that has run out once is not tried again; the warp goes on to the barriers that its partner waits at
-            if (ok) ok = mbar_wait_near(&full[s], ph, 81);
+            if (ok) ok = __all_sync(0xffffffffu, wait(&full[s], ph, 81));
             const uint32_t w0 = smem_u32(ring + s * SLOT) + lane * 16;
             auto slice = [&](int sl, auto ks) {
                 const uint32_t w = w0 + sl * (16 * WB), q = static_cast<uint32_t>((c * (kGsWords / 16) + sl) * M * SLICE);

@@ -129,7 +129,7 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
                  "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
                  : "memory");
 }
-template <int LV>
+template <int LV, bool PROBE = false>
 __global__ void __launch_bounds__(kGtThreads, 1)
 gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant__ GatedTcParams tp) {
     constexpr int SPS = gt_slices(LV), SROWS = gt_slice_rows(LV), RB = 64 * SPS * SROWS;   // bytes of a row block in a step
@@ -149,9 +149,9 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
     uint64_t* a_empty = a_full + 2 * kGtRing;
     uint64_t* d_full = a_empty + 2 * kGtRing;
     uint64_t* d_empty = d_full + 1;
-    float* scale = reinterpret_cast<float*>(d_empty + 1);             // [kGtTokens] of the tokens
+    uint64_t* never = d_empty + 1;                                    // (self-test)
+    float* scale = reinterpret_cast<float*>(never + 1);               // [kGtTokens] of the tokens
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(scale + kGtTokens);
-    volatile int* fail = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int steps = (packed_pitch(p.K, LV) / 16 + SPS - 1) / SPS;
@@ -165,7 +165,7 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
         for (int s = 0; s < stages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 2 + kGtExpanders / 2);
         for (int s = 0; s < 2 * kGtRing; ++s) mbar_init(&a_full[s], 4), mbar_init(&a_empty[s], 1);
         mbar_init(d_full, 2), mbar_init(d_empty, kGtExpanders);
-        *fail = 0;
+        if constexpr (PROBE) mbar_init(never, 1);
         mbar_fence_init();
     }
     if (warp == 1) {
@@ -176,6 +176,7 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    GatedWait<PROBE> wait(p.probe, never, warp);
 
     if (warp == 0) {
         // ------------------------------------------------------------------ words and activations
@@ -191,47 +192,43 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
         };
         // the words depend on no kernel before this one: the first stages' are asked for before the wait for it
         const int early = min(stages, steps);
-        for (int i = 0, step = first_step; i < early; ++i, step = step + 1 == steps ? 0 : step + 1)
-            if (elect_one()) words(i, (blockIdx.x / tp.blocks) * 8, step);
-        pdl_wait();
-        int s = 0, k = 0;
-        uint32_t ph = 1;                                               // the first round finds the stages empty
-        bool ok = true;
-        for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
-            const int rb = (item / tp.blocks) * 8, m0 = (item % tp.blocks) * ntok;
-            for (int i = 0, step = first_step; i < steps; ++i, ++k) {
-                if (!mbar_wait_near(&empty[s], ph, 82)) {
-                    *fail = 1, ok = false;
-                    break;
-                }
-                if (elect_one()) {
+        if (elect_one()) {
+            for (int i = 0, step = first_step; i < early; ++i, step = step + 1 == steps ? 0 : step + 1) words(i, (blockIdx.x / tp.blocks) * 8, step);
+            pdl_wait();
+            int s = 0, k = 0;
+            uint32_t ph = 1;                                           // the first round finds the stages empty
+            bool ok = true;
+            for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
+                const int rb = (item / tp.blocks) * 8, m0 = (item % tp.blocks) * ntok;
+                for (int i = 0, step = first_step; i < steps; ++i, ++k) {
+                    if (!(ok = wait(&empty[s], ph, 82))) break;
                     if (k >= early) words(s, rb, step);
                     activations(s, m0, step);
+                    if (++s == stages) s = 0, ph ^= 1;
+                    if (++step == steps) step = 0;
                 }
-                __syncwarp();
-                if (++s == stages) s = 0, ph ^= 1;
-                if (++step == steps) step = 0;
             }
+            // given up: what has been asked for still arrives before the CTA ends
+            for (int i = 0; !ok && i < min(k > early ? k : early, stages); ++i) mbar_wait(&full[i], ((max(k, early) - 1 - i) / stages) & 1, 82, 1000000ull);
         }
-        // given up: what has been asked for still arrives before the CTA ends
-        for (int i = 0; !ok && i < min(k > early ? k : early, stages); ++i) mbar_wait(&full[i], ((max(k, early) - 1 - i) / stages) & 1, 82, 1000000ull);
+        __syncwarp();
     } else if (warp <= 2) {
         // ------------------------------------------------------------------ products of a matrix
         const int mat = warp - 1;
         const uint64_t desc0 = make_kmajor_sw128_desc(smem_u32(staged) + 2 * WORDS);
         const uint32_t d = tmem + mat * ntok, a = tmem + kGtOperands + mat * kGtRing * 64;
-        int s = 0, count = 0;
-        uint32_t ph = 0, turn = 0, turn_ph = 0;                        // turn: the step's slot of operands, the parity of its running number
-        bool ok = true;
-        for (int item = blockIdx.x; item < items && ok; item += gridDim.x, ++count) {
-            if (count > 0) ok = mbar_wait_near(d_empty, (count - 1) & 1, 83);
-            tc_fence_after();
-            for (int i = 0; i < steps; ++i) {
-                if (ok) ok = mbar_wait_near(&full[s], ph, 84);
-                if (ok) ok = mbar_wait_near(&a_full[mat * kGtRing + turn], turn_ph, 85);
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
+        if (elect_one()) {
+            int s = 0, count = 0;
+            uint32_t ph = 0, turn = 0, turn_ph = 0;                    // turn: the step's slot of operands, the parity of its running number
+            uint32_t issued = 0;                                       // steps
+            bool ok = true;
+            for (int item = blockIdx.x; item < items && ok; item += gridDim.x, ++count) {
+                if (count > 0) ok = wait(d_empty, (count - 1) & 1, 83);
+                for (int i = 0; i < steps; ++i) {
+                    if (ok) ok = wait(&full[s], ph, 84);
+                    if (ok) ok = wait(&a_full[mat * kGtRing + turn], turn_ph, 85);
+                    if (!ok) break;
+                    tc_fence_after();
                     const uint64_t b = desc0 + s * (stage_bytes >> 4);
                     const uint32_t at = a + turn * 64;
 #pragma unroll
@@ -239,13 +236,15 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
                     tc_commit(&a_empty[mat * kGtRing + turn]);
                     tc_commit(&empty[s]);
                     if (i + 1 == steps) tc_commit(d_full);
+                    ++issued;
+                    if (++s == stages) s = 0, ph ^= 1;
+                    if ((turn ^= 1) == 0) turn_ph ^= 1;
                 }
-                __syncwarp();
-                if (++s == stages) s = 0, ph ^= 1;
-                if ((turn ^= 1) == 0) turn_ph ^= 1;
             }
+            // products under way end before the CTA does, also where nobody waits for their sums any more
+            if (issued) mbar_wait_near(&a_empty[mat * kGtRing + ((issued - 1) & 1)], ((issued - 1) >> 1) & 1, 86);
         }
-        if (!ok) *fail = 1;
+        __syncwarp();
     } else if (warp >= kGtExpander0) {
         // ------------------------------------------------------------------ operands, then the epilogue
         const int quarter = warp & 3;                                  // the lanes of tensor memory that this warp can reach
@@ -263,7 +262,9 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
         uint64_t* const mine_full = &a_full[mat * kGtRing + odd];
         const GateFunction act(p.act);
         pdl_wait();
-        // a wait that has run out is not tried again: the warp goes through the motions, keeps coming to the barriers of the sixteen and stores nothing
+        // A wait that has run out is not tried again: the warp keeps coming to the barriers of the sixteen and hands nothing over any more.  Without its
+        // operands the products of the item never end, so that no warp stores any of it, and without its word that the sums have been read
+        // there is no next item.
         bool ok = true;
         int s = 0, count = 0;
         uint32_t ph = 0, turn = 0, a_ph = 1;                           // turn: the running step's parity
@@ -275,8 +276,8 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
             const int r = 32 * e + lane;
             if (r < ntok) scale[r] = r < rows ? p.s_a[m0 + r] : 0.0f;
             for (int i = 0; i < steps; ++i, turn ^= 1) {
-                if (turn == odd) {
-                    if (ok) ok = mbar_wait_near(&full[s], ph, 87);
+                if (ok && turn == odd) {
+                    ok = wait(&full[s], ph, 87);
                     uint32_t w[2][4 * PIECES], hi[2][4] = {};
                     const uint32_t from = get + s * stage_bytes;
 #pragma unroll
@@ -291,26 +292,25 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
                                 hi[half][2 * j] = u.x, hi[half][2 * j + 1] = u.y;
                             }
                         }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&empty[s]);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (ok && lane == 0) mbar_arrive(&empty[s]);
                     uint32_t o[32];
                     gt_operands<LV>(w[0], hi[0], o);
-                    if (ok) ok = mbar_wait_near(mine_empty, a_ph, 88);
-                    tc_fence_after();
+                    if (ok) ok = wait(mine_empty, a_ph, 88);
+                    tc_fence_after();                                  // (operands without a slot spoil sums that nobody will be given)
                     tc_st32(put, o);
                     gt_operands<LV>(w[1], hi[1], o);
                     tc_st32(put + 32, o);
                     tc_wait_st();
                     tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(mine_full);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (ok && lane == 0) mbar_arrive(mine_full);
                     a_ph ^= 1;
                 }
                 if (++s == stages) s = 0, ph ^= 1;
             }
-            if (!ok) *fail = 1;
             asm volatile("bar.sync 1, %0;" ::"n"(32 * kGtExpanders) : "memory");      // the scales are there
-            if (ok && !mbar_wait_near(d_full, count & 1, 89)) ok = false, *fail = 1;
+            if (ok) ok = __all_sync(0xffffffffu, wait(d_full, count & 1, 89));
             if (ok) {
                 tc_fence_after();
                 const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
@@ -357,7 +357,7 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
                 tc_fence_before();
             }
             asm volatile("bar.sync 1, %0;" ::"n"(32 * kGtExpanders) : "memory");       // and have been read
-            if (lane == 0) mbar_arrive(d_empty);
+            if (ok && lane == 0) mbar_arrive(d_empty);
         }
     }
 

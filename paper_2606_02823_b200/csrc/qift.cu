@@ -2004,9 +2004,9 @@ inline bool gs_applies(int M, int N, int K, int lv) {
     if (M > kGsMaxM || gs_slots(M, K, lv, gs_pairs(M, N, K, lv)) < 2) return false;
     return M <= 8 || lv == QIFT_LEVELS_POT || (N + 15) / 16 <= (lv == QIFT_LEVELS_INT4 ? 2 : 4) * sm_count() || K % 16 != 0;
 }
-template <int LV, int NT>
+template <int LV, int NT, bool PROBE = false>
 int launch_gated_stream(const GatedParams& p, cudaStream_t st) {
-    auto kernel = gated_stream_kernel<LV, NT>;
+    auto kernel = gated_stream_kernel<LV, NT, PROBE>;
     const int tiles = (p.N + 15) / 16, grid = std::min(tiles, sm_count()), chunks = (packed_pitch(p.K, LV) + kGsWords - 1) / kGsWords;
     const int pairs = gs_pairs(p.M, p.N, p.K, LV), each = (tiles + grid * pairs - 1) / (grid * pairs);
     const int slots = static_cast<int>(std::min<long long>(gs_slots(p.M, p.K, LV, pairs), static_cast<long long>(each) * chunks));
@@ -2034,7 +2034,7 @@ bool make_words_map(CUtensorMap* map, const uint32_t* packed, int N, int pitch, 
               CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int LV>
+template <int LV, bool PROBE = false>
 int run_gated_tc(const GatedParams& p, cudaStream_t st) {
     GatedTcParams tp{};
     tp.g = p, tp.blocks = (p.M + kGtTokens - 1) / kGtTokens;
@@ -2045,7 +2045,7 @@ int run_gated_tc(const GatedParams& p, cudaStream_t st) {
     if (!make_i8_map(&maps.act, p.q_a, p.M, p.K, tp.ntok)) return QIFT_ERR_CUDA;
     for (int i = 0; i < 2; ++i)
         if (!make_words_map(&maps.words[i], p.w[i].packed, p.N, packed_pitch(p.K, LV), gt_slice_rows(LV), gt_slices(LV))) return QIFT_ERR_CUDA;
-    auto kernel = gated_tc_kernel<LV>;
+    auto kernel = gated_tc_kernel<LV, PROBE>;
     const cudaError_t e = allow_smem(kernel, kGtSmem);
     if (e != cudaSuccess) return cuda_status(e);
     const long long items = static_cast<long long>((p.N + kGtRows - 1) / kGtRows) * tp.blocks;
@@ -2207,6 +2207,22 @@ int qift_qk_norm_rope(const void* Q, const void* K, int x_dtype, long long q_str
 }
 
 int qift_gated_levels_min_rows(void) { return kGatedLevelsMinM; }
+
+int qift_selftest_gated_wait(int kernel, int warp, int waits, unsigned int limit_us, const int8_t* q_a, const float* s_a, int M, int K,
+                             const qift_linear_output* gate_up, float* H, void* stream) {
+    if (!q_a || !s_a || (kernel != 0 && kernel != 1) || warp < 0 || waits < 0 || limit_us == 0 || limit_us > 1000000u) return QIFT_ERR_INVALID_ARG;
+    if (warp >= (kernel == 0 ? kGsThreads : kGtThreads) / 32) return QIFT_ERR_INVALID_ARG;
+    const int rc = check_gated(M, K, QIFT_LEVELS_MNZ, gate_up, QIFT_ACT_SILU, H, QIFT_F32, nullptr, 0, 0, nullptr);
+    if (rc != QIFT_OK) return rc;
+    if (kernel == 0 ? M > 8 || !gs_applies(M, gate_up[0].N, K, QIFT_LEVELS_MNZ) : K >= kGtMaxK) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(q_a) || !aligned16(s_a)) return QIFT_ERR_ALIGNMENT;
+    GatedParams p{};
+    for (int i = 0; i < 2; ++i) p.w[i] = GatedMatrix{gate_up[i].packed, gate_up[i].s_n, nullptr};
+    p.q_a = q_a, p.s_a = s_a, p.H = H, p.M = M, p.N = gate_up[0].N, p.K = K, p.act = QIFT_ACT_SILU;
+    p.probe = GatedProbe{warp, waits, static_cast<uint32_t>(limit_us * 1000ull / kNearTripNs) + 1};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return kernel == 0 ? launch_gated_stream<QIFT_LEVELS_MNZ, 1, true>(p, st) : run_gated_tc<QIFT_LEVELS_MNZ, true>(p, st);
+}
 
 int qift_gated_linear(const int8_t* q_a, const float* s_a, int M, int K, int levels, const qift_linear_output* gate_up, int activation,
                       void* H, int h_dtype, void* levels_buf, size_t levels_bytes, int levels_ready, const qift_decode_ahead* ahead,

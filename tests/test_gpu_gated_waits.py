@@ -1,0 +1,75 @@
+"""Gated kernels in which a wait runs out: what they store is right, the rest stays as it was, the host learns of it, and the next call is an ordinary one."""
+import time
+
+import pytest
+import torch
+
+import paper_2606_02823_b200 as qift
+from gated_ref import Case
+
+pytestmark = pytest.mark.gpu
+OLD = 12345.5
+FEW, TC = 0, 1
+_made = {}
+
+
+def made(M, N, K):
+    """The case of a size, and its result by an ordinary call."""
+    if (M, N, K) not in _made:
+        c = Case(M + N, M, N, K, "mnz")
+        _made[M, N, K] = c, qift.qift_gated_linear(c.q, c.s, *c.weights, c.lv)
+    return _made[M, N, K]
+
+
+def probe(kernel, warp, waits, M, N, K):
+    """-> which results were stored, [M, N]; all of them are right.  The status and the time, too."""
+    c, want = made(M, N, K)
+    assert qift.qift_device_status() == (qift.OK, 0)
+    out = torch.full((M, N), OLD, device="cuda")
+    t0 = time.perf_counter()
+    qift.qift_selftest_gated_wait(kernel, warp, waits, 1000, c.q, c.s, *c.weights, out)
+    rc, detail = qift.qift_device_status()
+    assert time.perf_counter() - t0 < 1.0, "waits of 1 ms"
+    stored = out != OLD
+    assert torch.equal(out[stored], want[stored])
+    assert rc == qift.OK or (rc == qift.ERR_TIMEOUT and detail & 0xff in ({81} if kernel == FEW else set(range(82, 90)))), (rc, hex(detail))
+    assert (rc == qift.OK) == bool(stored.all())
+    assert qift.qift_device_status() == (qift.OK, 0)
+    return stored
+
+
+def ordinary(M, N, K):
+    c, want = made(M, N, K)
+    assert torch.equal(qift.qift_gated_linear(c.q, c.s, *c.weights, c.lv), want)
+    c.check(want)
+
+
+@pytest.mark.parametrize("warp", [0, 1, 2, 4, 9, 14, 19])
+@pytest.mark.parametrize("waits", [0, 1, 2, 3, 5])
+def test_nothing_of_an_item_without_its_operands(warp, waits):
+    """Two to three items for every CTA, of more steps than there are stages: the one warp has not done its share of the first item, so nobody has sums."""
+    size = 200, 19200, 1536
+    stored = probe(TC, warp, waits, *size)
+    assert not stored.any()
+    ordinary(*size)
+
+
+def test_a_warp_that_never_waits():
+    size = 200, 19200, 1536
+    assert probe(TC, 3, 0, *size).all()
+    assert probe(TC, 9, 1 << 20, *size).all()
+
+
+@pytest.mark.parametrize("warp", [0, 1, 6, 15])
+@pytest.mark.parametrize("waits", [0, 1, 3, 1 << 20])
+def test_few_rows(warp, waits):
+    """Two or three tiles for every pair of warps, two waits each: the tiles whose sums one of the pair has not finished stay as they were."""
+    M, N, K = 5, 38400, 1536
+    stored = probe(FEW, warp, waits, M, N, K).view(M, N // 16, 16).any(2).any(0).cpu()
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    tiles = torch.arange(N // 16)
+    mine = tiles[(tiles // sms) % 8 == warp // 2]
+    done = mine // (8 * sms) < waits // 2
+    assert not stored[mine[~done]].any()                             # (of other pairs' tiles those before they learned of it)
+    assert waits < 1 << 20 or stored.all()
+    ordinary(M, N, K)

@@ -208,8 +208,10 @@ gated_tc_kernel(const __grid_constant__ GatedTcMaps maps, const __grid_constant_
                     if (++step == steps) step = 0;
                 }
             }
-            // given up: what has been asked for still arrives before the CTA ends
-            for (int i = 0; !ok && i < min(k > early ? k : early, stages); ++i) mbar_wait(&full[i], ((max(k, early) - 1 - i) / stages) & 1, 82, 1000000ull);
+            // what has been asked for arrives before the CTA ends, also where those who should wait for it have given up (and given up itself, this
+            // thread may have asked for words alone, whose stages never fill: a millisecond each)
+            const int asked = max(k, early);
+            for (int i = 0; i < min(asked, stages); ++i) mbar_wait(&full[i], ((asked - 1 - i) / stages) & 1, 82, ok ? kWaitLimitNs : 1000000ull);
         }
         __syncwarp();
     } else if (warp <= 2) {

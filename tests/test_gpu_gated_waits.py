@@ -60,6 +60,39 @@ def test_a_warp_that_never_waits():
     assert probe(TC, 9, 1 << 20, *size).all()
 
 
+@pytest.mark.parametrize("K", [256, 1024, 2048])
+@pytest.mark.parametrize("warp, waits", [(0, 0), (1, 0), (1, 1), (2, 0), (4, 0), (4, 1), (9, 0), (17, 0), (19, 1)])
+def test_calls_that_fit_the_stages(warp, waits, K):
+    """All copies of a CTA are asked for at once, so the warp that asks for them has no wait that could run out: they arrive before the CTA ends all
+    the same, and calls right behind it have their shared memory to themselves."""
+    size = 48, 1300, K
+    c, want = made(*size)
+    if K == 256 and warp in (17, 19):
+        K = 512                                                      # (a single step leaves warps of the odd ones without waits)
+        c, want = made(48, 1300, K)
+    outs = [torch.full((48, 1300), OLD, device="cuda") for _ in range(4)]
+    for out in outs[:2]:
+        qift.qift_selftest_gated_wait(TC, warp, waits, 1000, c.q, c.s, *c.weights, out)
+        qift.qift_gated_linear(c.q, c.s, *c.weights, c.lv, out=outs[2])
+    rc, detail = qift.qift_device_status()
+    assert rc == qift.ERR_TIMEOUT and 82 <= (detail & 0xff) <= 89, (rc, hex(detail))
+    assert (outs[0] == OLD).all() and (outs[1] == OLD).all() and torch.equal(outs[2], want)
+    ordinary(48, 1300, K)
+
+
+@pytest.mark.parametrize("warp, waits", [(1, 13), (2, 26), (4, 8), (9, 12), (17, 12), (0, 11)])
+def test_later_items(warp, waits):
+    """The warp stops in a later item of its CTA: those before are there, and right."""
+    size = 200, 19200, 1536
+    stored = probe(TC, warp, waits, *size)
+    items = 300
+    whole = [bool(stored[r0:min(r0 + 112, 200), n0:n0 + 128].all()) for n0 in range(0, 19200, 128) for r0 in (0, 112)]
+    some = [bool(stored[r0:min(r0 + 112, 200), n0:n0 + 128].any()) for n0 in range(0, 19200, 128) for r0 in (0, 112)]
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert len(whole) == items and whole == some and all(whole[:sms]) and not all(whole)
+    ordinary(*size)
+
+
 @pytest.mark.parametrize("warp", [0, 1, 6, 15])
 @pytest.mark.parametrize("waits", [0, 1, 3, 1 << 20])
 def test_few_rows(warp, waits):

@@ -633,6 +633,10 @@ int qift_selftest_wait_timeout(int which, unsigned int limit_us, void* stream);
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (what the kernel does not take), ALIGNMENT, WORKSPACE (more rows), CUDA. */
 int qift_selftest_gated_wait(int kernel, int warp, int waits, unsigned int limit_us, const int8_t* q_a, const float* s_a, int M, int K,
                              const qift_linear_output* gate_up, float* H, void* stream);
+/* And for the kernel on decoded levels (levels_buf as with levels_ready, from 449 rows on; MNZ, SiLU, fp32 H): every wait gives up after limit_us, in
+ * the midst of things where that is shorter than copies take.  Site byte 30 .. 35. */
+int qift_selftest_gated_pairs_wait(unsigned int limit_us, const int8_t* q_a, const float* s_a, int M, int K, const qift_linear_output* gate_up,
+                                   float* H, const void* levels_buf, size_t levels_bytes, void* stream);
 
 /* Measurement helpers (no counterpart in the paper; used by the benchmark to calibrate its roofline
  * denominators on the GPU it runs on; neither touches the quantized layer).

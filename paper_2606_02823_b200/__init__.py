@@ -16,4 +16,4 @@ from .binding import (lib, status_string, QiftError, qift_packed_bytes, qift_wor
                       Kv4FreePages, Kv4Rows, qift_kv4_pages_begin, qift_kv4_pages_end, qift_qk_norm_rope, qift_gated_levels_min_rows,
                       qift_gated_linear, qift_gated_forward, qift_lora_workspace_bytes, qift_lora_linear, qift_expand_weights, qift_expanded_linear, qift_diag_grid_quantize,
                       qift_diag_bucket_stats, qift_diag_ratio_scan_workspace_bytes, qift_diag_ratio_scan,
-                      qift_selftest_wait_timeout, qift_selftest_gated_wait, qift_levels_bytes, qift_forward_multi, qift_linear_multi)
+                      qift_selftest_wait_timeout, qift_selftest_gated_wait, qift_selftest_gated_pairs_wait, qift_levels_bytes, qift_forward_multi, qift_linear_multi)

@@ -40,7 +40,7 @@ EXPORTS = [
     "qift_gated_levels_min_rows", "qift_gated_linear", "qift_gated_forward_scratch_bytes", "qift_gated_forward",
     "qift_expand_weights", "qift_expanded_linear",
     "qift_diag_grid_quantize", "qift_diag_bucket_stats", "qift_diag_ratio_scan_workspace_bytes", "qift_diag_ratio_scan",
-    "qift_selftest_wait_timeout", "qift_selftest_gated_wait", "qift_levels_bytes", "qift_forward_multi_scratch_bytes", "qift_forward_multi",
+    "qift_selftest_wait_timeout", "qift_selftest_gated_wait", "qift_selftest_gated_pairs_wait", "qift_levels_bytes", "qift_forward_multi_scratch_bytes", "qift_forward_multi",
     "qift_linear_multi_workspace_bytes", "qift_linear_multi", "qift_calib_hbm_read", "qift_calib_mma_i8",
 ]
 
@@ -130,6 +130,7 @@ def lib() -> ctypes.CDLL:
         L.qift_diag_ratio_scan.argtypes = [vp, ctypes.c_longlong, vp, ci, vp, vp, vp, sz, vp]
         L.qift_selftest_wait_timeout.argtypes = [ci, ctypes.c_uint, vp]
         L.qift_selftest_gated_wait.argtypes = [ci, ci, ci, ctypes.c_uint, vp, vp, ci, ci, vp, vp, vp]
+        L.qift_selftest_gated_pairs_wait.argtypes = [ctypes.c_uint, vp, vp, ci, ci, vp, vp, vp, sz, vp]
         L.qift_levels_bytes.restype = sz
         L.qift_levels_bytes.argtypes = [ci, vp, ci]
         L.qift_forward_multi_scratch_bytes.restype = sz
@@ -907,6 +908,16 @@ def qift_selftest_gated_wait(kernel: int, warp: int, waits: int, limit_us: int, 
     outputs = _outputs_array([gate, up])
     _call(q_a, lib().qift_selftest_gated_wait, kernel, warp, waits, limit_us, _on(q_a, torch.int8), _on(s_a, torch.float32), M, K, ctypes.addressof(outputs),
           _on(out, torch.float32, M, gate[1].shape[0]))
+
+
+def qift_selftest_gated_pairs_wait(limit_us: int, q_a, s_a, gate, up, levels_buf, out):
+    """The same product on decoded levels into out fp32 [M, N], whose waits give up after limit_us."""
+    M, K = q_a.shape
+    assert s_a.numel() >= M, "a scale for every row"
+    _same_device(q_a, s_a, *gate, *up, levels_buf, out)
+    outputs = _outputs_array([gate, up])
+    _call(q_a, lib().qift_selftest_gated_pairs_wait, limit_us, _on(q_a, torch.int8), _on(s_a, torch.float32), M, K, ctypes.addressof(outputs),
+          _on(out, torch.float32, M, gate[1].shape[0]), *_space(levels_buf))
 
 
 # ---------------------------------------------------------------------------------------- resident decoded weights

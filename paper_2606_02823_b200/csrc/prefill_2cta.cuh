@@ -263,6 +263,11 @@ gemm_i8_pair_kernel(const __grid_constant__ PairParams p) {
                     tma_load_2d_pair(smem + s * STAGE + A_BYTES, mb, kb * kGemmBK, n0, &full[s]);
                 }
             }
+            // copies of both CTAs that are under way arrive before the pair leaves, also where those who should wait for them have given up
+            // (they are counted on the leader's barriers; its peer, given up, waits a millisecond for its own, which nobody signals)
+            for (uint32_t s = 0; leader && s < min(it, static_cast<uint32_t>(kPairStages)); ++s)
+                mbar_wait(&full[s], ((it - 1 - s) / kPairStages) & 1, 34, *fail ? 1000000ull : kWaitLimitNs);
+            if (!leader && *fail && it > 0) mbar_wait(&full[0], 0, 34, 1000000ull);
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer (leader CTA only)
@@ -294,6 +299,8 @@ gemm_i8_pair_kernel(const __grid_constant__ PairParams p) {
                 if (*fail) break;
                 tc_commit_pair(&tfull[buf]);
             }
+            // and products end before tensor memory is freed
+            if (it > 0) mbar_wait(&empty[(it - 1) % kPairStages], ((it - 1) / kPairStages) & 1, 35);
         }
     } else if (warp < 6) {
         // ------------------------------------------------------------------ epilogue warps (both CTAs)

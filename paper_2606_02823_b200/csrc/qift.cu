@@ -2224,6 +2224,22 @@ int qift_selftest_gated_wait(int kernel, int warp, int waits, unsigned int limit
     return kernel == 0 ? launch_gated_stream<QIFT_LEVELS_MNZ, 1, true>(p, st) : run_gated_tc<QIFT_LEVELS_MNZ, true>(p, st);
 }
 
+int qift_selftest_gated_pairs_wait(unsigned int limit_us, const int8_t* q_a, const float* s_a, int M, int K, const qift_linear_output* gate_up,
+                                   float* H, const void* levels_buf, size_t levels_bytes, void* stream) {
+    if (!q_a || !s_a || limit_us == 0 || limit_us > 1000000u) return QIFT_ERR_INVALID_ARG;
+    if (M < kGatedReadyMinM || K % 16 != 0) return QIFT_ERR_UNSUPPORTED_SHAPE;
+    const int rc = check_gated(M, K, QIFT_LEVELS_MNZ, gate_up, QIFT_ACT_SILU, H, QIFT_F32, levels_buf, levels_bytes, 1, nullptr);
+    if (rc != QIFT_OK) return rc;
+    if (!aligned16(q_a) || !aligned16(s_a)) return QIFT_ERR_ALIGNMENT;
+    PairCall c = {};
+    c.q_a = q_a, c.s_a = s_a, c.M = M, c.K = K, c.nseg = 2, c.H = H, c.act = QIFT_ACT_SILU, c.wait_limit_ns = limit_us * 1000ull;
+    for (int i = 0; i < 2; ++i) {
+        c.seg[i].wexp = static_cast<const int8_t*>(levels_buf) + levels_offset(K, gate_up, i);
+        c.seg[i].s_n = gate_up[i].s_n, c.seg[i].N = gate_up[i].N;
+    }
+    return run_pair_gemm(c, static_cast<cudaStream_t>(stream));
+}
+
 int qift_gated_linear(const int8_t* q_a, const float* s_a, int M, int K, int levels, const qift_linear_output* gate_up, int activation,
                       void* H, int h_dtype, void* levels_buf, size_t levels_bytes, int levels_ready, const qift_decode_ahead* ahead,
                       void* stream) {

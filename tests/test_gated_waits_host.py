@@ -19,3 +19,15 @@ def probe(L, kernel=1, warp=4, waits=0, limit=1000, q=P, s=P, M=4, K=256, H=P, p
                                         (dict(s=ODD), ALIGN), (dict(H=ODD), ALIGN), (dict(packed=4104), ALIGN)])
 def test_refused(L, bad, status):  # noqa: F811
     assert probe(L, **bad) == status
+
+
+def pairs(L, limit=1000, q=P, s=P, M=500, K=256, H=P, buf=P, bufb=1 << 40, pair=None, **kw):  # noqa: F811
+    pair = pair or outputs(**kw)
+    return L.qift_selftest_gated_pairs_wait(limit, q, s, M, K, ctypes.addressof(pair), H, buf, bufb, None)
+
+
+@pytest.mark.parametrize("bad, status", [(dict(q=NULL), ARG), (dict(s=NULL), ARG), (dict(H=NULL), ARG), (dict(limit=0), ARG), (dict(limit=1_000_001), ARG), (dict(N2=65), ARG),
+                                        (dict(M=448), SHAPE), (dict(K=24), SHAPE), (dict(buf=NULL), SPACE), (dict(bufb=2 * 64 * 256 - 1), SPACE),
+                                        (dict(buf=4224), ALIGN), (dict(q=ODD), ALIGN), (dict(s=ODD), ALIGN), (dict(H=ODD), ALIGN)])
+def test_pairs_refused(L, bad, status):  # noqa: F811
+    assert pairs(L, **bad) == status

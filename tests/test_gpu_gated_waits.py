@@ -106,3 +106,23 @@ def test_few_rows(warp, waits):
     assert not stored[mine[~done]].any()                             # (of other pairs' tiles those before they learned of it)
     assert waits < 1 << 20 or stored.all()
     ordinary(M, N, K)
+
+
+@pytest.mark.parametrize("limit", [1, 3, 20, 1_000_000])
+@pytest.mark.parametrize("M, N, K", [(450, 264, 512), (600, 9000, 4096), (2100, 3000, 1040)])
+def test_pairs_of_ctas(M, N, K, limit):
+    """Products on decoded levels whose waits are shorter than a copy, or than a call: what is stored is right, and calls right behind it are ordinary ones."""
+    c, _ = made(M, N, K)
+    buf = torch.zeros(qift.qift_levels_bytes(K, c.weights), dtype=torch.uint8, device="cuda")
+    qift.qift_gated_linear(c.q[:1].clone(), c.s[:1].clone(), *c.weights, c.lv, ahead=(c.weights, K, c.lv, buf))
+    want = qift.qift_gated_linear(c.q, c.s, *c.weights, c.lv, levels_buf=buf, levels_ready=True)
+    c.check(want)
+    out, behind = (torch.full((M, N), OLD, device="cuda") for _ in range(2))
+    for _ in range(2):
+        qift.qift_selftest_gated_pairs_wait(limit, c.q, c.s, *c.weights, buf, out)
+        qift.qift_gated_linear(c.q, c.s, *c.weights, c.lv, levels_buf=buf, levels_ready=True, out=behind)
+    rc, detail = qift.qift_device_status()
+    stored = out != OLD
+    assert torch.equal(out[stored], want[stored]) and torch.equal(behind, want)
+    assert rc == qift.OK and stored.all() or rc == qift.ERR_TIMEOUT and limit < 1_000_000 and 30 <= (detail & 0xff) <= 35, (rc, hex(detail))
+    assert qift.qift_device_status() == (qift.OK, 0)

@@ -20,14 +20,18 @@
 namespace qift {
 
 // act(g): g sigmoid(z) with z = g (SiLU) or z = 2 sqrt(2 / pi) (g + 0.044715 g^3) (GELU in its tanh form: (1 + tanh t) / 2 = sigmoid(2t)), as
-// z = g (a + b g^2) for both: no branch per output.  exp(-z) beyond the range is an infinity, and the quotient the limit, 0.  The
-// quotient is g times a reciprocal, within 2 ulp and 0 for denominators beyond 2^126: a third of the rounded division's instructions.
+// z = g (a + b g^2) for both: no branch per output.  With e = exp(-|z|), which does not overflow, the values are g / (1 + e) and g e / (1 + e):
+// those of far negative gates fade out with e, down to 2^-149.  The denominator lies in 1 .. 2, so that the quotient may be a product with
+// its reciprocal, within 2 units in the last place (a quotient that minds the range of its denominator: 512 rows, 4096 -> 14336, 58.6 us against 57.8).
 struct GateFunction {
     float a, b;
     __host__ __device__ explicit GateFunction(int act) : a(act == QIFT_ACT_SILU ? 1.0f : 1.5957691216057308f), b(act == QIFT_ACT_SILU ? 0.0f : 0.0713548162726f) {}
     __device__ __forceinline__ float operator()(float g) const {
         const float z = g * fmaf(b, fminf(g * g, 1e30f), a);
-        return __fdividef(g, 1.0f + expf(-z));
+        const float e = expf(-fabsf(z));
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));     // within one unit in the last place
+        return (z < 0.0f ? g * e : g) * r;
     }
 };
 __device__ __forceinline__ float gated_value(int acc_g, int acc_u, float s_a, float s_gate, float s_up, GateFunction act) {

@@ -850,7 +850,8 @@ def qift_gated_levels_min_rows() -> int:
     return int(lib().qift_gated_levels_min_rows())
 
 
-_GATE_UP = struct.Struct("@PPPPiiPPPPii")      # two qift_linear_output
+_GATE_UP = struct.Struct("@PPPPiiPPPPii")      # two LinearOutput, without a ctypes object per call
+assert _GATE_UP.size == 2 * ctypes.sizeof(LinearOutput), "two layouts of qift_linear_output"
 
 
 def _gated(fn, X, dtype, K, levels, gate, up, out, out_dtype, want_acc, levels_buf, levels_ready, ahead, activation, before, after):

@@ -552,7 +552,8 @@ int qift_qk_norm_rope(const void* Q, const void* K, int x_dtype, long long q_str
  * qift_gated_forward takes the activation itself, X [M,K], and rotates and quantizes it first (qift_quantize_act);
  *   scratch     dev, >= qift_gated_forward_scratch_bytes(M, K), 256-byte aligned: q_a and s_a
  * No other workspace.  The sums are exact: h follows from the accumulators in fp32, and does not depend on the route.  Scales have to be such that g
- * and u are finite.
+ * and u are finite.  Neither product leaves the call, so requests with adapters on gate or up (qift_lora_linear adds to finished products) cannot
+ * take it: for these, qift_linear_multi, the adapters, and the activation as a step of the caller's.
  * Errors: INVALID_ARG (null pointers, different N, enums, ahead), UNSUPPORTED_SHAPE, ALIGNMENT, WORKSPACE, CUDA. */
 typedef enum { QIFT_ACT_SILU = 0, QIFT_ACT_GELU_TANH = 1 } qift_activation;
 int qift_gated_levels_min_rows(void);

@@ -8,9 +8,10 @@
 // (mma_tile_step) against activations that stand in shared memory for the whole kernel; at the end of a tile one warp of the pair hands its
 // sums to the other (64-thread barrier, two buffers by turns), which writes h.
 //
-// 4096 -> 14336 in two bits: 1 row 9.6 us, 8 rows 10.0; from nine rows on there are two tiles of tokens (16 rows 13.6, INT4 16.0, three bits
-// 21.3, PoT 14.3).  The first bytes arrive some 3 us after the launch, which longer calls make up for (8192 -> 28672, 4 rows: 23.7 us, 5.0
-// TB/s).
+// 4096 -> 14336, 1 row and 8: two bits 9.4 us and 10.2, PoT 12.0 and 12.8, three bits 12.3 and 12.8, INT4 11.8 and 12.8.  From nine rows on there
+// are two tiles of tokens, and this kernel is left with calls of fewer channels and PoT (16 rows: PoT 14.5; 4096 -> 9472: two bits 11.0,
+// three bits 13.3, PoT 11.4; 4096 -> 4736: INT4 11.0).  The first bytes arrive some 3 us after the launch, which longer calls make up for
+// (8192 -> 28672, 4 rows: 23.4 us, 5.0 TB/s).  PoT: the table lookup (7 rows, under the profiler: ALU 49 %, issue 40 %; two bits 26 and 30).
 //
 // The CTA itself turns q_a into the operands' order (even planes times four, or table order) and sums each token's values, so there is no
 // launch before this one and no workspace.

@@ -6,7 +6,8 @@
 //
 //   warp 0        fills a ring of steps (256 codes deep) with tensor copies: the packed words of both matrices (three dimensions: a row's 64
 //                 bytes of a slice, swizzled; rows; blocks of sixteen rows) and the q_a rows of the token block, two 128-byte k-blocks
-//   warps 1, 2    issue the products D[matrix][128 channels x tokens] of a matrix each, eight a step
+//   warps 1, 2    issue the products D[matrix][128 channels x tokens] of a matrix each, eight a step (here and above one elected thread of a
+//                 warp does it all: with a vote of the lanes after each wait 48 rows took 14.2 us)
 //   warps 4-19    expanders, two per matrix and lane quarter, for the even and the odd steps: the packed words of their 32 channels, one to
 //                 four operations per operand word, tcgen05.st into their slot of the matrix's operands; then the epilogue, four per
 //                 lane quarter on 8-token pieces by turns: both accumulators, h, stores of 32 channels
@@ -25,8 +26,8 @@
 // step is expanded meanwhile (each step shared between both: 8 to 15 % longer over 8192 codes; a hand-over per 128 codes: 15 to 25 %).  A
 // thread that a whole warp has elected issues a product in 16 cycles; one that a comparison of lanes has picked takes 60 (the compiler
 // cannot know it is alone, and tries every lane's operands), which alone set the pace at first: 23 us for 48 rows.  Waits carry no time
-// hint (with one they are a loop around a sleep) and are bounded by their trips.  4096 -> 14336 in two bits: 9 rows 11.3 us, 48 rows
-// 13.0, 128 rows 17.8, 512 rows 57; of 48 rows 1.5 us are the epilogue (issue: 35 instructions an output).
+// hint (with one they are a loop around a sleep) and are bounded by their trips.  4096 -> 14336 in two bits: 9 rows 11.0 us, 48 rows
+// 12.8, 128 rows 17.8, 512 rows 57.5.
 #pragma once
 
 #include "common.cuh"

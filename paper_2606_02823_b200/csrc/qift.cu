@@ -1979,6 +1979,7 @@ int run_qk_rope(const RopeParams& p, bool near, int lanes, dim3 grid, cudaStream
 // are and decoded; 4096 -> 14336 in two bits: 768 rows 75 and 98, 1024 rows 104 and 112, 1536 rows 151 to 181 and 164, 4096 rows 479 and 352;
 // three bits: 1024 rows 124 and 120; 8192 -> 28672: 1024 rows 365 and 421, 1536 rows 614 and 582, 2048 rows 806 and 744) and with levels that are
 // there already (384 rows 47 and 48, 512 rows 60 and 50, 1024 rows 104 and 83; 8192 -> 28672: 384 rows 136 and 177, 512 rows 199 and 165).
+// One count for all widths, since callers ask for it before they know the layer: wide layers lose up to 15 % from it to some 1500 rows.
 constexpr int kGatedLevelsMinM = 1025, kGatedReadyMinM = 449;
 inline bool gated_by_levels(int M, int K, int levels_ready) { return K % 16 == 0 && M >= (levels_ready ? kGatedReadyMinM : kGatedLevelsMinM); }
 
